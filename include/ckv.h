@@ -94,7 +94,8 @@ typedef enum ckv_entry {
   CKV_ENTRY_CRITICAL_KV_ATTN = 3,
   CKV_ENTRY_CORRECTED_ATTN = 4,
   CKV_ENTRY_DUAL_TOKEN_ATTN = 5,
-  CKV_ENTRY_DECODE_STEP = 6  /* ckv_decode_step with any kind of layer */
+  CKV_ENTRY_DECODE_STEP = 6, /* ckv_decode_step with any kind of layer */
+  CKV_ENTRY_PAGED_DECODE_ATTN = 7  /* k: the number of query tokens */
 } ckv_entry;
 
 typedef struct ckv_shape {
@@ -359,6 +360,179 @@ int ckv_chunked_kv_attn(const ckv_shape* shape, int32_t chunk, const uint16_t* q
                         int32_t* n_rows, float* out, void* ws, size_t ws_bytes,
                         void* stream);
 
+/* ---- rotary positions --------------------------------------------------------
+ * Rotary position embedding of query and key rows.  With n = rot_dim, pair i
+ * (0 <= i < n/2) of a head row holds the elements
+ *   CKV_ROPE_HALF          x[i], x[i + n/2]
+ *   CKV_ROPE_INTERLEAVED   x[2i], x[2i + 1]
+ * and a token at position p turns it by the angle a = p * inv_freq[i]:
+ *   y1 = scale * (x1 cos a - x2 sin a),   y2 = scale * (x2 cos a + x1 sin a);
+ * elements from rot_dim on are copied.  With inverse set the angle is -a.
+ * The gradient of a rotation is the same call on the outputs' gradients with
+ * inverse set (and the same scale); a rotation is undone with inverse set and
+ * 1 / scale.  Angles are formed and reduced in fp64 (an angle a is off by less
+ * than 2^-51 |a|, so by less than an fp32 step up to 2^26 radians); sines,
+ * cosines and products are fp32, rounded once to the rows' type (nearest, ties
+ * to even).  Any int32 position will do. */
+typedef enum ckv_rope_layout { CKV_ROPE_HALF = 0, CKV_ROPE_INTERLEAVED = 1 } ckv_rope_layout;
+typedef enum ckv_rope_type { CKV_ROPE_BF16 = 0, CKV_ROPE_F32 = 1 } ckv_rope_type;
+
+typedef struct ckv_rope {
+  const double* inv_freq; /* [rot_dim / 2] device, radians per position         */
+  int32_t head_dim;       /* elements of a head row: 8 .. 1024, multiple of 8   */
+  int32_t rot_dim;        /* elements that are rotated: even, 2 .. head_dim     */
+  int32_t layout;         /* ckv_rope_layout                                    */
+  int32_t type;           /* ckv_rope_type of the rows                          */
+  int32_t inverse;        /* 0: by the angle, 1: back by the angle              */
+  float scale;            /* factor of the rotated elements (finite, normally 1) */
+} ckv_rope;
+
+/* Head rows of num_tokens tokens: row (token, head) at element token *
+ * token_stride + head * head_stride, its elements adjacent.  Strides are
+ * multiples of 16 bytes, so rows may be slices of one projection's output.
+ * dst is src (in place, the same strides) or does not overlap it. */
+typedef struct ckv_rows {
+  const void* src;
+  void* dst;
+  int64_t src_token_stride, src_head_stride;
+  int64_t dst_token_stride, dst_head_stride;
+  int32_t heads;
+  int32_t reserved;       /* must be 0 */
+} ckv_rows;
+
+/* Rotates the rows of q and, if k is not NULL, of k, token t by positions[t]
+ * (int32, device), in one launch.  0 <= num_tokens <= 2^24; at most 4096
+ * heads in q and k together. */
+int ckv_rope_rows(const ckv_rope* rope, int32_t num_tokens, const int32_t* positions,
+                  const ckv_rows* q, const ckv_rows* k, void* stream);
+
+/* The frequencies of ckv_rope, on the host: inv_freq[i] = base^(-2i/rot_dim)
+ * for i < rot_dim / 2 (fp64), stretched for contexts `factor` times longer
+ * than the orig_ctx positions a model was trained on, as scaling says (NULL:
+ * CKV_ROPE_PLAIN).  With f the plain frequency:
+ *   CKV_ROPE_LINEAR  f / factor
+ *   CKV_ROPE_BASE    the base times factor^(rot_dim / (rot_dim - 2)), so that the
+ *                    slowest pair is stretched by factor and the fastest kept
+ *                    (rot_dim > 2)
+ *   CKV_ROPE_BANDS   by the turns r = orig_ctx * f / 2 pi a pair makes over the
+ *                    original context: f from `high` turns up, f / factor up to
+ *                    `low` turns, linear in r between (0 <= low < high)
+ *   CKV_ROPE_RAMP    the same with the ramp linear in the pair's index between
+ *                    the floor of the index that makes `high` turns and the
+ *                    ceiling of the one that makes `low` turns, both kept in
+ *                    [0, rot_dim - 1] (0 < low < high; arXiv 2309.00071)
+ * *rot_scale (may be NULL) gets the factor for ckv_rope.scale: 0.1 ln(factor) + 1
+ * for CKV_ROPE_RAMP with factor > 1, else 1.  base > 1, factor >= 1. */
+typedef enum ckv_rope_stretch {
+  CKV_ROPE_PLAIN = 0,
+  CKV_ROPE_LINEAR = 1,
+  CKV_ROPE_BASE = 2,
+  CKV_ROPE_BANDS = 3,
+  CKV_ROPE_RAMP = 4
+} ckv_rope_stretch;
+
+typedef struct ckv_rope_scaling {
+  int32_t kind;      /* ckv_rope_stretch                             */
+  int32_t orig_ctx;  /* CKV_ROPE_BANDS, CKV_ROPE_RAMP: at least 1    */
+  double factor, low, high;
+} ckv_rope_scaling;
+
+int ckv_rope_frequencies(int32_t rot_dim, double base, const ckv_rope_scaling* scaling,
+                         double* inv_freq, float* rot_scale);
+
+/* ---- paged cache --------------------------------------------------------------
+ * K and V rows of all requests in pages of page_size positions: position p of
+ * request b is row p % page_size of page page_table[b][p / page_size].  An
+ * entry outside [0, num_pages) (-1: evicted, or not yet allocated) means that
+ * the page's positions are not there: they are not attended, score -inf, and
+ * are neither read nor written.  Requests may share pages.
+ *   k_pages, v_pages  row r of page g, KV head h at element
+ *                     g * page_stride + h * head_stride + r * row_stride, so
+ *                     that [page][head][row][d], [page][row][head][d] and K|V
+ *                     interleaved pools are all strides of one kind
+ *   CKV_CACHE_BF16    16-bit elements
+ *   CKV_CACHE_E4M3    8-bit e4m3 codes (no infinities; 0x7f and 0xff are NaN)
+ *                     with one exponent byte a row, k_exps / v_exps
+ *                     [num_pages][Hkv][page_size]: an element is code *
+ *                     2^(byte - 127)
+ * Strides are multiples of 16 bytes and at least 128 elements; page_size is a
+ * power of two up to 65536, and page_size * row_stride elements take less than
+ * 2^31 bytes.  Entries of page_table past ceil(n_b / page_size) are not used.
+ * Rows at or past n_b may hold anything; rows below it are finite.  ckv_shape
+ * gives batch, heads and max_ctx (its row strides are checked and not used);
+ * positions live in [0, max_ctx). */
+typedef enum ckv_cache_kind { CKV_CACHE_BF16 = 0, CKV_CACHE_E4M3 = 1 } ckv_cache_kind;
+
+typedef struct ckv_paged_cache {
+  void* k_pages;
+  void* v_pages;
+  uint8_t* k_exps;            /* CKV_CACHE_E4M3, else NULL */
+  uint8_t* v_exps;
+  const int32_t* page_table;  /* [B][table_stride] device  */
+  int64_t page_stride, head_stride, row_stride; /* elements */
+  int32_t kind;               /* ckv_cache_kind            */
+  int32_t page_size;
+  int32_t num_pages;          /* at least 1                */
+  int32_t table_stride;       /* >= ceil(max_ctx / page_size) */
+} ckv_paged_cache;
+
+/* Writes the K and V rows of num_tokens tokens into their pages: token t goes
+ * to position positions[t] of request requests[t] (NULL: request t).  k, v:
+ * [num_tokens][Hkv][d] bf16 at token stride kv_token_stride elements (a
+ * multiple of 8, at least Hkv * d).  A token whose position is outside
+ * [0, max_ctx) (-1: padding), whose request is outside [0, B) or whose page is
+ * not there is not written.  Positions written by one call are distinct (the
+ * bytes of a row written twice are unspecified, inside the row).  All other
+ * rows keep their bytes.
+ *   With rope (bf16, head_dim 128), K rows are turned by their positions on the
+ * way, in fp32, and rounded once to what is stored; with q as well, the query
+ * rows of the same tokens (all of them, padding included) are rotated as
+ * ckv_rope_rows does, in the same launch.
+ *   CKV_CACHE_BF16 rows that are not rotated keep their bits.  CKV_CACHE_E4M3:
+ * with amax the largest finite |x| of the row and e the smallest integer in
+ * [-127, 127] with amax <= 448 * 2^e, the byte e + 127 and the codes of x /
+ * 2^e (exact) rounded to nearest, ties to even; an infinity or NaN is stored as
+ * NaN.  A power of two loses nothing: e4m3's own exponent carries the rest. */
+int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t num_tokens,
+                    const int32_t* requests, const int32_t* positions, const uint16_t* k,
+                    const uint16_t* v, int64_t kv_token_stride, const ckv_rope* rope,
+                    const ckv_rows* q, void* stream);
+
+/* Reads rows of a paged cache back as bf16 (values of CKV_CACHE_E4M3 rows are
+ * exact, or rounded where they fall among bf16's subnormals):
+ *   idx NULL:  slot i < min(k, n_b) of k_dst/v_dst [B][Hkv][k][d] gets position i;
+ *   idx given: slot i < n_sel[b][h] (clamped to [0, k]) gets position
+ *              idx[b][h][i], as ckv_gather_kv does from a dense cache; entries
+ *              outside [0, n_b) are skipped.
+ * Slots past the count, and of positions that are not there, are not written.
+ * n_sel is NULL exactly when idx is. */
+int ckv_paged_read(const ckv_shape* shape, const ckv_paged_cache* cache,
+                   const int32_t* ctx_lens, const int32_t* idx, const int32_t* n_sel, int32_t k,
+                   uint16_t* k_dst, uint16_t* v_dst, void* stream);
+
+/* ckv_score_keys over paged keys: scores [B][Hkv][max_ctx]; positions at or
+ * past n_b, and those not there, get -inf. */
+int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
+                         const uint16_t* q, const int32_t* ctx_lens, float scale,
+                         float* scores, void* stream);
+
+/* Attention of the last num_tokens tokens of every request over everything it
+ * has in its pages (their own rows included, so they are written first).  With
+ * T = num_tokens, token t (0 <= t < T) is position n_b - T + t and attends to the
+ * positions p <= n_b - T + t that are there:
+ *   l_p = scale * q[b][t][g] . K_p,   out[b][t][g] = sum_p softmax(l)_p V_p,
+ *   lse[b][t][g] = log sum_p exp(l_p)        (natural logarithm; may be NULL)
+ * q [B][T][Hq][d] bf16, out [B][T][Hq][d] fp32, lse [B][T][Hq] fp32.  A token
+ * with nothing to attend to gets out = 0 and lse = -inf.  Logits, weights and
+ * sums are fp32.  T >= 1 and T * G <= 16.  The positions of all units are cut
+ * into equal ranges, one a workgroup; a unit that ranges share is joined by a
+ * second launch, in a fixed order: the same call gives the same bits.
+ * Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
+int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
+                          int32_t num_tokens, const uint16_t* q, const int32_t* ctx_lens,
+                          float scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                          void* stream);
+
 /* ---- layer pipeline --------------------------------------------------------
  * The decode loop of Sec. 5.3 (layer-aware transfer overlap) and Sec. 5.4
  * (two-layer ping-pong buffer): the set selected for a layer at step t-1 is
@@ -520,10 +694,18 @@ typedef enum ckv_kernel_id {
   CKV_K_SELECT_ATTN = 13, /* same-step selection and attention in one launch */
   CKV_K_PROBE = 14,   /* read-rate probe (ckv_probe_read_rows)              */
   CKV_K_CRITICAL = 15, /* same-step scoring, selection and attention in one launch */
-  CKV_K_COUNT = 16
+  CKV_K_COUNT = 16,    /* classes that ckv_profile_end reports                */
+  CKV_K_ROPE = 16,        /* rotary positions                               */
+  CKV_K_PAGED_WRITE = 17, /* rows (and rotated queries) into a paged cache  */
+  CKV_K_PAGED_READ = 18,  /* rows out of a paged cache                      */
+  CKV_K_PAGED_SCORE = 19, /* scores of paged keys                           */
+  CKV_K_PAGED_ATTN = 20,  /* attention over a paged cache, by ranges        */
+  CKV_K_PAGED_MERGE = 21, /* join of the ranges that share a unit           */
+  CKV_K_TOTAL = 22        /* all classes (ckv_profile_end_n)                */
 } ckv_kernel_id;
 
-#define CKV_K_ALL ((1u << CKV_K_COUNT) - 1u)
+#define CKV_K_ALL ((1u << CKV_K_COUNT) - 1u)     /* those of ckv_profile_end */
+#define CKV_K_EVERY ((1u << CKV_K_TOTAL) - 1u)
 
 typedef struct ckv_kernel_stats {
   int64_t launches;   /* dispatches of this kernel class                    */
@@ -549,6 +731,12 @@ int ckv_profile_begin_sampled(uint32_t kernel_mask, uint32_t every);
  * entry per ckv_kernel_id into stats[0 .. CKV_K_COUNT). */
 int ckv_profile_end(ckv_kernel_stats* stats);
 
+/* ckv_profile_end for the first `count` classes (1 <= count <= CKV_K_TOTAL,
+ * else CKV_EINVAL and recording goes on): stats[0 .. count).  The classes
+ * from CKV_K_COUNT on are recorded when their bits are in the mask and
+ * reported here only, so that the array of ckv_profile_end keeps its size. */
+int ckv_profile_end_n(ckv_kernel_stats* stats, int count);
+
 /* ---- debug mode -----------------------------------------------------------
  * For development, not for serving (on: nonzero; process-wide; off by default,
  * on by default in a library built with -DCKV_DEBUG).  In debug mode every
@@ -559,7 +747,10 @@ int ckv_profile_end(ckv_kernel_stats* stats);
  *   0 <= n_sel[u] <= k for an input count (n_sel, n_sel_in, n_pred);
  *   entries 0 .. n_sel[u] - 1 of an input index set (idx, idx_in, idx_pred;
  *   all k without a count) are -1 or positions below the unit's context
- *   length (below max_ctx where the entry takes no ctx_lens).
+ *   length (below max_ctx where the entry takes no ctx_lens);
+ *   page_table entries of positions below n_b are -1 or in [0, num_pages);
+ *   written tokens: positions[t] is -1 or in [0, max_ctx), and then
+ *   requests[t] is in [0, B) and the page's entry in [0, num_pages).
  * Outside debug mode these are the caller's preconditions, and kernels only
  * clamp what they read.  Every kernel launch then also synchronises its
  * stream, so that a failing kernel is reported by the entry that launched it

@@ -30,6 +30,11 @@ __all__ = [
     "EXPORTS", "probe_read_rows", "probe_sink_words", "PROBE_STANDALONE", "PROBE_ROW_HALVES",
     "PROBE_HEAD_HALVES", "set_debug", "set_one_launch_same_step", "ONE_LAUNCH_OFF",
     "ONE_LAUNCH_ROW_HALVES", "ONE_LAUNCH_HEAD_HALVES",
+    "Rope", "rope_for", "rope_frequencies", "Rows", "rows_for", "rope_rows",
+    "ROPE_HALF", "ROPE_INTERLEAVED", "ROPE_BF16", "ROPE_F32", "ROPE_PLAIN", "ROPE_LINEAR",
+    "ROPE_BASE", "ROPE_BANDS", "ROPE_RAMP", "PagedCache", "paged_cache_for", "paged_write",
+    "paged_read", "paged_score_keys", "paged_decode_attn", "CACHE_BF16", "CACHE_E4M3",
+    "ENTRY_PAGED_DECODE_ATTN",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libckv.so")
@@ -37,6 +42,7 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libckv.so")
 SRC_DEVICE, SRC_HOST_PINNED = 0, 1
 ENTRY_SELECT_TOPK, ENTRY_SPARSE_DECODE_ATTN, ENTRY_CRITICAL_KV_ATTN = 1, 2, 3
 ENTRY_CORRECTED_ATTN, ENTRY_DUAL_TOKEN_ATTN, ENTRY_DECODE_STEP = 4, 5, 6
+ENTRY_PAGED_DECODE_ATTN = 7  # workspace_bytes: k is the number of query tokens
 PROBE_STANDALONE, PROBE_ROW_HALVES, PROBE_HEAD_HALVES = 0, 1, 2
 EXPORTS = ("ckv_abi_version", "ckv_status_str", "ckv_last_error_detail",
            "ckv_workspace_bytes", "ckv_score_keys", "ckv_select_topk",
@@ -46,13 +52,15 @@ EXPORTS = ("ckv_abi_version", "ckv_status_str", "ckv_last_error_detail",
            "ckv_chunked_kv_attn", "ckv_dual_token_attn", "ckv_reconstruct_keys",
            "ckv_corrected_attn_lowrank",
            "ckv_kernel_name", "ckv_profile_begin", "ckv_profile_begin_sampled",
-           "ckv_profile_end",
+           "ckv_profile_end", "ckv_profile_end_n",
            "ckv_pipeline_create", "ckv_pipeline_destroy", "ckv_pipeline_set_gather_width",
            "ckv_pipeline_set_checks",
            "ckv_pipeline_prime",
            "ckv_decode_step", "ckv_probe_read_rows", "ckv_probe_sink_words", "ckv_set_debug",
-           "ckv_set_one_launch_same_step")
-KERNEL_COUNT = 16
+           "ckv_set_one_launch_same_step", "ckv_rope_rows", "ckv_rope_frequencies",
+           "ckv_paged_write", "ckv_paged_read", "ckv_paged_score_keys",
+           "ckv_paged_decode_attn")
+KERNEL_COUNT = 22
 MAX_RANK = 4096
 ABI_VERSION = 9  # CKV_ABI_VERSION of include/ckv.h that this binding marshals for
 
@@ -87,6 +95,39 @@ class Shape(ctypes.Structure):
                 ("max_ctx", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("key_row_stride", ctypes.c_int64),
                 ("kv_row_stride", ctypes.c_int64)]
+
+
+class Rope(ctypes.Structure):
+    """Mirror of ``ckv_rope``."""
+    _fields_ = [("inv_freq", ctypes.c_void_p), ("head_dim", ctypes.c_int32),
+                ("rot_dim", ctypes.c_int32), ("layout", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class RopeScaling(ctypes.Structure):
+    """Mirror of ``ckv_rope_scaling``."""
+    _fields_ = [("kind", ctypes.c_int32), ("orig_ctx", ctypes.c_int32),
+                ("factor", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double)]
+
+
+class Rows(ctypes.Structure):
+    """Mirror of ``ckv_rows``."""
+    _fields_ = [("src", ctypes.c_void_p), ("dst", ctypes.c_void_p),
+                ("src_token_stride", ctypes.c_int64), ("src_head_stride", ctypes.c_int64),
+                ("dst_token_stride", ctypes.c_int64), ("dst_head_stride", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("reserved", ctypes.c_int32)]
+
+
+class PagedCache(ctypes.Structure):
+    """Mirror of ``ckv_paged_cache``."""
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("k_exps", ctypes.c_void_p), ("v_exps", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("kind", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("num_pages", ctypes.c_int32), ("table_stride", ctypes.c_int32)]
 
 
 def _load() -> ctypes.CDLL:
@@ -132,6 +173,21 @@ def _load() -> ctypes.CDLL:
         "ckv_profile_begin": (ctypes.c_int, [ctypes.c_uint32]),
         "ckv_profile_begin_sampled": (ctypes.c_int, [ctypes.c_uint32, ctypes.c_uint32]),
         "ckv_profile_end": (ctypes.c_int, [ctypes.POINTER(KernelStats)]),
+        "ckv_profile_end_n": (ctypes.c_int, [ctypes.POINTER(KernelStats), ctypes.c_int]),
+        "ckv_rope_rows": (ctypes.c_int, [ctypes.POINTER(Rope), i32, vp, ctypes.POINTER(Rows),
+                                         ctypes.POINTER(Rows), vp]),
+        "ckv_rope_frequencies": (ctypes.c_int, [i32, ctypes.c_double,
+                                                ctypes.POINTER(RopeScaling), vp,
+                                                ctypes.POINTER(ctypes.c_float)]),
+        "ckv_paged_write": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), i32, vp, vp, vp, vp,
+                                           ctypes.c_int64, ctypes.POINTER(Rope),
+                                           ctypes.POINTER(Rows), vp]),
+        "ckv_paged_read": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), vp, vp, vp, i32, vp,
+                                          vp, vp]),
+        "ckv_paged_score_keys": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), vp, vp,
+                                                ctypes.c_float, vp, vp]),
+        "ckv_paged_decode_attn": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), i32, vp, vp,
+                                                 ctypes.c_float, vp, vp, vp, sz, vp]),
         "ckv_probe_read_rows": (ctypes.c_int, [sp, vp, vp, vp, i32, ctypes.c_int, vp, sz, vp]),
         "ckv_probe_sink_words": (sz, [sp, i32, ctypes.c_int]),
         "ckv_set_debug": (ctypes.c_int, [ctypes.c_int]),
@@ -331,10 +387,228 @@ def chunked_kv_attn(shape: Shape, chunk: int, q_att, q_sel, landmarks, ctx_lens,
         ws.numel() if ws is not None else 0, _stream(stream)))
 
 
+# ---- rotary positions and the paged cache -------------------------------------------
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_BF16, ROPE_F32 = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
+CACHE_BF16, CACHE_E4M3 = 0, 1
+
+
+class _On:
+    """Makes a tensor's device current for a call and gives the stream to call
+    on: the caller's, or that device's current one."""
+
+    def __init__(self, t: torch.Tensor, stream):
+        self.dev, self.stream, self.back = t.device, stream, None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.dev.index:
+            self.back = torch.cuda.current_device()
+            torch.cuda.set_device(self.dev)
+        return _stream(self.stream)
+
+    def __exit__(self, *exc):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
+
+
+def _int32(name: str, t: torch.Tensor, n: int) -> None:
+    """What the kernels index by has to be int32, dense and long enough."""
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: a dense int32 tensor of {n} elements, not {t.dtype} "
+                         f"{tuple(t.shape)}")
+
+
+def rope_frequencies(rot_dim: int, base: float, kind: int = ROPE_PLAIN, factor: float = 1.0,
+                     orig_ctx: int = 0, low: float = 0.0, high: float = 0.0):
+    """``ckv_rope_frequencies``: (float64 CPU tensor of rot_dim / 2 radians per
+    position, the factor for the rotated elements)."""
+    out = torch.empty(max(rot_dim // 2, 1), dtype=torch.float64)
+    s = RopeScaling(kind, orig_ctx, factor, low, high)
+    scale = ctypes.c_float(1.0)
+    _check("ckv_rope_frequencies", _lib.ckv_rope_frequencies(
+        rot_dim, base, ctypes.byref(s), out.data_ptr(), ctypes.byref(scale)))
+    return out, scale.value
+
+
+def rope_for(inv_freq: torch.Tensor, head_dim: int = 128, rot_dim: Optional[int] = None,
+             layout: int = ROPE_HALF, dtype: int = ROPE_BF16, inverse: bool = False,
+             scale: float = 1.0) -> Rope:
+    """The rotation handle over a device tensor of float64 frequencies (kept
+    alive by the handle)."""
+    rot = 2 * inv_freq.numel() if rot_dim is None else rot_dim
+    if inv_freq.dtype != torch.float64 or not inv_freq.is_contiguous() or \
+            2 * inv_freq.numel() < rot:
+        raise ValueError(f"inv_freq: {rot // 2} dense float64 frequencies")
+    r = Rope(inv_freq.data_ptr(), head_dim, rot, layout, dtype, int(inverse), scale)
+    r.keep = inv_freq
+    return r
+
+
+def rows_for(src: torch.Tensor, dst: Optional[torch.Tensor] = None) -> Rows:
+    """Head rows [tokens][heads][d] of one tensor (any token and head strides)
+    into those of another of the same shape, or in place."""
+    dst = src if dst is None else dst
+    if src.dim() != 3 or src.shape != dst.shape or src.dtype != dst.dtype or \
+            src.stride(2) != 1 or dst.stride(2) != 1:
+        raise ValueError(f"rows: [tokens][heads][d] with adjacent elements, the same twice, not "
+                         f"{tuple(src.shape)} and {tuple(dst.shape)}")
+    r = Rows(src.data_ptr(), dst.data_ptr(), src.stride(0), src.stride(1), dst.stride(0),
+             dst.stride(1), src.shape[1], 0)
+    r.keep = (src, dst)
+    return r
+
+
+_ROPE_TYPES = {torch.bfloat16: ROPE_BF16, torch.float32: ROPE_F32}
+
+
+def _rows_ok(name: str, rows: Rows, rope: Rope, n: int) -> None:
+    if not hasattr(rows, "keep"):
+        return  # filled in by hand
+    t = rows.keep[0]
+    if t.shape[0] < n or t.shape[2] != rope.head_dim or _ROPE_TYPES.get(t.dtype) != rope.type:
+        raise ValueError(f"{name}: {n} tokens of rows of {rope.head_dim} elements of the rope's "
+                         f"type, not {t.dtype} {tuple(t.shape)}")
+
+
+def rope_rows(rope: Rope, positions: torch.Tensor, q: Rows, k: Optional[Rows] = None,
+              stream=None) -> None:
+    """Rotates the head rows of q (and k) by their tokens' positions."""
+    n = positions.numel()
+    _int32("positions", positions, n)
+    _rows_ok("q", q, rope, n)
+    if k is not None:
+        _rows_ok("k", k, rope, n)
+    with _On(positions, stream) as s:
+        _check("ckv_rope_rows", _lib.ckv_rope_rows(rope, n, positions.data_ptr(), q, k, s))
+
+
+def paged_cache_for(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                    k_exps: Optional[torch.Tensor] = None,
+                    v_exps: Optional[torch.Tensor] = None) -> PagedCache:
+    """The handle of a paged cache: pages as [pages][Hkv][page_size][d] views
+    of one pair of strides (bf16, or uint8 / float8_e4m3fn codes with uint8
+    exponents [pages][Hkv][page_size]), page_table [B][pages per request].
+    The handle keeps the tensors alive."""
+    if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or \
+            k_pages.stride() != v_pages.stride() or k_pages.dtype != v_pages.dtype or \
+            k_pages.stride(3) != 1 or k_pages.shape[3] != 128:
+        raise ValueError("k_pages, v_pages: [pages][Hkv][page_size][128], alike, rows dense")
+    kind = CACHE_BF16 if k_pages.element_size() == 2 else CACHE_E4M3
+    if k_pages.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
+        raise ValueError(f"pages of {k_pages.dtype}")
+    for e in (k_exps, v_exps):
+        if (e is not None) != (kind == CACHE_E4M3) or (e is not None and (
+                e.dtype != torch.uint8 or e.shape != k_pages.shape[:3] or not e.is_contiguous())):
+            raise ValueError("k_exps, v_exps: dense uint8 [pages][Hkv][page_size] of e4m3 pages")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.stride(1) != 1:
+        raise ValueError("page_table: int32 [B][pages]")
+    c = PagedCache(k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exps), _ptr(v_exps),
+                   page_table.data_ptr(), *(_stride(k_pages, i) for i in range(3)), kind,
+                   k_pages.shape[2], k_pages.shape[0],
+                   page_table.shape[1] if page_table.shape[0] == 1 else page_table.stride(0))
+    c.keep = (k_pages, v_pages, page_table, k_exps, v_exps)
+    return c
+
+
+def _stride(t: torch.Tensor, i: int) -> int:
+    """A dimension's stride; of one that holds a single entry any will do."""
+    return t.stride(i) if t.shape[i] > 1 else max(t.stride(i), t.shape[3])
+
+
+def _cache_ok(shape: Shape, cache: PagedCache) -> None:
+    if not hasattr(cache, "keep"):
+        return  # filled in by hand
+    pages, table = cache.keep[0], cache.keep[2]
+    if pages.shape[1] != shape.num_kv_heads or table.shape[0] < shape.batch:
+        raise ValueError(f"a cache of {pages.shape[1]} heads and {table.shape[0]} requests for a "
+                         f"shape of {shape.num_kv_heads} and {shape.batch}")
+
+
+def paged_write(shape: Shape, cache: PagedCache, requests, positions: torch.Tensor,
+                k: torch.Tensor, v: torch.Tensor, rope: Optional[Rope] = None,
+                q: Optional[Rows] = None, stream=None) -> None:
+    """Writes k, v [tokens][Hkv][128] into their pages (requests None: token t
+    is request t's); with rope, keys (and the rows of q) are rotated."""
+    n = positions.numel()
+    _cache_ok(shape, cache)
+    _int32("positions", positions, n)
+    if requests is not None:
+        _int32("requests", requests, n)
+    want = (n, shape.num_kv_heads, 128)
+    if k.shape != want or v.shape != want or k.stride() != v.stride() or k.stride(2) != 1 or \
+            (k.stride(1) != 128 and want[1] > 1) or k.dtype != torch.bfloat16 or \
+            v.dtype != torch.bfloat16:
+        raise ValueError(f"k, v: bf16 {want} with dense heads, not {k.dtype} {tuple(k.shape)}")
+    if q is not None and rope is not None:
+        _rows_ok("q", q, rope, n)
+    stride = k.stride(0) if n > 1 else max(k.stride(0), 128 * want[1])
+    with _On(positions, stream) as s:
+        _check("ckv_paged_write", _lib.ckv_paged_write(
+            shape, cache, n, _ptr(requests), positions.data_ptr(), k.data_ptr(), v.data_ptr(),
+            stride, rope, q, s))
+
+
+def paged_read(shape: Shape, cache: PagedCache, ctx_lens: torch.Tensor, idx, n_sel, k: int,
+               k_dst: torch.Tensor, v_dst: torch.Tensor, stream=None) -> None:
+    """Rows idx of the pages (idx None: positions 0 .. k - 1) into k_dst, v_dst
+    [B][Hkv][k][128] bf16."""
+    _cache_ok(shape, cache)
+    _int32("ctx_lens", ctx_lens, shape.batch)
+    units = shape.batch * shape.num_kv_heads
+    if idx is not None:
+        _int32("idx", idx, units * k)
+    if n_sel is not None:
+        _int32("n_sel", n_sel, units)
+    for t in (k_dst, v_dst):
+        if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.numel() < units * k * 128:
+            raise ValueError(f"k_dst, v_dst: dense bf16 of {units * k * 128} elements")
+    with _On(ctx_lens, stream) as s:
+        _check("ckv_paged_read", _lib.ckv_paged_read(
+            shape, cache, ctx_lens.data_ptr(), _ptr(idx), _ptr(n_sel), k, k_dst.data_ptr(),
+            v_dst.data_ptr(), s))
+
+
+def _dense(name: str, t: torch.Tensor, dtype, n: int) -> None:
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
+        raise ValueError(f"{name}: a dense {dtype} tensor of {n} elements, not {t.dtype} "
+                         f"{tuple(t.shape)}")
+
+
+def paged_score_keys(shape: Shape, cache: PagedCache, q: torch.Tensor, ctx_lens: torch.Tensor,
+                     scale: float, scores: torch.Tensor, stream=None) -> None:
+    _cache_ok(shape, cache)
+    _int32("ctx_lens", ctx_lens, shape.batch)
+    _dense("q", q, torch.bfloat16, shape.batch * shape.num_q_heads * 128)
+    _dense("scores", scores, torch.float32, shape.batch * shape.num_kv_heads * shape.max_ctx)
+    with _On(ctx_lens, stream) as s:
+        _check("ckv_paged_score_keys", _lib.ckv_paged_score_keys(
+            shape, cache, q.data_ptr(), ctx_lens.data_ptr(), scale, scores.data_ptr(), s))
+
+
+def paged_decode_attn(shape: Shape, cache: PagedCache, num_tokens: int, q: torch.Tensor,
+                      ctx_lens: torch.Tensor, scale: float, out: torch.Tensor, lse, ws,
+                      stream=None) -> None:
+    """Attention of the last num_tokens tokens (q [B][T][Hq][128]) over the
+    paged cache into out (fp32, like q) and, unless None, lse [B][T][Hq]."""
+    _cache_ok(shape, cache)
+    _int32("ctx_lens", ctx_lens, shape.batch)
+    rows = shape.batch * num_tokens * shape.num_q_heads
+    _dense("q", q, torch.bfloat16, rows * 128)
+    _dense("out", out, torch.float32, rows * 128)
+    if lse is not None:
+        _dense("lse", lse, torch.float32, rows)
+    with _On(ctx_lens, stream) as s:
+        _check("ckv_paged_decode_attn", _lib.ckv_paged_decode_attn(
+            shape, cache, num_tokens, q.data_ptr(), ctx_lens.data_ptr(), scale, out.data_ptr(),
+            _ptr(lse), _ptr(ws), ws.numel() if ws is not None else 0, s))
+
+
 KERNEL_IDS = {"zero": 0, "score": 1, "hist": 2, "filter": 3, "finish": 4, "attn": 5,
               "combine": 6, "dual": 7, "gather": 8, "miss": 9, "landmarks": 10,
               "expand": 11, "reconstruct": 12, "select_attn": 13, "probe": 14,
-              "critical": 15}
+              "critical": 15, "rope": 16, "paged_write": 17, "paged_read": 18,
+              "paged_score": 19, "paged_attn": 20, "paged_merge": 21}
 
 
 def profile_begin(kernels=None, every: int = 1) -> None:
@@ -353,7 +627,7 @@ def profile_end() -> dict:
     """Stop recording; {kernel name: (launches, total_ms, max_ms)} for every
     kernel class that ran (waits for the recorded kernels)."""
     arr = (KernelStats * KERNEL_COUNT)()
-    _check("ckv_profile_end", _lib.ckv_profile_end(arr))
+    _check("ckv_profile_end_n", _lib.ckv_profile_end_n(arr, KERNEL_COUNT))
     return {_lib.ckv_kernel_name(i).decode(): (arr[i].launches, arr[i].total_ms, arr[i].max_ms)
             for i in range(KERNEL_COUNT) if arr[i].launches}
 

@@ -10,7 +10,9 @@
 #include <string>
 
 #include "ckv.h"
+#include "ckv_check.hpp"
 #include "ckv_launch.hpp"
+#include "ckv_paged.hpp"
 #include "ckv_profile.hpp"
 
 namespace ckv {
@@ -83,17 +85,6 @@ namespace {
 
 using namespace ckv;
 
-#define CKV_TRY_HIP(expr, what)                 \
-  do {                                          \
-    hipError_t e_ = (expr);                     \
-    if (e_ != hipSuccess) return hip_fail(e_, what); \
-  } while (0)
-
-struct Dims {
-  int B, Hq, Hkv, G, U, max_ctx;
-  int64_t key_stride, kv_stride;
-};
-
 // ckv_set_one_launch_same_step
 std::atomic<int> g_one_launch{CKV_ONE_LAUNCH_ROW_HALVES};
 
@@ -107,65 +98,11 @@ uint64_t next_fused_tag() {
   return ((uint64_t)t << 32) | (uint32_t)~t;
 }
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-int check_shape(const ckv_shape* s, Dims* d) {
-  if (!s) return fail(CKV_EINVAL, "shape is NULL");
-  if (s->reserved != 0) return fail(CKV_EINVAL, "shape.reserved must be 0");
-  if (s->batch < 0 || s->num_q_heads < 1 || s->num_kv_heads < 1)
-    return fail(CKV_ESHAPE, "batch=%d num_q_heads=%d num_kv_heads=%d", s->batch,
-                s->num_q_heads, s->num_kv_heads);
-  if (s->num_q_heads % s->num_kv_heads)
-    return fail(CKV_ESHAPE, "num_q_heads %d not a multiple of num_kv_heads %d",
-                s->num_q_heads, s->num_kv_heads);
-  if (s->head_dim != kD)
-    return fail(CKV_EUNSUPPORTED, "head_dim %d (only %d is supported)", s->head_dim, kD);
-  const int G = s->num_q_heads / s->num_kv_heads;
-  if (G != 1 && G != 2 && G != 4 && G != 8 && G != 16)
-    return fail(CKV_EUNSUPPORTED, "group size %d not in {1,2,4,8,16}", G);
-  if (s->max_ctx < 1 || s->max_ctx > (1 << 30))
-    return fail(CKV_ESHAPE, "max_ctx %d outside [1, 2^30]", s->max_ctx);
-  if (s->key_row_stride < kD || (s->key_row_stride & 7))
-    return fail(CKV_ESHAPE, "key_row_stride %lld (>= 128, multiple of 8)",
-                (long long)s->key_row_stride);
-  if (s->kv_row_stride < kD || (s->kv_row_stride & 7))
-    return fail(CKV_ESHAPE, "kv_row_stride %lld (>= 128, multiple of 8)",
-                (long long)s->kv_row_stride);
-  const int64_t units = (int64_t)s->batch * s->num_kv_heads;
-  if (units > (1 << 24)) return fail(CKV_EUNSUPPORTED, "batch*num_kv_heads too large");
-  d->B = s->batch;
-  d->Hq = s->num_q_heads;
-  d->Hkv = s->num_kv_heads;
-  d->G = G;
-  d->U = (int)units;
-  d->max_ctx = s->max_ctx;
-  d->key_stride = s->key_row_stride;
-  d->kv_stride = s->kv_row_stride;
-  return CKV_OK;
-}
-
-int check_k(int32_t k) {
-  if (k < 1 || k > (1 << 20)) return fail(CKV_ESHAPE, "k %d outside [1, 2^20]", k);
-  return CKV_OK;
-}
-
 int check_rank(int32_t rank) {
   if (rank < 1 || rank > CKV_MAX_RANK)
     return fail(CKV_ESHAPE, "rank %d outside [1, %d]", rank, CKV_MAX_RANK);
   return CKV_OK;
 }
-
-int check_scale(float scale) {
-  if (!(scale > 0.f) || scale > 3.0e38f)
-    return fail(CKV_EINVAL, "scale must be a finite positive number");
-  return CKV_OK;
-}
-
-#define CKV_PTR(p)                                                          \
-  do {                                                                      \
-    if (!(p)) return fail(CKV_EINVAL, "%s is NULL", #p);                    \
-    if (!aligned16(p)) return fail(CKV_EINVAL, "%s is not 16-byte aligned", #p); \
-  } while (0)
 
 // Debug mode: the entry's device-side inputs, checked before its launches
 // (d: the entry's Dims).
@@ -175,8 +112,6 @@ int check_scale(float scale) {
                                 d.max_ctx, (kk));                                         \
     if (rc_) return rc_;                                                                  \
   } while (0)
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // Workspace regions, each 256-byte aligned.  [0, zero_end) is cleared at the
 // start of every selecting call.
@@ -832,6 +767,11 @@ int ckv_workspace_bytes(const ckv_shape* shape, int32_t k, int entry, size_t* by
   if (rc) return rc;
   if ((rc = check_k(k))) return rc;
   if (!bytes) return fail(CKV_EINVAL, "bytes is NULL");
+  if (entry == CKV_ENTRY_PAGED_DECODE_ATTN) {  // k: the number of query tokens
+    if ((rc = check_tokens(d, k))) return rc;
+    *bytes = paged_attn_ws_bytes(d, k);
+    return CKV_OK;
+  }
   if (entry != CKV_ENTRY_SELECT_TOPK && entry != CKV_ENTRY_SPARSE_DECODE_ATTN &&
       entry != CKV_ENTRY_CRITICAL_KV_ATTN && entry != CKV_ENTRY_CORRECTED_ATTN &&
       entry != CKV_ENTRY_DUAL_TOKEN_ATTN && entry != CKV_ENTRY_DECODE_STEP)

@@ -1,0 +1,960 @@
+// ckv_paged.hip -- gfx950 kernels of the rotary positions and the paged cache,
+// and their host-side launchers.
+#include "ckv_paged.hpp"
+#include "ckv_profile.hpp"
+
+namespace ckv {
+
+// ---- small helpers -------------------------------------------------------------
+// bf16 bits of x, nearest, ties to even; NaN stays NaN.
+__device__ __forceinline__ uint32_t bf16_bits(float x) {
+  const uint32_t u = __float_as_uint(x);
+  return x != x ? (u >> 16) | 0x40u : (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;
+}
+
+__device__ __forceinline__ uint4 pack8_bf16(const float* y) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = bf16_bits(y[2 * i]) | (bf16_bits(y[2 * i + 1]) << 16);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// 2^(byte - 127), the value of an exponent byte (255: NaN, as the format has it).
+__device__ __forceinline__ float exp_value(uint32_t byte) {
+  return __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7fc00000u : byte << 23);
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Two e4m3 codes (the low or the high half of w) as two bf16: exact.
+template <bool HI>
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, HI));
+}
+
+// Eight codes as eight bf16.
+__device__ __forceinline__ uint4 e4m3_octet(uint2 w) {
+  return make_uint4(e4m3_pair<false>(w.x), e4m3_pair<true>(w.x), e4m3_pair<false>(w.y),
+                    e4m3_pair<true>(w.y));
+}
+
+// ---- rotary positions ------------------------------------------------------------
+// (cos, sin) of pos * inv_freq.  The angle is formed in quarter turns in fp64
+// (a position of 2^20 leaves fp32 5 correct bits of a radian's fraction), its
+// whole quarters are taken off there, and what is left, |x| <= pi/4, goes through
+// the Taylor series of sine (to x^9, remainder below 1.8e-9) and cosine (to
+// x^10, below 1.2e-10) in fp32.
+__device__ __forceinline__ float2 cos_sin(double quarters) {
+  const double whole = rint(quarters);
+  const float x = (float)(quarters - whole) * 1.5707963267948966f;
+  const int n = (int)(whole - 4.0 * floor(whole * 0.25));  // 0 .. 3
+  const float x2 = x * x;
+  float s = fmaf(x2, 2.7557319e-6f, -1.9841270e-4f);
+  s = fmaf(x2, s, 8.3333333e-3f);
+  s = fmaf(x2, s, -1.6666667e-1f);
+  s = fmaf(x * x2, s, x);
+  float c = fmaf(x2, -2.7557319e-7f, 2.4801587e-5f);
+  c = fmaf(x2, c, -1.3888889e-3f);
+  c = fmaf(x2, c, 4.1666667e-2f);
+  c = fmaf(x2, c, -0.5f);
+  c = fmaf(x2, c, 1.0f);
+  const float a = n & 1 ? s : c, b = n & 1 ? c : s;
+  return make_float2(n == 1 || n == 2 ? -a : a, n >= 2 ? -b : b);
+}
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopeTokens = 4;       // tokens of a workgroup in a long call
+constexpr int kRopeMaxPairs = 512;
+
+// The workgroup's cosines and sines, scale (and direction) included: tab[t *
+// pairs + i] for its `tokens` tokens from t0 on.
+__device__ __forceinline__ void rope_table(const RopeSpec& r, const int32_t* pos, int t0,
+                                           int tokens, float2* tab) {
+  const int pairs = r.rot >> 1;
+  for (int e = threadIdx.x; e < tokens * pairs; e += kRopeThreads) {
+    const int t = e / pairs, i = e - t * pairs;
+    // 2 / pi: quarter turns of a radian
+    const double q = (double)pos[t0 + t] * (r.inv_freq[i] * 0.63661977236758134308);
+    float2 cs = cos_sin(q);
+    cs.x *= r.scale;
+    cs.y *= r.inverse ? -r.scale : r.scale;
+    tab[e] = cs;
+  }
+}
+
+template <typename T>
+struct RopeVec;  // 16 bytes of a row
+template <>
+struct RopeVec<uint16_t> {
+  static constexpr int kN = 8;
+  static __device__ __forceinline__ void load(const uint16_t* p, float* x) { unpack8(ld16(p), x); }
+  static __device__ __forceinline__ void store(uint16_t* p, const float* y) {
+    *reinterpret_cast<uint4*>(p) = pack8_bf16(y);
+  }
+  static __device__ __forceinline__ float one(const uint16_t* p) {
+    return __uint_as_float((uint32_t)*p << 16);
+  }
+  static __device__ __forceinline__ void put(uint16_t* p, float y) { *p = (uint16_t)bf16_bits(y); }
+};
+template <>
+struct RopeVec<float> {
+  static constexpr int kN = 4;
+  static __device__ __forceinline__ void load(const float* p, float* x) {
+    const float4 v = *reinterpret_cast<const float4*>(p);
+    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float* y) {
+    *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+  }
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ void put(float* p, float y) { *p = y; }
+};
+
+// A row's work in items that each own what they read, so that a row may be
+// rotated in place.  Whole vectors where the pairs fill them (rot_dim a
+// multiple of 16 bytes, of 32 for halves): an item is a vector of first
+// elements with the vector of their partners, or a vector of neighbouring
+// pairs; else an item is one pair.  What lies past rot_dim is copied in
+// vectors, from the next whole one on (elements before it one by one), and
+// not at all in place.
+template <typename T>
+__host__ __device__ __forceinline__ bool rope_whole(int rot, int layout) {
+  const int n = sizeof(T) == 2 ? 8 : 4;
+  return rot % (layout == CKV_ROPE_HALF ? 2 * n : n) == 0;
+}
+
+struct RopeItems {
+  int turn, copy;  // items that rotate, items that copy
+};
+
+template <typename T>
+__host__ __device__ __forceinline__ RopeItems rope_items(int head_dim, int rot, int layout,
+                                                         bool in_place) {
+  const int n = sizeof(T) == 2 ? 8 : 4;
+  RopeItems it;
+  const bool whole = rope_whole<T>(rot, layout);
+  it.turn = !whole ? rot / 2 : layout == CKV_ROPE_HALF ? rot / (2 * n) : rot / n;
+  it.copy = in_place ? 0 : whole ? (head_dim - rot) / n : head_dim - rot;
+  return it;
+}
+
+template <typename T>
+__device__ __forceinline__ void rope_item(const RopeSpec& r, const T* src, T* dst, int item,
+                                          RopeItems it, const float2* cs) {
+  using V = RopeVec<T>;
+  constexpr int N = V::kN;
+  const bool whole = rope_whole<T>(r.rot, r.layout);
+  if (item >= it.turn) {
+    const int e = item - it.turn;
+    if (whole) {
+      *reinterpret_cast<uint4*>(dst + r.rot + N * e) =
+          *reinterpret_cast<const uint4*>(src + r.rot + N * e);
+    } else {
+      dst[r.rot + e] = src[r.rot + e];
+    }
+    return;
+  }
+  if (!whole) {
+    const int i1 = r.layout == CKV_ROPE_HALF ? item : 2 * item;
+    const int i2 = r.layout == CKV_ROPE_HALF ? item + r.rot / 2 : 2 * item + 1;
+    const float x1 = V::one(src + i1), x2 = V::one(src + i2);
+    const float2 c = cs[item];
+    V::put(dst + i1, x1 * c.x - x2 * c.y);
+    V::put(dst + i2, x2 * c.x + x1 * c.y);
+    return;
+  }
+  if (r.layout == CKV_ROPE_HALF) {
+    const int i1 = N * item, i2 = i1 + r.rot / 2;
+    float x1[N], x2[N], y1[N], y2[N];
+    V::load(src + i1, x1);
+    V::load(src + i2, x2);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float2 c = cs[i1 + j];
+      y1[j] = x1[j] * c.x - x2[j] * c.y;
+      y2[j] = x2[j] * c.x + x1[j] * c.y;
+    }
+    V::store(dst + i1, y1);
+    V::store(dst + i2, y2);
+  } else {
+    float x[N], y[N];
+    V::load(src + N * item, x);
+#pragma unroll
+    for (int j = 0; j < N; j += 2) {
+      const float2 c = cs[(N * item + j) / 2];
+      y[j] = x[j] * c.x - x[j + 1] * c.y;
+      y[j + 1] = x[j + 1] * c.x + x[j] * c.y;
+    }
+    V::store(dst + N * item, y);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int per) {
+  __shared__ float2 tab[kRopeTokens * kRopeMaxPairs];
+  const int t0 = blockIdx.x * per;
+  const int tokens = min(per, a.tokens - t0);
+  rope_table(a.r, a.pos, t0, tokens, tab);
+  __syncthreads();
+  const RopeItems iq = rope_items<T>(a.r.head_dim, a.r.rot, a.r.layout, a.q.src == a.q.dst);
+  const RopeItems ik = rope_items<T>(a.r.head_dim, a.r.rot, a.r.layout, a.k.src == a.k.dst);
+  const int nq = a.q.heads * (iq.turn + iq.copy), nk = a.k.heads * (ik.turn + ik.copy);
+  for (int e = threadIdx.x; e < tokens * (nq + nk); e += kRopeThreads) {
+    const int t = e / (nq + nk);
+    int item = e - t * (nq + nk);
+    const bool second = item >= nq;
+    const RopeRows& rows = second ? a.k : a.q;
+    const RopeItems it = second ? ik : iq;
+    if (second) item -= nq;
+    const int head = item / (it.turn + it.copy);
+    rope_item<T>(a.r,
+                 static_cast<const T*>(rows.src) + (int64_t)(t0 + t) * rows.src_tok +
+                     head * rows.src_head,
+                 static_cast<T*>(rows.dst) + (int64_t)(t0 + t) * rows.dst_tok +
+                     head * rows.dst_head,
+                 item - head * (it.turn + it.copy), it, tab + t * (a.r.rot >> 1));
+  }
+}
+
+// ---- writing -----------------------------------------------------------------------
+// Row of position pos in its page, or a page of -1 where it is not there.
+__device__ __forceinline__ int page_of(const PagedPages& pg, int b, int pos) {
+  const int page = pg.table[(int64_t)b * pg.table_stride + (pos >> pg.shift)];
+  return (unsigned)page < (unsigned)pg.num_pages ? page : -1;
+}
+
+__device__ __forceinline__ int64_t row_offset(const PagedPages& pg, int page, int h, int pos) {
+  const int row = pos & ((1 << pg.shift) - 1);
+  return page * pg.page_bytes + h * pg.head_bytes + (int64_t)row * pg.row_bytes;
+}
+
+__device__ __forceinline__ int64_t exp_offset(const PagedPages& pg, int page, int h, int pos) {
+  return (((int64_t)page * pg.Hkv + h) << pg.shift) + (pos & ((1 << pg.shift) - 1));
+}
+
+// Eight elements [8c, 8c + 8) of a K row, turned by its position.
+__device__ __forceinline__ void turned8(const RopeSpec& r, const uint16_t* row, int c,
+                                        const float2* cs, float* y) {
+  float x[8];
+  unpack8(ld16(row + 8 * c), x);
+  const int half = r.rot >> 1;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int e = 8 * c + j;
+    if (e >= r.rot) {
+      y[j] = x[j];
+    } else if (r.layout == CKV_ROPE_HALF) {
+      const bool first = e < half;
+      const float o = RopeVec<uint16_t>::one(row + (first ? e + half : e - half));
+      const float2 k = cs[first ? e : e - half];
+      y[j] = first ? x[j] * k.x - o * k.y : x[j] * k.x + o * k.y;
+    } else {
+      const float o = x[j ^ 1];
+      const float2 k = cs[e >> 1];
+      y[j] = (j & 1) == 0 ? x[j] * k.x - o * k.y : x[j] * k.x + o * k.y;
+    }
+  }
+}
+
+// Sixteen lanes write a row: lane c its elements [8c, 8c + 8).
+template <bool E4M3>
+__device__ __forceinline__ void store_row(uint8_t* row, uint8_t* exp, int c, const float* y) {
+  if (!E4M3) {
+    *reinterpret_cast<uint4*>(row + 16 * c) = pack8_bf16(y);
+    return;
+  }
+  float most = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const float m = fabsf(y[j]);
+    most = fmaxf(most, m < INFINITY ? m : 0.f);
+  }
+  most = row16_max(most);
+  // 448 = 1.75 * 2^8: the byte is the leading power's field less 8, one more
+  // where the row's largest is above 1.75 times it; fields below 8 hold rows
+  // under 448 * 2^-127
+  const uint32_t u = __float_as_uint(most);
+  const int byte = max((int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), 0);
+  const float inv = __uint_as_float((uint32_t)(254 - byte) << 23);  // 2^(127 - byte)
+  float z[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) z[j] = fabsf(y[j]) < INFINITY ? y[j] * inv : NAN;
+  int lo = __builtin_amdgcn_cvt_pk_fp8_f32(z[0], z[1], 0, false);
+  lo = __builtin_amdgcn_cvt_pk_fp8_f32(z[2], z[3], lo, true);
+  int hi = __builtin_amdgcn_cvt_pk_fp8_f32(z[4], z[5], 0, false);
+  hi = __builtin_amdgcn_cvt_pk_fp8_f32(z[6], z[7], hi, true);
+  *reinterpret_cast<uint2*>(row + 8 * c) = make_uint2((uint32_t)lo, (uint32_t)hi);
+  if (c == 0) *exp = (uint8_t)byte;
+}
+
+template <bool E4M3>
+__global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, int per) {
+  __shared__ float2 tab[kRopeTokens * (kD / 2)];
+  const int t0 = blockIdx.x * per;
+  const int tokens = min(per, a.rope.tokens - t0);
+  const bool turn = a.rope.r.inv_freq != nullptr;
+  if (turn) {
+    rope_table(a.rope.r, a.rope.pos, t0, tokens, tab);
+    __syncthreads();
+  }
+  const int Hkv = a.pg.Hkv;
+  const RopeItems iq = rope_items<uint16_t>(kD, a.rope.r.rot, a.rope.r.layout,
+                                            a.rope.q.src == a.rope.q.dst);
+  const int nkv = 32 * Hkv;  // (head, K | V, 16 lanes)
+  const int n = nkv + a.rope.q.heads * (iq.turn + iq.copy);
+  for (int e = threadIdx.x; e < tokens * n; e += kRopeThreads) {
+    const int t = e / n, item = e - t * n, tok = t0 + t;
+    const float2* cs = tab + t * (a.rope.r.rot >> 1);
+    if (item >= nkv) {
+      const int i = item - nkv, head = i / (iq.turn + iq.copy);
+      const RopeRows& q = a.rope.q;
+      rope_item<uint16_t>(a.rope.r,
+                          static_cast<const uint16_t*>(q.src) + tok * q.src_tok + head * q.src_head,
+                          static_cast<uint16_t*>(q.dst) + tok * q.dst_tok + head * q.dst_head,
+                          i - head * (iq.turn + iq.copy), iq, cs);
+      continue;
+    }
+    const int pos = a.rope.pos[tok], b = a.req ? a.req[tok] : tok;
+    if ((unsigned)pos >= (unsigned)a.max_ctx || (unsigned)b >= (unsigned)a.B) continue;
+    const int page = page_of(a.pg, b, pos);
+    if (page < 0) continue;
+    const int h = item >> 5, c = item & 15;
+    const bool is_v = item & 16;
+    const uint16_t* src = (is_v ? a.v : a.k) + tok * a.tok + h * kD;
+    uint8_t* row = (is_v ? a.pg.v : a.pg.k) + row_offset(a.pg, page, h, pos);
+    if (!E4M3 && (is_v || !turn)) {  // the bits as they are
+      *reinterpret_cast<uint4*>(row + 16 * c) = ld16(src + 8 * c);
+      continue;
+    }
+    float y[8];
+    if (turn && !is_v) turned8(a.rope.r, src, c, cs, y);
+    else unpack8(ld16(src + 8 * c), y);
+    uint8_t* exp = E4M3 ? (is_v ? a.pg.v_exps : a.pg.k_exps) + exp_offset(a.pg, page, h, pos)
+                        : nullptr;
+    store_row<E4M3>(row, exp, c, y);
+  }
+}
+
+// ---- reading back --------------------------------------------------------------------
+// A thread moves 16 bytes of the output: item (unit, slot, K | V, part).
+constexpr int kPagedReadThreads = 256;
+
+template <bool E4M3>
+__global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs a) {
+  const int64_t stride = (int64_t)gridDim.x * kPagedReadThreads;
+  for (int64_t i = (int64_t)blockIdx.x * kPagedReadThreads + threadIdx.x; i < a.items;
+       i += stride) {
+    const int c = (int)(i & 15);
+    const bool is_v = i & 16;
+    const int64_t slot = i >> 5;  // unit * k + s
+    const int unit = (int)(slot / a.k), s = (int)(slot - (int64_t)unit * a.k);
+    const int b = unit / a.pg.Hkv, h = unit - b * a.pg.Hkv;
+    const int n = clamp_len(a.ctx_lens[b], a.max_ctx);
+    int pos = s;
+    if (a.idx) pos = s < a.n_sel[unit] ? a.idx[slot] : -1;
+    if ((unsigned)pos >= (unsigned)n) continue;
+    const int page = page_of(a.pg, b, pos);
+    if (page < 0) continue;
+    const uint8_t* row = (is_v ? a.pg.v : a.pg.k) + row_offset(a.pg, page, h, pos);
+    uint4 y;
+    if (E4M3) {
+      const float f =
+          exp_value(((is_v ? a.pg.v_exps : a.pg.k_exps) + exp_offset(a.pg, page, h, pos))[0]);
+      float x[8];
+      unpack8(e4m3_octet(*reinterpret_cast<const uint2*>(row + 8 * c)), x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] *= f;
+      y = pack8_bf16(x);
+    } else {
+      y = *reinterpret_cast<const uint4*>(row + 16 * c);
+    }
+    *reinterpret_cast<uint4*>((is_v ? a.v_dst : a.k_dst) + slot * kD + 8 * c) = y;
+  }
+}
+
+// ---- keys and values of 16 positions ---------------------------------------------------
+// Sixteen consecutive positions from a multiple of 16 on.  With pages of at
+// least 16 positions (WIDE) they lie in one page, whose number is the same for
+// the whole wave; else every lane looks its rows' pages up.  Rows at or past
+// the context's end are read as its last row (rows there may hold anything, and
+// a weight of zero times a NaN is a NaN).
+struct Ctx {
+  int b, h, n;            // request, KV head, positions (> 0 where rows are read)
+  const int32_t* table;   // the request's
+};
+
+// Page of a group's row `i` (0 .. 15) of the group that begins at p0, and the
+// row's position after clamping.
+template <bool WIDE>
+__device__ __forceinline__ void group_row(const PagedPages& pg, const Ctx& x, int p0, int i,
+                                          int* page, int* pos) {
+  if (WIDE) {
+    const int first = min(p0, (x.n - 1) & ~15);
+    *page = x.table[first >> pg.shift];
+    *pos = min(first + i, x.n - 1);
+  } else {
+    *pos = min(p0 + i, x.n - 1);
+    *page = x.table[*pos >> pg.shift];
+  }
+}
+
+// Position i of a group in the order that feeds a product's K operand: lane
+// (g, r) = (lane / 16, lane % 16) holds row r, in the fragments f = 0 .. 3 the
+// elements frag_base(f) + 0 .. 7, 16 bytes a load.  Any order of the 128
+// products will do as long as the queries' fragments have the same.
+template <bool E4M3>
+__device__ __forceinline__ int frag_base(int f, int g) {
+  return E4M3 ? 64 * (f >> 1) + 16 * g + 8 * (f & 1) : 32 * f + 8 * g;
+}
+
+template <bool E4M3>
+struct KRaw {
+  uint4 w[E4M3 ? 2 : 4];
+  __device__ __forceinline__ void load(const uint8_t* row, int g) {
+#pragma unroll
+    for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+      w[i] = *reinterpret_cast<const uint4*>(row + 64 * i + 16 * g);
+  }
+  __device__ __forceinline__ bf16x8 frag(int f) const {
+    if (!E4M3) return as_bf16x8(w[f]);
+    const uint4 q = w[f >> 1];
+    return as_bf16x8(e4m3_octet(f & 1 ? make_uint2(q.z, q.w) : make_uint2(q.x, q.y)));
+  }
+};
+
+// ---- scores ----------------------------------------------------------------------------
+// Four waves score kPagedScoreRows positions of a unit, 64 a step: queries x
+// keys on 16x16x32 products, heads in the rows, so that the largest over a
+// group's heads is taken over a lane's registers and, past four heads, over
+// lane rows.
+constexpr int kPagedScoreThreads = 256;
+
+template <bool E4M3, bool WIDE, int G>
+__global__ __launch_bounds__(kPagedScoreThreads) void k_paged_score(PagedScoreArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4, r = lane & 15;
+  const int unit = blockIdx.x / a.chunks, chunk = blockIdx.x - unit * a.chunks;
+  Ctx x;
+  x.b = unit / a.pg.Hkv;
+  x.h = unit - x.b * a.pg.Hkv;
+  x.n = clamp_len(a.ctx_lens[x.b], a.max_ctx);
+  x.table = a.pg.table + (int64_t)x.b * a.pg.table_stride;
+  float* scores = a.scores + (int64_t)unit * a.max_ctx;
+  bf16x8 q[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+    q[f] = as_bf16x8(r < G ? ld16(a.q + ((int64_t)x.b * a.Hq + x.h * G + r) * kD +
+                                  frag_base<E4M3>(f, g))
+                           : make_uint4(0u, 0u, 0u, 0u));
+  constexpr int kRows = kPagedScoreRows / 4;  // of a wave
+  for (int p = chunk * kPagedScoreRows + wave * kRows;
+       p < min((chunk * kPagedScoreRows) + (wave + 1) * kRows, a.max_ctx); p += 64) {
+    float mine = -INFINITY;  // of position p + lane
+    if (p < x.n) {
+      KRaw<E4M3> k[4];
+      int page[4], pos[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        group_row<WIDE>(a.pg, x, p + 16 * i, r, &page[i], &pos[i]);
+        const bool there = (unsigned)page[i] < (unsigned)a.pg.num_pages;
+        if (!there) page[i] = -1;
+        k[i].load(a.pg.k + row_offset(a.pg, max(page[i], 0), x.h, pos[i]), g);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc = mfma_16x16x32(q[f], k[i].frag(f), acc);
+        // register j of lane (g, r): head 4g + j at position r
+        float best = acc[0];
+#pragma unroll
+        for (int j = 1; j < (G < 4 ? G : 4); ++j) best = fmaxf(best, acc[j]);
+        if (G <= 4) best = __shfl(best, r);  // heads are in lane row 0
+        if (G >= 8) best = fmaxf(best, __shfl_xor(best, 16));
+        if (G == 8) best = __shfl(best, r);
+        if (G == 16) best = fmaxf(best, __shfl_xor(best, 32));
+        best *= a.scale;
+        if (E4M3)
+          best *= exp_value(a.pg.k_exps[exp_offset(a.pg, max(page[i], 0), x.h, pos[i])]);
+        if (page[i] >= 0 && p + 16 * i + r < x.n && g == i) mine = best;
+      }
+    }
+    if (p + lane < a.max_ctx) scores[p + lane] = mine;
+  }
+}
+
+// ---- attention -----------------------------------------------------------------------
+// Work is counted in steps of kPagedStep positions of a unit (request, KV
+// head), over all units in order: workgroup w of W takes the steps [total * w /
+// W, total * (w + 1) / W), whatever requests they belong to, so that a ragged
+// batch, one long request and many short ones all fill the device evenly, and
+// the division is the device's own (lengths are device data; max_ctx says
+// little about them).  Fewer steps than workgroups: one each for the first ones.  A unit inside one range is finished there; the partials
+// of one that ranges share are joined by k_paged_merge.
+__device__ __forceinline__ int64_t range_start(int64_t total, int w, int nwg) {
+  return total * w / nwg;
+}
+
+__device__ __forceinline__ int steps_of(const PagedAttnArgs& a, int b) {
+  return (clamp_len(a.ctx_lens[b], a.max_ctx) + kPagedStep - 1) / kPagedStep;
+}
+
+constexpr int kPagedAttnThreads = 256;
+
+struct PagedAttnLds {
+  float m[4][16], l[4][16];
+  float o[4][16][kPartStride];
+  int64_t wave_sum[4];
+  int64_t off;             // of the range's first step in its request
+  int32_t b;
+};
+
+// Steps of all requests; lds.b and lds.off get the request of step `first` and
+// the step's offset there (the range is not empty).
+__device__ __forceinline__ int64_t find_range(const PagedAttnArgs& a, PagedAttnLds& lds,
+                                              int64_t* s0, int64_t* s1) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int per = (a.B + kPagedAttnThreads - 1) / kPagedAttnThreads;
+  const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  int64_t mine = 0;
+  for (int b = b0; b < b1; ++b) mine += (int64_t)steps_of(a, b) * a.pg.Hkv;
+  int64_t incl = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t up = __shfl_up(incl, o);
+    if (lane >= o) incl += up;
+  }
+  if (lane == 63) lds.wave_sum[wave] = incl;
+  __syncthreads();
+  int64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) incl += lds.wave_sum[w];
+    total += lds.wave_sum[w];
+  }
+  const int nwg = (int)min((int64_t)a.nwg, total), w = min((int)blockIdx.x, nwg);
+  *s0 = nwg ? range_start(total, w, nwg) : 0;
+  *s1 = nwg ? range_start(total, min(w + 1, nwg), nwg) : 0;
+  int64_t at = incl - mine;
+  if (*s0 < *s1 && *s0 >= at && *s0 < incl) {
+    for (int b = b0; b < b1; ++b) {
+      const int64_t n = (int64_t)steps_of(a, b) * a.pg.Hkv;
+      if (*s0 < at + n) {
+        lds.b = b;
+        lds.off = *s0 - at;
+        break;
+      }
+      at += n;
+    }
+  }
+  __syncthreads();
+  return total;
+}
+
+// One wave's state over the positions it has seen of a unit: lane (g, r) has
+// query row r's running maximum m (of logits times log2 e, the same in every
+// g), its own positions' sum of weights l, and the weighted V sums
+// o[e][j] = O[row r][8 (4g + j) + e].
+struct WaveState {
+  float m, l;
+  f32x4 o[8];
+};
+
+// A wave's step: 32 positions from p0 on.
+//   logits   S^T = K Q^T: positions in the rows, so lane (g, r) gets query row
+//            r at positions 4g + 0 .. 3 of each half
+//   weights  exp2 of logits less the running maximum, fp32; split exactly
+//            into three bf16 parts (8 + 8 + 8 bits, each the truncation of
+//            what the ones before leave), so that the products with V's bf16
+//            are exact too and only the fp32 accumulation rounds
+//   output   O^T += V^T P^T, 32 positions a product in the order that the
+//            weights already have: operand entry (g, j) is position 4g + j of
+//            the first half (j < 4) or 4g + j - 4 of the second, and lane (g,
+//            r) reads channels [8r, 8r + 8) of those eight rows, 16 bytes a
+//            row, and picks its operands out of them by byte permutes
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void attn_tile(const PagedAttnArgs& a, const Ctx& x, int p0, int limit,
+                                          float c, const bf16x8* q, WaveState& st) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const PagedPages& pg = a.pg;
+  KRaw<E4M3> k[2];
+  uint4 v[8];                       // bf16 rows (e4m3: codes, then widened)
+  float ke[8], ve[8];
+  bool there[8];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int page, pos;
+    group_row<WIDE>(pg, x, p0 + 16 * i, r, &page, &pos);
+    k[i].load(pg.k + row_offset(pg, (unsigned)page < (unsigned)pg.num_pages ? page : 0, x.h, pos),
+              g);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    int page, pos;
+    const int i = j >> 2, row = 4 * g + (j & 3);
+    group_row<WIDE>(pg, x, p0 + 16 * i, row, &page, &pos);
+    there[j] = (unsigned)page < (unsigned)pg.num_pages;
+    if (!there[j]) page = 0;
+    const uint8_t* p = pg.v + row_offset(pg, page, x.h, pos);
+    if (E4M3) {
+      const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * r);
+      v[j] = make_uint4(w.x, w.y, 0u, 0u);
+      const int64_t at = exp_offset(pg, page, x.h, pos);
+      ke[j] = exp_value(pg.k_exps[at]);
+      ve[j] = exp_value(pg.v_exps[at]);
+    } else {
+      v[j] = *reinterpret_cast<const uint4*>(p + 16 * r);
+    }
+  }
+  f32x4 s[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int f = 0; f < 4; ++f) s[i] = mfma_16x16x32(k[i].frag(f), q[f], s[i]);
+  }
+  float top = -INFINITY;
+  float lg[8];
+  bool ok[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const int pos = p0 + 16 * (j >> 2) + 4 * g + (j & 3);
+    ok[j] = pos < limit && there[j];
+    lg[j] = E4M3 ? s[j >> 2][j & 3] * ke[j] : s[j >> 2][j & 3];
+    if (ok[j]) top = fmaxf(top, lg[j]);
+  }
+  top = fmaxf(top, __shfl_xor(top, 16));
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float m = fmaxf(st.m, top * c);
+  if (__any(m > st.m)) {
+    const float f = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
+    st.l *= f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) st.o[e][j] *= f;
+    st.m = m;
+  }
+  uint32_t part[3][8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float p = ok[j] ? __builtin_amdgcn_exp2f(fmaf(lg[j], c, -m)) : 0.f;
+    st.l += p;
+    if (E4M3) p = ok[j] ? p * ve[j] : 0.f;
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      part[t][j] = __float_as_uint(p);
+      p -= __uint_as_float(part[t][j] & 0xffff0000u);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    if (E4M3) v[j] = e4m3_octet(make_uint2(v[j].x, v[j].y));
+    if (!there[j]) v[j] = make_uint4(0u, 0u, 0u, 0u);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t* lo = reinterpret_cast<const uint32_t*>(&v[2 * j]);
+      const uint32_t* hi = reinterpret_cast<const uint32_t*>(&v[2 * j + 1]);
+      w[j] = __builtin_amdgcn_perm(hi[e >> 1], lo[e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+    }
+    const bf16x8 vt = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      uint32_t y[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        y[j] = __builtin_amdgcn_perm(part[t][2 * j + 1], part[t][2 * j], 0x07060302u);
+      st.o[e] = mfma_16x16x32(vt, as_bf16x8(make_uint4(y[0], y[1], y[2], y[3])), st.o[e]);
+    }
+  }
+}
+
+__device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h, int row) {
+  const int t = row >> a.lg, g = row & ((1 << a.lg) - 1);
+  return ((int64_t)b * a.T + t) * a.Hq + (h << a.lg) + g;
+}
+
+template <bool E4M3, bool WIDE>
+__global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs a) {
+  __shared__ PagedAttnLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int rows = a.T << a.lg, w = blockIdx.x;
+  const float c = a.scale * 1.4426950408889634f;
+  // requests without any position: their outputs, shared out over the grid
+  for (int u = w; u < a.B; u += a.nwg) {
+    if (steps_of(a, u) != 0) continue;
+    for (int64_t i = tid; i < (int64_t)a.T * a.Hq * (kD / 4); i += kPagedAttnThreads)
+      reinterpret_cast<float4*>(a.out)[(int64_t)u * a.T * a.Hq * (kD / 4) + i] =
+          make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.lse)
+      for (int i = tid; i < a.T * a.Hq; i += kPagedAttnThreads)
+        a.lse[(int64_t)u * a.T * a.Hq + i] = -INFINITY;
+  }
+  int64_t s0, s1;
+  const int64_t total = find_range(a, lds, &s0, &s1);
+  PagedTail tail = {0, total, -1, 0};
+  int64_t at = s0;
+  int b = __builtin_amdgcn_readfirstlane(lds.b);
+  int steps = at < s1 ? steps_of(a, b) : 1;
+  int h = at < s1 ? __builtin_amdgcn_readfirstlane((int)(lds.off / steps)) : 0;
+  int step = at < s1 ? __builtin_amdgcn_readfirstlane((int)(lds.off % steps)) : 0;
+  while (at < s1) {
+    const int take = (int)min((int64_t)(steps - step), s1 - at);
+    Ctx x;
+    x.b = b;
+    x.h = h;
+    x.n = clamp_len(a.ctx_lens[b], a.max_ctx);
+    x.table = a.pg.table + (int64_t)b * a.pg.table_stride;
+    const int64_t qrow = out_row(a, b, h, r);
+    const int limit = r < rows ? x.n - (a.T - 1 - (r >> a.lg)) : 0;
+    bf16x8 q[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      q[f] = as_bf16x8(r < rows ? ld16(a.q + qrow * kD + frag_base<E4M3>(f, g))
+                                : make_uint4(0u, 0u, 0u, 0u));
+    WaveState st;
+    st.m = -INFINITY;
+    st.l = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = step; s < step + take; ++s) {
+      const int p0 = s * kPagedStep + wave * kPagedTile;
+      if (p0 < x.n) attn_tile<E4M3, WIDE>(a, x, p0, limit, c, q, st);
+    }
+    st.l += __shfl_xor(st.l, 16);
+    st.l += __shfl_xor(st.l, 32);
+    if (g == 0) {
+      lds.m[wave][r] = st.m;
+      lds.l[wave][r] = st.l;
+    }
+    if (r < rows) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        float* o = &lds.o[wave][r][8 * (4 * g + j)];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = st.o[e][j];
+      }
+    }
+    __syncthreads();
+    const bool whole = step == 0 && take == steps;
+    const int slot = at == s0 ? 0 : 1;
+    for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
+      const int row = i >> 5, d = 4 * (i & 31);
+      float M = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) M = fmaxf(M, lds.m[k][row]);
+      float L = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float m = lds.m[k][row];
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+        const float4 ok = *reinterpret_cast<const float4*>(&lds.o[k][row][d]);
+        L = fmaf(f, lds.l[k][row], L);
+        o.x = fmaf(f, ok.x, o.x);
+        o.y = fmaf(f, ok.y, o.y);
+        o.z = fmaf(f, ok.z, o.z);
+        o.w = fmaf(f, ok.w, o.w);
+      }
+      if (whole) {
+        const int64_t at_row = out_row(a, b, h, row);
+        const float inv = L > 0.f ? 1.f / L : L;  // NaN stays
+        *reinterpret_cast<float4*>(a.out + at_row * kD + d) =
+            make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+        if (a.lse && d == 0)
+          a.lse[at_row] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+      } else {
+        float* p = a.part + (((int64_t)w * 2 + slot) * rows + row) * kPartStride;
+        *reinterpret_cast<float4*>(p + 4 + d) = o;
+        if (d == 0) {
+          p[0] = M;
+          p[1] = L;
+        }
+      }
+    }
+    __syncthreads();
+    if (step == 0 && take < steps) {  // begins here and goes on: this range's to join
+      tail.unit = b * a.pg.Hkv + h;
+      tail.end = at + steps;
+      tail.slot = slot;
+    }
+    at += take;
+    step = 0;
+    if (++h == a.pg.Hkv && at < s1) {
+      h = 0;
+      do {
+        ++b;
+        steps = steps_of(a, b);
+      } while (steps == 0);
+    }
+  }
+  if (tid == 0) a.tail[w] = tail;
+}
+
+// Joins the unit that workgroup blockIdx.x's range left unfinished: query row
+// blockIdx.y over the range's own partial and the first partials of the ranges
+// after it, in order.
+constexpr int kPagedMergeThreads = 256;
+
+__global__ __launch_bounds__(kPagedMergeThreads) void k_paged_merge(PagedAttnArgs a) {
+  __shared__ float weight[kMaxPagedWgs];
+  __shared__ float4 sums[kPagedMergeThreads / 32][32];
+  __shared__ float red[kPagedMergeThreads / 64];
+  const int w = blockIdx.x, row = blockIdx.y, rows = a.T << a.lg;
+  const PagedTail t = a.tail[w];
+  if (t.unit < 0) return;
+  // the last range that begins before the unit's end: total * i / nwg < end
+  const int64_t nwg = min((int64_t)a.nwg, t.total);
+  const int n = (int)((t.end * nwg - 1) / t.total) - w + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto partial = [&](int i) {
+    return a.part + (((int64_t)(w + i) * 2 + (i == 0 ? t.slot : 0)) * rows + row) * kPartStride;
+  };
+  float M = -INFINITY;
+  for (int i = tid; i < n; i += kPagedMergeThreads) M = fmaxf(M, partial(i)[0]);
+  M = wave_max(M);
+  if (lane == 0) red[wave] = M;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kPagedMergeThreads / 64; ++i) M = fmaxf(M, red[i]);
+  __syncthreads();
+  float L = 0.f;
+  for (int i = tid; i < n; i += kPagedMergeThreads) {
+    const float m = partial(i)[0];
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+    weight[i] = f;
+    L = fmaf(f, partial(i)[1], L);
+  }
+  L = wave_sum(L);
+  if (lane == 0) red[wave] = L;
+  __syncthreads();
+  L = 0.f;
+#pragma unroll
+  for (int i = 0; i < kPagedMergeThreads / 64; ++i) L += red[i];
+  const int d = tid & 31, part = tid >> 5;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = part; i < n; i += kPagedMergeThreads / 32) {
+    const float4 x = *reinterpret_cast<const float4*>(partial(i) + 4 + 4 * d);
+    const float f = weight[i];
+    o.x = fmaf(f, x.x, o.x);
+    o.y = fmaf(f, x.y, o.y);
+    o.z = fmaf(f, x.z, o.z);
+    o.w = fmaf(f, x.w, o.w);
+  }
+  sums[part][d] = o;
+  __syncthreads();
+  if (part != 0) return;
+  for (int i = 1; i < kPagedMergeThreads / 32; ++i) {
+    const float4 x = sums[i][d];
+    o.x += x.x, o.y += x.y, o.z += x.z, o.w += x.w;
+  }
+  const int b = t.unit / a.pg.Hkv, h = t.unit - b * a.pg.Hkv;
+  const int64_t at = out_row(a, b, h, row);
+  const float inv = L > 0.f ? 1.f / L : L;
+  *reinterpret_cast<float4*>(a.out + at * kD + 4 * d) =
+      make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  if (a.lse && d == 0)
+    a.lse[at] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+}
+
+// ---- debug mode ------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void k_paged_check(PagedCheckArgs a) {
+  const int64_t stride = (int64_t)gridDim.x * blockDim.x;
+  const int64_t total = a.ctx_lens ? (int64_t)a.B * a.pg.table_stride : a.tokens;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
+    unsigned long long kind = 0;
+    if (a.ctx_lens) {
+      const int b = (int)(i / a.pg.table_stride), s = (int)(i - (int64_t)b * a.pg.table_stride);
+      const int n = clamp_len(a.ctx_lens[b], a.max_ctx);
+      const int page = a.pg.table[i];
+      if (((int64_t)s << a.pg.shift) < n && page != -1 &&
+          (unsigned)page >= (unsigned)a.pg.num_pages)
+        kind = 4;
+    } else if (a.pos[i] != -1) {
+      const int b = a.req ? a.req[i] : (int)i;
+      if ((unsigned)a.pos[i] >= (unsigned)a.max_ctx) kind = 5;
+      else if ((unsigned)b >= (unsigned)a.B) kind = 6;
+      else if (page_of(a.pg, b, a.pos[i]) < 0) kind = 7;
+    }
+    if (kind) atomicMin(a.flag, kind << 56 | (unsigned long long)i);
+  }
+}
+
+// ---- launchers ---------------------------------------------------------------------------
+static inline int grid_for(int64_t n, int per, int cap) {
+  const int64_t b = (n + per - 1) / per;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(b, cap));
+}
+
+// Tokens of a workgroup: one while that gives at most kRopeFew workgroups.
+constexpr int kRopeFew = 2048;
+static inline int rope_per(int tokens) { return tokens <= kRopeFew ? 1 : kRopeTokens; }
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
+  const int per = rope_per(a.tokens);
+  const dim3 grid((a.tokens + per - 1) / per), block(kRopeThreads);
+  if (a.r.f32) launch_kernel(CKV_K_ROPE, k_rope<float>, grid, block, s, a, per);
+  else launch_kernel(CKV_K_ROPE, k_rope<uint16_t>, grid, block, s, a, per);
+  return launch_status();
+}
+
+hipError_t launch_paged_write(const PagedWriteArgs& a, bool e4m3, hipStream_t s) {
+  const int per = rope_per(a.rope.tokens);
+  const dim3 grid((a.rope.tokens + per - 1) / per), block(kRopeThreads);
+  if (e4m3) launch_kernel(CKV_K_PAGED_WRITE, k_paged_write<true>, grid, block, s, a, per);
+  else launch_kernel(CKV_K_PAGED_WRITE, k_paged_write<false>, grid, block, s, a, per);
+  return launch_status();
+}
+
+hipError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, hipStream_t s) {
+  const dim3 grid(grid_for(a.items, kPagedReadThreads, 1 << 16)), block(kPagedReadThreads);
+  if (e4m3) launch_kernel(CKV_K_PAGED_READ, k_paged_read<true>, grid, block, s, a);
+  else launch_kernel(CKV_K_PAGED_READ, k_paged_read<false>, grid, block, s, a);
+  return launch_status();
+}
+
+template <bool E4M3, bool WIDE>
+static void launch_score_g(const PagedScoreArgs& a, int G, hipStream_t s) {
+  const dim3 grid((unsigned)(a.units * a.chunks)), block(kPagedScoreThreads);
+  switch (G) {
+    case 1: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 1>, grid, block, s, a); break;
+    case 2: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 2>, grid, block, s, a); break;
+    case 4: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 4>, grid, block, s, a); break;
+    case 8: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 8>, grid, block, s, a); break;
+    default: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 16>, grid, block, s, a);
+  }
+}
+
+hipError_t launch_paged_score(const PagedScoreArgs& a, bool e4m3, int G, hipStream_t s) {
+  const bool wide = a.pg.shift >= 4;
+  if (e4m3) wide ? launch_score_g<true, true>(a, G, s) : launch_score_g<true, false>(a, G, s);
+  else wide ? launch_score_g<false, true>(a, G, s) : launch_score_g<false, false>(a, G, s);
+  return launch_status();
+}
+
+hipError_t launch_paged_attn(const PagedAttnArgs& a, bool e4m3, hipStream_t s) {
+  const bool wide = a.pg.shift >= 4;
+  const dim3 grid(a.nwg), block(kPagedAttnThreads);
+  if (e4m3 && wide) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<true, true>, grid, block, s, a);
+  else if (e4m3) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<true, false>, grid, block, s, a);
+  else if (wide) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<false, true>, grid, block, s, a);
+  else launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<false, false>, grid, block, s, a);
+  const hipError_t e = launch_status();
+  if (e != hipSuccess) return e;
+  launch_kernel(CKV_K_PAGED_MERGE, k_paged_merge, dim3(a.nwg, a.T << a.lg),
+                dim3(kPagedMergeThreads), s, a);
+  return launch_status();
+}
+
+hipError_t launch_paged_check(const PagedCheckArgs& a, hipStream_t s) {
+  const int64_t total = a.ctx_lens ? (int64_t)a.B * a.pg.table_stride : a.tokens;
+  hipLaunchKernelGGL(k_paged_check, dim3(grid_for(total, 256, 4096)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace ckv

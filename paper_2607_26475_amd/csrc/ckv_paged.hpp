@@ -1,0 +1,142 @@
+// ckv_paged.hpp -- launch arguments and launchers of the rotary positions and
+// the paged cache (ckv_paged.hip), and what their host side shares.
+#pragma once
+
+#include <algorithm>
+
+#include "ckv_check.hpp"
+
+namespace ckv {
+
+// Pages as the kernels see them: byte strides, sizes as shifts.
+struct PagedPages {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* k_exps;        // [num_pages][Hkv][page_size], e4m3 only
+  uint8_t* v_exps;
+  const int32_t* table;   // [B][table_stride]
+  int64_t page_bytes, head_bytes;
+  int32_t row_bytes;      // page_size * row_bytes < 2^31
+  int32_t shift;          // log2(page_size)
+  int32_t num_pages, table_stride, Hkv;
+};
+
+struct RopeSpec {
+  const double* inv_freq;
+  int32_t head_dim, rot, layout, f32, inverse;
+  float scale;
+};
+
+struct RopeRows {
+  const void* src;
+  void* dst;
+  int64_t src_tok, src_head, dst_tok, dst_head;  // elements
+  int32_t heads;
+};
+
+struct RopeArgs {
+  RopeSpec r;
+  RopeRows q, k;           // k.heads 0: none
+  const int32_t* pos;
+  int32_t tokens;
+};
+
+struct PagedWriteArgs {
+  PagedPages pg;
+  RopeArgs rope;           // r.inv_freq NULL: rows are stored as they are; q: heads 0, or rotated too
+  const int32_t* req;      // NULL: token t is request t's
+  const uint16_t* k;
+  const uint16_t* v;
+  int64_t tok;             // elements between tokens of k and v
+  int32_t B, max_ctx;
+};
+
+struct PagedReadArgs {
+  PagedPages pg;
+  const int32_t* ctx_lens;
+  const int32_t* idx;      // [U][k], NULL: position i in slot i
+  const int32_t* n_sel;    // [U]
+  uint16_t* k_dst;
+  uint16_t* v_dst;
+  int64_t items;           // U * k * 32
+  int32_t max_ctx, k;
+};
+
+struct PagedScoreArgs {
+  PagedPages pg;
+  const uint16_t* q;
+  const int32_t* ctx_lens;
+  float* scores;
+  float scale;
+  int32_t Hq, max_ctx, chunks, units;
+};
+
+// A unit that begins in a workgroup's range and goes on in the next ones:
+// left for the join (unit -1: none).
+struct PagedTail {
+  int64_t end;             // the unit's last step + 1, over all units
+  int64_t total;           // steps of all units
+  int32_t unit;
+  int32_t slot;            // of the workgroup's own partial
+};
+
+constexpr int kPagedTile = 32;              // positions of a wave's step
+constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
+constexpr int kMaxPagedWgs = 1024;
+constexpr int kPagedWgsPerCu = 2;
+constexpr int kPagedScoreRows = 512;        // positions of a scoring workgroup
+
+struct PagedAttnArgs {
+  PagedPages pg;
+  const uint16_t* q;       // [B][T][Hq][d]
+  const int32_t* ctx_lens;
+  float* out;              // [B][T][Hq][d]
+  float* lse;              // [B][T][Hq] or NULL
+  float* part;             // [nwg][2][T*G][kPartStride]
+  PagedTail* tail;         // [nwg]
+  float scale;
+  int32_t B, Hq, T, lg;    // lg: log2 G
+  int32_t max_ctx, nwg;
+};
+
+// Debug mode's checks of paged inputs (CheckArgs' codes go on: 4 page_table
+// entry, 5 positions[t], 6 requests[t], 7 the page of a written token).
+struct PagedCheckArgs {
+  PagedPages pg;
+  const int32_t* ctx_lens; // reading entries
+  const int32_t* req;      // writing entries
+  const int32_t* pos;
+  unsigned long long* flag;
+  int32_t B, max_ctx, tokens;
+};
+
+hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
+hipError_t launch_paged_write(const PagedWriteArgs& a, bool e4m3, hipStream_t s);
+hipError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, hipStream_t s);
+hipError_t launch_paged_score(const PagedScoreArgs& a, bool e4m3, int G, hipStream_t s);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, bool e4m3, hipStream_t s);
+hipError_t launch_paged_check(const PagedCheckArgs& a, hipStream_t s);
+
+inline int check_tokens(const Dims& d, int32_t tokens) {
+  if (tokens < 1 || (int64_t)tokens * d.G > 16)
+    return fail(CKV_EUNSUPPORTED, "%d tokens of %d heads a group (1 <= tokens * heads <= 16)",
+                tokens, d.G);
+  return CKV_OK;
+}
+
+// Workgroups that a call can have at most: no more than steps.
+inline int paged_wgs_cap(const Dims& d) {
+  const int64_t steps = (int64_t)d.U * ((d.max_ctx + kPagedStep - 1) / kPagedStep);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(steps, kMaxPagedWgs));
+}
+
+inline size_t paged_tail_bytes(const Dims& d) {
+  return align256((size_t)paged_wgs_cap(d) * sizeof(PagedTail));
+}
+
+inline size_t paged_attn_ws_bytes(const Dims& d, int32_t tokens) {
+  return paged_tail_bytes(d) +
+         align256((size_t)paged_wgs_cap(d) * 2 * tokens * d.G * kPartStride * sizeof(float));
+}
+
+}  // namespace ckv

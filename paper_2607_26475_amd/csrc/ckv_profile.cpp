@@ -17,7 +17,7 @@ struct Record {
 std::atomic<bool> g_on{false};
 std::atomic<uint32_t> g_mask{0};
 uint32_t g_every = 1;                 // stamp one launch in g_every per class
-uint64_t g_seen[CKV_K_COUNT] = {};    // launches of each class since begin
+uint64_t g_seen[CKV_K_TOTAL] = {};    // launches of each class since begin
 std::mutex g_mu;
 std::vector<Record> g_records;
 std::vector<hipEvent_t> g_pool;
@@ -93,11 +93,12 @@ int ckv_set_debug(int on) {
 }
 
 const char* ckv_kernel_name(int id) {
-  static const char* names[CKV_K_COUNT] = {"zero", "score", "hist", "filter", "finish",
+  static const char* names[CKV_K_TOTAL] = {"zero", "score", "hist", "filter", "finish",
                                            "attn", "combine", "dual", "gather", "miss",
                                            "landmarks", "expand", "reconstruct",
-                                           "select_attn", "probe", "critical"};
-  return (id >= 0 && id < CKV_K_COUNT) ? names[id] : "";
+                                           "select_attn", "probe", "critical", "rope", "paged_write",
+                                           "paged_read", "paged_score", "paged_attn", "paged_merge"};
+  return (id >= 0 && id < CKV_K_TOTAL) ? names[id] : "";
 }
 
 int ckv_profile_begin_sampled(uint32_t kernel_mask, uint32_t every) {
@@ -106,20 +107,25 @@ int ckv_profile_begin_sampled(uint32_t kernel_mask, uint32_t every) {
   ckv::recycle_all();
   ckv::g_every = every;
   for (uint64_t& c : ckv::g_seen) c = 0;
-  ckv::g_mask.store(kernel_mask & CKV_K_ALL);
+  ckv::g_mask.store(kernel_mask & CKV_K_EVERY);
   ckv::g_on.store(true);
   return CKV_OK;
 }
 
 int ckv_profile_begin(uint32_t kernel_mask) { return ckv_profile_begin_sampled(kernel_mask, 1); }
 
-int ckv_profile_end(ckv_kernel_stats* stats) {
+int ckv_profile_end(ckv_kernel_stats* stats) { return ckv_profile_end_n(stats, CKV_K_COUNT); }
+
+int ckv_profile_end_n(ckv_kernel_stats* stats, int count) {
+  if (count < 1 || count > CKV_K_TOTAL)
+    return ckv::fail(CKV_EINVAL, "count %d outside [1, %d]", count, (int)CKV_K_TOTAL);
   if (!stats) return ckv::fail(CKV_EINVAL, "stats is NULL");
   std::lock_guard<std::mutex> lk(ckv::g_mu);
   ckv::g_on.store(false);
-  for (int i = 0; i < CKV_K_COUNT; ++i) stats[i] = ckv_kernel_stats{0, 0.0, 0.0};
+  for (int i = 0; i < count; ++i) stats[i] = ckv_kernel_stats{0, 0.0, 0.0};
   int rc = CKV_OK;
   for (const ckv::Record& r : ckv::g_records) {
+    if (r.id >= count) continue;
     float ms = 0.f;
     hipError_t e = hipEventSynchronize(r.stop);
     if (e == hipSuccess) e = hipEventElapsedTime(&ms, r.start, r.stop);
