@@ -19,9 +19,9 @@ __device__ __forceinline__ uint4 pack8_bf16(const float* y) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// 2^(byte - 127), the value of an exponent byte (255: NaN, as the format has it).
-__device__ __forceinline__ float exp_value(uint32_t byte) {
-  return __uint_as_float(byte == 0u ? 0x00400000u : byte == 255u ? 0x7fc00000u : byte << 23);
+// x * 2^(byte - 127).
+__device__ __forceinline__ float times_exp(float x, uint32_t byte) {
+  return __builtin_amdgcn_ldexpf(x, (int)byte - 127);
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -358,12 +358,12 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
     const uint8_t* row = (is_v ? a.pg.v : a.pg.k) + row_offset(a.pg, page, h, pos);
     uint4 y;
     if (E4M3) {
-      const float f =
-          exp_value(((is_v ? a.pg.v_exps : a.pg.k_exps) + exp_offset(a.pg, page, h, pos))[0]);
+      const uint32_t e =
+          ((is_v ? a.pg.v_exps : a.pg.k_exps) + exp_offset(a.pg, page, h, pos))[0];
       float x[8];
       unpack8(e4m3_octet(*reinterpret_cast<const uint2*>(row + 8 * c)), x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] *= f;
+      for (int j = 0; j < 8; ++j) x[j] = times_exp(x[j], e);
       y = pack8_bf16(x);
     } else {
       y = *reinterpret_cast<const uint4*>(row + 16 * c);
@@ -476,7 +476,7 @@ __global__ __launch_bounds__(kPagedScoreThreads) void k_paged_score(PagedScoreAr
         if (G == 16) best = fmaxf(best, __shfl_xor(best, 32));
         best *= a.scale;
         if (E4M3)
-          best *= exp_value(a.pg.k_exps[exp_offset(a.pg, max(page[i], 0), x.h, pos[i])]);
+          best = times_exp(best, a.pg.k_exps[exp_offset(a.pg, max(page[i], 0), x.h, pos[i])]);
         if (page[i] >= 0 && p + 16 * i + r < x.n && g == i) mine = best;
       }
     }
@@ -573,56 +573,128 @@ struct WaveState {
 //            the first half (j < 4) or 4g + j - 4 of the second, and lane (g,
 //            r) reads channels [8r, 8r + 8) of those eight rows, 16 bytes a
 //            row, and picks its operands out of them by byte permutes
-template <bool E4M3, bool WIDE>
-__device__ __forceinline__ void attn_tile(const PagedAttnArgs& a, const Ctx& x, int p0, int limit,
-                                          float c, const bf16x8* q, WaveState& st) {
-  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const PagedPages& pg = a.pg;
+// K of the next step is asked for once this step's logits have taken theirs,
+// V once the products have taken its rows: a wave always has one of them in
+// flight, and none needs a second set of registers.
+template <bool E4M3>
+struct Tile {
   KRaw<E4M3> k[2];
-  uint4 v[8];                       // bf16 rows (e4m3: codes, then widened)
-  float ke[8], ve[8];
-  bool there[8];
+  uint32_t v[8][E4M3 ? 2 : 4];      // row j: bf16, or codes
+  uint32_t ke[E4M3 ? 2 : 1], ve[E4M3 ? 2 : 1];  // exponent bytes of each half's four positions
+  uint32_t there;                   // bit j: position j has a page (lane's own rows)
+  bool all;                         // every lane's positions have pages
+};
+
+// Pages of a step's two halves: with WIDE pages the same for every lane.
+struct TilePages {
+  int first[2], page[2];
+};
+
+template <bool WIDE>
+__device__ __forceinline__ TilePages tile_pages(const PagedPages& pg, const Ctx& x, int p0) {
+  TilePages t;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    int page, pos;
-    group_row<WIDE>(pg, x, p0 + 16 * i, r, &page, &pos);
-    k[i].load(pg.k + row_offset(pg, (unsigned)page < (unsigned)pg.num_pages ? page : 0, x.h, pos),
-              g);
+    t.first[i] = min(p0 + 16 * i, (x.n - 1) & ~15);
+    t.page[i] = WIDE ? x.table[t.first[i] >> pg.shift] : 0;
   }
+  return t;
+}
+
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TilePages& tp,
+                                       Tile<E4M3>& t) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    int page, pos;
-    const int i = j >> 2, row = 4 * g + (j & 3);
-    group_row<WIDE>(pg, x, p0 + 16 * i, row, &page, &pos);
-    there[j] = (unsigned)page < (unsigned)pg.num_pages;
-    if (!there[j]) page = 0;
-    const uint8_t* p = pg.v + row_offset(pg, page, x.h, pos);
-    if (E4M3) {
-      const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * r);
-      v[j] = make_uint4(w.x, w.y, 0u, 0u);
-      const int64_t at = exp_offset(pg, page, x.h, pos);
-      ke[j] = exp_value(pg.k_exps[at]);
-      ve[j] = exp_value(pg.v_exps[at]);
-    } else {
-      v[j] = *reinterpret_cast<const uint4*>(p + 16 * r);
+  for (int i = 0; i < 2; ++i) {
+    const int pos = min(tp.first[i] + r, x.n - 1);
+    int page = WIDE ? tp.page[i] : x.table[pos >> pg.shift];
+    if ((unsigned)page >= (unsigned)pg.num_pages) page = 0;
+    const int row = pos & ((1 << pg.shift) - 1);
+    t.k[i].load(pg.k + (page * pg.page_bytes + x.h * pg.head_bytes) + row * pg.row_bytes, g);
+  }
+}
+
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TilePages& tp,
+                                       Tile<E4M3>& t) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int mask = (1 << pg.shift) - 1;
+  t.there = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    int page = tp.page[i];
+    const bool has = (unsigned)page < (unsigned)pg.num_pages;
+    if (WIDE) {
+      if (!has) page = 0;
+      if (has) t.there |= 15u << (4 * i);
+      if (E4M3) {  // four positions' bytes at once: rows of one page, a multiple of 4
+        const int64_t at = (((int64_t)page * pg.Hkv + x.h) << pg.shift) +
+                           (tp.first[i] & mask) + 4 * g;
+        t.ke[i] = *reinterpret_cast<const uint32_t*>(pg.k_exps + at);
+        t.ve[i] = *reinterpret_cast<const uint32_t*>(pg.v_exps + at);
+      }
+    } else if (E4M3) {
+      t.ke[i] = t.ve[i] = 0;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int pos = min(tp.first[i] + 4 * g + j, x.n - 1);
+      const int row = pos & mask;
+      if (!WIDE) {
+        page = x.table[pos >> pg.shift];
+        if ((unsigned)page < (unsigned)pg.num_pages) t.there |= 1u << (4 * i + j);
+        else page = 0;
+        if (E4M3) {
+          const int64_t at = (((int64_t)page * pg.Hkv + x.h) << pg.shift) + row;
+          t.ke[i] |= (uint32_t)pg.k_exps[at] << (8 * j);
+          t.ve[i] |= (uint32_t)pg.v_exps[at] << (8 * j);
+        }
+      }
+      const uint8_t* p = pg.v + (page * pg.page_bytes + x.h * pg.head_bytes) + row * pg.row_bytes;
+      uint32_t* v = t.v[4 * i + j];
+      if (E4M3) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * r);
+        v[0] = w.x, v[1] = w.y;
+      } else {
+        const uint4 w = *reinterpret_cast<const uint4*>(p + 16 * r);
+        v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+      }
     }
   }
-  f32x4 s[2];
+  t.all = WIDE ? t.there == 255u : __all(t.there == 255u);
+}
+
+// x * 2^(byte j of w - 128), bytes already taken as signed (w ^ 0x80808080).
+__device__ __forceinline__ float scaled(float x, uint32_t w, int j) {
+  return __builtin_amdgcn_ldexpf(x, (int)(w << (24 - 8 * j)) >> 24);
+}
+
+// Products of a step for query row r: lg[j] at position p0 + 16 (j / 4) + 4g +
+// j % 4, keys' exponents and the scale not yet in them.
+template <bool E4M3>
+__device__ __forceinline__ void tile_logits(const Tile<E4M3>& t, const bf16x8* q, float* lg) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    s[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int f = 0; f < 4; ++f) s[i] = mfma_16x16x32(k[i].frag(f), q[f], s[i]);
+    for (int f = 0; f < 4; ++f) s = mfma_16x16x32(t.k[i].frag(f), q[f], s);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lg[4 * i + j] = s[j];
   }
-  float top = -INFINITY;
-  float lg[8];
+}
+
+template <bool E4M3, bool MASKED>
+__device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, int p0, int limit, float c,
+                                             float* lg, uint32_t part[3][8], WaveState& st) {
+  const int g = (threadIdx.x & 63) >> 4;
   bool ok[8];
+  float top = -INFINITY;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    const int pos = p0 + 16 * (j >> 2) + 4 * g + (j & 3);
-    ok[j] = pos < limit && there[j];
-    lg[j] = E4M3 ? s[j >> 2][j & 3] * ke[j] : s[j >> 2][j & 3];
-    if (ok[j]) top = fmaxf(top, lg[j]);
+    if (E4M3) lg[j] = scaled(lg[j], t.ke[j >> 2] ^ 0x80808080u, j & 3);
+    ok[j] = !MASKED || (p0 + 16 * (j >> 2) + 4 * g + (j & 3) < limit && (t.there >> j & 1u));
+    top = fmaxf(top, ok[j] ? lg[j] : -INFINITY);
   }
   top = fmaxf(top, __shfl_xor(top, 16));
   top = fmaxf(top, __shfl_xor(top, 32));
@@ -636,41 +708,99 @@ __device__ __forceinline__ void attn_tile(const PagedAttnArgs& a, const Ctx& x, 
       for (int j = 0; j < 4; ++j) st.o[e][j] *= f;
     st.m = m;
   }
-  uint32_t part[3][8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float p = ok[j] ? __builtin_amdgcn_exp2f(fmaf(lg[j], c, -m)) : 0.f;
+    float p = __builtin_amdgcn_exp2f(fmaf(lg[j], c, -m));
+    if (MASKED) p = ok[j] ? p : 0.f;
     st.l += p;
-    if (E4M3) p = ok[j] ? p * ve[j] : 0.f;
+    if (E4M3) {
+      p = scaled(p, t.ve[j >> 2] ^ 0x80808080u, j & 3);
+      if (MASKED) p = ok[j] ? p : 0.f;
+    }
 #pragma unroll
-    for (int t = 0; t < 3; ++t) {
-      part[t][j] = __float_as_uint(p);
-      p -= __uint_as_float(part[t][j] & 0xffff0000u);
+    for (int i = 0; i < 3; ++i) {
+      part[i][j] = __float_as_uint(p);
+      p -= __uint_as_float(part[i][j] & 0xffff0000u);
     }
   }
+}
+
+template <bool E4M3>
+__device__ __forceinline__ void tile_output(const Tile<E4M3>& t, const uint32_t part[3][8],
+                                            WaveState& st) {
+  bf16x8 w[3];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    if (E4M3) v[j] = e4m3_octet(make_uint2(v[j].x, v[j].y));
-    if (!there[j]) v[j] = make_uint4(0u, 0u, 0u, 0u);
+  for (int i = 0; i < 3; ++i) {
+    uint32_t y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      y[j] = __builtin_amdgcn_perm(part[i][2 * j + 1], part[i][2 * j], 0x07060302u);
+    w[i] = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    uint32_t w[4];
+  for (int e = 0; e < 8; e += 2) {
+    uint32_t even[4], odd[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const uint32_t* lo = reinterpret_cast<const uint32_t*>(&v[2 * j]);
-      const uint32_t* hi = reinterpret_cast<const uint32_t*>(&v[2 * j + 1]);
-      w[j] = __builtin_amdgcn_perm(hi[e >> 1], lo[e >> 1], e & 1 ? 0x07060302u : 0x05040100u);
+      uint32_t lo, hi;  // channels e, e + 1 of two rows
+      if (E4M3) {
+        lo = e & 2 ? e4m3_pair<true>(t.v[2 * j][e >> 2]) : e4m3_pair<false>(t.v[2 * j][e >> 2]);
+        hi = e & 2 ? e4m3_pair<true>(t.v[2 * j + 1][e >> 2])
+                   : e4m3_pair<false>(t.v[2 * j + 1][e >> 2]);
+      } else {
+        lo = t.v[2 * j][e >> 1];
+        hi = t.v[2 * j + 1][e >> 1];
+      }
+      even[j] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+      odd[j] = __builtin_amdgcn_perm(hi, lo, 0x07060302u);
     }
-    const bf16x8 vt = as_bf16x8(make_uint4(w[0], w[1], w[2], w[3]));
+    const bf16x8 a = as_bf16x8(make_uint4(even[0], even[1], even[2], even[3]));
+    const bf16x8 b = as_bf16x8(make_uint4(odd[0], odd[1], odd[2], odd[3]));
 #pragma unroll
-    for (int t = 0; t < 3; ++t) {
-      uint32_t y[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        y[j] = __builtin_amdgcn_perm(part[t][2 * j + 1], part[t][2 * j], 0x07060302u);
-      st.o[e] = mfma_16x16x32(vt, as_bf16x8(make_uint4(y[0], y[1], y[2], y[3])), st.o[e]);
+    for (int i = 0; i < 3; ++i) {
+      st.o[e] = mfma_16x16x32(a, w[i], st.o[e]);
+      st.o[e + 1] = mfma_16x16x32(b, w[i], st.o[e + 1]);
     }
+  }
+}
+
+// A wave's steps of a piece: positions [p, end) in strides of kPagedStep.
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x, int p, int end,
+                                           int limit, int least, float c, const bf16x8* q,
+                                           WaveState& st) {
+  if (p >= end) return;
+  const PagedPages& pg = a.pg;
+  Tile<E4M3> t;
+  TilePages tp = tile_pages<WIDE>(pg, x, p);
+  load_k<E4M3, WIDE>(pg, x, tp, t);
+  load_v<E4M3, WIDE>(pg, x, tp, t);
+  tp = tile_pages<WIDE>(pg, x, min(p + kPagedStep, end - 1) & ~31);
+  while (true) {
+    const int next = p + kPagedStep;
+    const bool more = next < end;
+    float lg[8];
+    uint32_t part[3][8];
+    tile_logits<E4M3>(t, q, lg);
+    if (more) load_k<E4M3, WIDE>(pg, x, tp, t);
+    // every query row sees all 32 positions, and all are there: no masks
+    if (p + kPagedTile <= least && t.all) {
+      tile_weights<E4M3, false>(t, p, limit, c, lg, part, st);
+    } else {
+      tile_weights<E4M3, true>(t, p, limit, c, lg, part, st);
+      if (!t.all) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+            if (!(t.there >> j & 1u)) t.v[j][i] = 0u;
+      }
+    }
+    tile_output<E4M3>(t, part, st);
+    if (!more) return;
+    load_v<E4M3, WIDE>(pg, x, tp, t);
+    p = next;
+    tp = tile_pages<WIDE>(pg, x, min(p + kPagedStep, end - 1) & ~31);
   }
 }
 
@@ -685,7 +815,9 @@ __global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs 
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int rows = a.T << a.lg, w = blockIdx.x;
-  const float c = a.scale * 1.4426950408889634f;
+  // e4m3 exponents are taken less 128: one power of two more in the logits'
+  // factor and, at the end, in the sums of V
+  const float ce = a.scale * (E4M3 ? 2.f : 1.f) * 1.4426950408889634f;
   // requests without any position: their outputs, shared out over the grid
   for (int u = w; u < a.B; u += a.nwg) {
     if (steps_of(a, u) != 0) continue;
@@ -723,10 +855,9 @@ __global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs 
     st.l = 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int s = step; s < step + take; ++s) {
-      const int p0 = s * kPagedStep + wave * kPagedTile;
-      if (p0 < x.n) attn_tile<E4M3, WIDE>(a, x, p0, limit, c, q, st);
-    }
+    attn_steps<E4M3, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
+                           min((step + take) * kPagedStep, x.n), limit, x.n - (a.T - 1), ce, q,
+                           st);
     st.l += __shfl_xor(st.l, 16);
     st.l += __shfl_xor(st.l, 32);
     if (g == 0) {
@@ -738,7 +869,7 @@ __global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs 
       for (int j = 0; j < 4; ++j) {
         float* o = &lds.o[wave][r][8 * (4 * g + j)];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = st.o[e][j];
+        for (int e = 0; e < 8; ++e) o[e] = E4M3 ? 2.f * st.o[e][j] : st.o[e][j];
       }
     }
     __syncthreads();
