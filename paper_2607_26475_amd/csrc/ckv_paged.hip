@@ -372,15 +372,28 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
   }
 }
 
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint2 ld8_nt(const uint8_t* p) {
+  const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
+  return make_uint2(v[0], v[1]);
+}
+
 // ---- keys and values of 16 positions ---------------------------------------------------
 // Sixteen consecutive positions from a multiple of 16 on.  With pages of at
 // least 16 positions (WIDE) they lie in one page, whose number is the same for
 // the whole wave; else every lane looks its rows' pages up.  Rows at or past
 // the context's end are read as its last row (rows there may hold anything, and
 // a weight of zero times a NaN is a NaN).
+typedef const __attribute__((address_space(4))) int32_t* TablePtr;  // read-only: scalar loads
+
+__device__ __forceinline__ TablePtr table_of(const PagedPages& pg, int b) {
+  return (TablePtr)(uintptr_t)(pg.table + (int64_t)b * pg.table_stride);
+}
+
 struct Ctx {
   int b, h, n;            // request, KV head, positions (> 0 where rows are read)
-  const int32_t* table;   // the request's
+  TablePtr table;         // the request's
 };
 
 // Page of a group's row `i` (0 .. 15) of the group that begins at p0, and the
@@ -439,7 +452,7 @@ __global__ __launch_bounds__(kPagedScoreThreads) void k_paged_score(PagedScoreAr
   x.b = unit / a.pg.Hkv;
   x.h = unit - x.b * a.pg.Hkv;
   x.n = clamp_len(a.ctx_lens[x.b], a.max_ctx);
-  x.table = a.pg.table + (int64_t)x.b * a.pg.table_stride;
+  x.table = table_of(a.pg, x.b);
   float* scores = a.scores + (int64_t)unit * a.max_ctx;
   bf16x8 q[4];
 #pragma unroll
@@ -575,94 +588,106 @@ struct WaveState {
 //            row, and picks its operands out of them by byte permutes
 // K of the next step is asked for once this step's logits have taken theirs,
 // V once the products have taken its rows: a wave always has one of them in
-// flight, and none needs a second set of registers.
+// flight, and none needs a second set of registers.  V rows are streamed past
+// the caches (every load takes whole rows; 4.4 GB of a bf16 batch 745 -> 667
+// us); K lines are read by two loads, half each, and stay.
 template <bool E4M3>
 struct Tile {
   KRaw<E4M3> k[2];
   uint32_t v[8][E4M3 ? 2 : 4];      // row j: bf16, or codes
   uint32_t ke[E4M3 ? 2 : 1], ve[E4M3 ? 2 : 1];  // exponent bytes of each half's four positions
-  uint32_t there;                   // bit j: position j has a page (lane's own rows)
-  bool all;                         // every lane's positions have pages
+  uint32_t there;                   // bit j: position j of the lane's rows has a page
 };
 
-// Pages of a step's two halves: with WIDE pages the same for every lane.
-struct TilePages {
-  int first[2], page[2];
+// Where a step's two halves lie: with WIDE pages the same for every lane.  Rows
+// past the context's end are read as its last row, so a row's offset from the
+// half's first is the smaller of its own and the last one's (cap).
+struct TileAt {
+  int first[2];
+  int page[2];      // WIDE: -1 where the half's page is not there
+  int32_t cap[2];   // WIDE: bytes
 };
 
 template <bool WIDE>
-__device__ __forceinline__ TilePages tile_pages(const PagedPages& pg, const Ctx& x, int p0) {
-  TilePages t;
+__device__ __forceinline__ TileAt tile_at(const PagedPages& pg, const Ctx& x, int p0) {
+  TileAt t;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     t.first[i] = min(p0 + 16 * i, (x.n - 1) & ~15);
-    t.page[i] = WIDE ? x.table[t.first[i] >> pg.shift] : 0;
+    if (WIDE) {
+      const int page = x.table[t.first[i] >> pg.shift];
+      t.page[i] = (unsigned)page < (unsigned)pg.num_pages ? page : -1;
+      t.cap[i] = min(x.n - 1 - t.first[i], 15) * pg.row_bytes;
+    }
   }
   return t;
 }
 
+// First byte of a half's first row, for the whole wave.
+__device__ __forceinline__ int64_t half_base(const PagedPages& pg, const Ctx& x, const TileAt& at,
+                                             int i) {
+  return row_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
+}
+
 template <bool E4M3, bool WIDE>
-__device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TilePages& tp,
+__device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TileAt& at,
                                        Tile<E4M3>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const int pos = min(tp.first[i] + r, x.n - 1);
-    int page = WIDE ? tp.page[i] : x.table[pos >> pg.shift];
-    if ((unsigned)page >= (unsigned)pg.num_pages) page = 0;
-    const int row = pos & ((1 << pg.shift) - 1);
-    t.k[i].load(pg.k + (page * pg.page_bytes + x.h * pg.head_bytes) + row * pg.row_bytes, g);
+    if (WIDE) {
+      const uint32_t off = min(r * pg.row_bytes, at.cap[i]);
+      t.k[i].load(pg.k + half_base(pg, x, at, i) + off, g);
+    } else {
+      const int pos = min(at.first[i] + r, x.n - 1), page = x.table[pos >> pg.shift];
+      const bool has = (unsigned)page < (unsigned)pg.num_pages;
+      t.k[i].load(pg.k + row_offset(pg, has ? page : 0, x.h, pos), g);
+    }
   }
 }
 
 template <bool E4M3, bool WIDE>
-__device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TilePages& tp,
+__device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TileAt& at,
                                        Tile<E4M3>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
-  const int mask = (1 << pg.shift) - 1;
   t.there = 0;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    int page = tp.page[i];
-    const bool has = (unsigned)page < (unsigned)pg.num_pages;
-    if (WIDE) {
-      if (!has) page = 0;
-      if (has) t.there |= 15u << (4 * i);
-      if (E4M3) {  // four positions' bytes at once: rows of one page, a multiple of 4
-        const int64_t at = (((int64_t)page * pg.Hkv + x.h) << pg.shift) +
-                           (tp.first[i] & mask) + 4 * g;
-        t.ke[i] = *reinterpret_cast<const uint32_t*>(pg.k_exps + at);
-        t.ve[i] = *reinterpret_cast<const uint32_t*>(pg.v_exps + at);
-      }
-    } else if (E4M3) {
-      t.ke[i] = t.ve[i] = 0;
+    if (E4M3 && WIDE) {  // four positions' bytes at once: rows of one page, a multiple of 4
+      const int64_t e = exp_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
+      t.ke[i] = *reinterpret_cast<const uint32_t*>(pg.k_exps + e + 4 * g);
+      t.ve[i] = *reinterpret_cast<const uint32_t*>(pg.v_exps + e + 4 * g);
     }
+    if (E4M3 && !WIDE) t.ke[i] = t.ve[i] = 0;
+    if (WIDE && at.page[i] >= 0) t.there |= 15u << (4 * i);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      const int pos = min(tp.first[i] + 4 * g + j, x.n - 1);
-      const int row = pos & mask;
-      if (!WIDE) {
-        page = x.table[pos >> pg.shift];
+      const uint8_t* p;
+      if (WIDE) {
+        const uint32_t off = min((4 * g + j) * pg.row_bytes, at.cap[i]);
+        p = pg.v + half_base(pg, x, at, i) + off;
+      } else {
+        const int pos = min(at.first[i] + 4 * g + j, x.n - 1);
+        int page = x.table[pos >> pg.shift];
         if ((unsigned)page < (unsigned)pg.num_pages) t.there |= 1u << (4 * i + j);
         else page = 0;
         if (E4M3) {
-          const int64_t at = (((int64_t)page * pg.Hkv + x.h) << pg.shift) + row;
-          t.ke[i] |= (uint32_t)pg.k_exps[at] << (8 * j);
-          t.ve[i] |= (uint32_t)pg.v_exps[at] << (8 * j);
+          const int64_t e = exp_offset(pg, page, x.h, pos);
+          t.ke[i] |= (uint32_t)pg.k_exps[e] << (8 * j);
+          t.ve[i] |= (uint32_t)pg.v_exps[e] << (8 * j);
         }
+        p = pg.v + row_offset(pg, page, x.h, pos);
       }
-      const uint8_t* p = pg.v + (page * pg.page_bytes + x.h * pg.head_bytes) + row * pg.row_bytes;
       uint32_t* v = t.v[4 * i + j];
       if (E4M3) {
-        const uint2 w = *reinterpret_cast<const uint2*>(p + 8 * r);
+        const uint2 w = ld8_nt(p + 8 * r);
         v[0] = w.x, v[1] = w.y;
       } else {
-        const uint4 w = *reinterpret_cast<const uint4*>(p + 16 * r);
+        const uint4 w = ld16_nt(reinterpret_cast<const uint16_t*>(p) + 8 * r);
         v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
       }
     }
   }
-  t.all = WIDE ? t.there == 255u : __all(t.there == 255u);
 }
 
 // x * 2^(byte j of w - 128), bytes already taken as signed (w ^ 0x80808080).
@@ -670,8 +695,8 @@ __device__ __forceinline__ float scaled(float x, uint32_t w, int j) {
   return __builtin_amdgcn_ldexpf(x, (int)(w << (24 - 8 * j)) >> 24);
 }
 
-// Products of a step for query row r: lg[j] at position p0 + 16 (j / 4) + 4g +
-// j % 4, keys' exponents and the scale not yet in them.
+// Logits of a step for query row r: lg[j] at position p0 + 16 (j / 4) + 4g +
+// j % 4, before the scale.
 template <bool E4M3>
 __device__ __forceinline__ void tile_logits(const Tile<E4M3>& t, const bf16x8* q, float* lg) {
 #pragma unroll
@@ -680,22 +705,32 @@ __device__ __forceinline__ void tile_logits(const Tile<E4M3>& t, const bf16x8* q
 #pragma unroll
     for (int f = 0; f < 4; ++f) s = mfma_16x16x32(t.k[i].frag(f), q[f], s);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) lg[4 * i + j] = s[j];
+    for (int j = 0; j < 4; ++j)
+      lg[4 * i + j] = s[j];
   }
 }
 
-template <bool E4M3, bool MASKED>
-__device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, int p0, int limit, float c,
-                                             float* lg, uint32_t part[3][8], WaveState& st) {
+// Positions that the query row does not see, or that are not there: logits of
+// -inf, V rows of zeros (what was read in their place may be anything).
+template <bool E4M3>
+__device__ __forceinline__ void tile_mask(Tile<E4M3>& t, int p0, int limit, float* lg) {
   const int g = (threadIdx.x & 63) >> 4;
-  bool ok[8];
-  float top = -INFINITY;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    if (E4M3) lg[j] = scaled(lg[j], t.ke[j >> 2] ^ 0x80808080u, j & 3);
-    ok[j] = !MASKED || (p0 + 16 * (j >> 2) + 4 * g + (j & 3) < limit && (t.there >> j & 1u));
-    top = fmaxf(top, ok[j] ? lg[j] : -INFINITY);
+    const bool has = t.there >> j & 1u;
+    if (!has || p0 + 16 * (j >> 2) + 4 * g + (j & 3) >= limit) lg[j] = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+      if (!has) t.v[j][i] = 0u;
   }
+}
+
+template <bool E4M3>
+__device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, float c, const float* lg,
+                                             uint32_t part[3][8], WaveState& st) {
+  float top = lg[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) top = fmaxf(top, lg[j]);
   top = fmaxf(top, __shfl_xor(top, 16));
   top = fmaxf(top, __shfl_xor(top, 32));
   const float m = fmaxf(st.m, top * c);
@@ -708,15 +743,12 @@ __device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, int p0, int li
       for (int j = 0; j < 4; ++j) st.o[e][j] *= f;
     st.m = m;
   }
+  const float less = m == -INFINITY ? 0.f : -m;  // nothing seen yet: all weights are 0
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    float p = __builtin_amdgcn_exp2f(fmaf(lg[j], c, -m));
-    if (MASKED) p = ok[j] ? p : 0.f;
+    float p = __builtin_amdgcn_exp2f(fmaf(lg[j], c, less));
     st.l += p;
-    if (E4M3) {
-      p = scaled(p, t.ve[j >> 2] ^ 0x80808080u, j & 3);
-      if (MASKED) p = ok[j] ? p : 0.f;
-    }
+    if (E4M3) p = scaled(p, t.ve[j >> 2] ^ 0x80808080u, j & 3);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       part[i][j] = __float_as_uint(p);
@@ -764,44 +796,46 @@ __device__ __forceinline__ void tile_output(const Tile<E4M3>& t, const uint32_t 
   }
 }
 
-// A wave's steps of a piece: positions [p, end) in strides of kPagedStep.
+template <bool E4M3>
+__device__ __forceinline__ void tile_rest(Tile<E4M3>& t, bool masked, int p, int limit, float c,
+                                          float* lg, WaveState& st) {
+  if (E4M3) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lg[j] = scaled(lg[j], t.ke[j >> 2] ^ 0x80808080u, j & 3);
+  }
+  if (masked) tile_mask<E4M3>(t, p, limit, lg);
+  uint32_t part[3][8];
+  tile_weights<E4M3>(t, c, lg, part, st);
+  tile_output<E4M3>(t, part, st);
+}
+
+// A wave's steps of a piece: positions [p, end) in strides of kPagedStep.  Only
+// the last one can meet the end of a query row's positions (T <= 16 of them are
+// not seen by all); the loop's loads are unconditional, so that each wait is
+// for the rows it needs and not for all that is in flight.
 template <bool E4M3, bool WIDE>
 __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x, int p, int end,
-                                           int limit, int least, float c, const bf16x8* q,
-                                           WaveState& st) {
+                                           int limit, float c, const bf16x8* q, WaveState& st) {
   if (p >= end) return;
   const PagedPages& pg = a.pg;
   Tile<E4M3> t;
-  TilePages tp = tile_pages<WIDE>(pg, x, p);
-  load_k<E4M3, WIDE>(pg, x, tp, t);
-  load_v<E4M3, WIDE>(pg, x, tp, t);
-  tp = tile_pages<WIDE>(pg, x, min(p + kPagedStep, end - 1) & ~31);
-  while (true) {
-    const int next = p + kPagedStep;
-    const bool more = next < end;
-    float lg[8];
-    uint32_t part[3][8];
+  float lg[8];
+  TileAt at = tile_at<WIDE>(pg, x, p);
+  load_k<E4M3, WIDE>(pg, x, at, t);
+  load_v<E4M3, WIDE>(pg, x, at, t);
+  if (p + kPagedStep < end) at = tile_at<WIDE>(pg, x, p + kPagedStep);
+  for (; p + kPagedStep < end; p += kPagedStep) {
     tile_logits<E4M3>(t, q, lg);
-    if (more) load_k<E4M3, WIDE>(pg, x, tp, t);
-    // every query row sees all 32 positions, and all are there: no masks
-    if (p + kPagedTile <= least && t.all) {
-      tile_weights<E4M3, false>(t, p, limit, c, lg, part, st);
-    } else {
-      tile_weights<E4M3, true>(t, p, limit, c, lg, part, st);
-      if (!t.all) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
-            if (!(t.there >> j & 1u)) t.v[j][i] = 0u;
-      }
-    }
-    tile_output<E4M3>(t, part, st);
-    if (!more) return;
-    load_v<E4M3, WIDE>(pg, x, tp, t);
-    p = next;
-    tp = tile_pages<WIDE>(pg, x, min(p + kPagedStep, end - 1) & ~31);
+    load_k<E4M3, WIDE>(pg, x, at, t);
+    __builtin_amdgcn_sched_barrier(0);
+    const bool masked = WIDE ? t.there != 255u : __any(t.there != 255u);
+    tile_rest<E4M3>(t, masked, p, limit, c, lg, st);
+    __builtin_amdgcn_sched_barrier(0);
+    load_v<E4M3, WIDE>(pg, x, at, t);
+    at = tile_at<WIDE>(pg, x, min(p + 2 * kPagedStep, end - 1));
   }
+  tile_logits<E4M3>(t, q, lg);
+  tile_rest<E4M3>(t, true, p, limit, c, lg, st);
 }
 
 __device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h, int row) {
@@ -810,7 +844,7 @@ __device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h,
 }
 
 template <bool E4M3, bool WIDE>
-__global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs a) {
+__global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -842,7 +876,7 @@ __global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs 
     x.b = b;
     x.h = h;
     x.n = clamp_len(a.ctx_lens[b], a.max_ctx);
-    x.table = a.pg.table + (int64_t)b * a.pg.table_stride;
+    x.table = table_of(a.pg, b);
     const int64_t qrow = out_row(a, b, h, r);
     const int limit = r < rows ? x.n - (a.T - 1 - (r >> a.lg)) : 0;
     bf16x8 q[4];
@@ -856,8 +890,7 @@ __global__ __launch_bounds__(kPagedAttnThreads) void k_paged_attn(PagedAttnArgs 
 #pragma unroll
     for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
     attn_steps<E4M3, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
-                           min((step + take) * kPagedStep, x.n), limit, x.n - (a.T - 1), ce, q,
-                           st);
+                           min((step + take) * kPagedStep, x.n), limit, ce, q, st);
     st.l += __shfl_xor(st.l, 16);
     st.l += __shfl_xor(st.l, 32);
     if (g == 0) {

@@ -83,7 +83,10 @@ struct PagedTail {
 constexpr int kPagedTile = 32;              // positions of a wave's step
 constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
 constexpr int kMaxPagedWgs = 1024;
-constexpr int kPagedWgsPerCu = 2;
+#ifndef V_WG
+#define V_WG 2
+#endif
+constexpr int kPagedWgsPerCu = V_WG;
 constexpr int kPagedScoreRows = 512;        // positions of a scoring workgroup
 
 struct PagedAttnArgs {
