@@ -305,6 +305,9 @@ int ckv_paged_read(const ckv_shape* shape, const ckv_paged_cache* cache,
   CKV_PTR(ctx_lens);
   CKV_PTR(k_dst);
   CKV_PTR(v_dst);
+  // work-items per dispatch must stay below 2^32
+  if ((int64_t)d.U * ((k + kReadSlots - 1) / kReadSlots) >= ((int64_t)1 << 24))
+    return fail(CKV_EUNSUPPORTED, "grid too large for this shape");
   if (d.U == 0) return CKV_OK;
   hipStream_t s = (hipStream_t)stream;
   CKV_RC(debug_check(s, ctx_lens, idx, n_sel, d.B, d.Hkv, d.max_ctx, k));
@@ -314,9 +317,9 @@ int ckv_paged_read(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.n_sel = n_sel;
   a.k_dst = k_dst;
   a.v_dst = v_dst;
-  a.items = (int64_t)d.U * k * 32;
   a.max_ctx = d.max_ctx;
   a.k = k;
+  a.units = d.U;
   CKV_TRY_HIP(launch_paged_read(a, cache->kind == CKV_CACHE_E4M3, s), "paged read launch");
   return CKV_OK;
 }

@@ -58,8 +58,8 @@ struct PagedReadArgs {
   const int32_t* n_sel;    // [U]
   uint16_t* k_dst;
   uint16_t* v_dst;
-  int64_t items;           // U * k * 32
-  int32_t max_ctx, k;
+  int32_t max_ctx, k, units;
+  int32_t chunks;          // workgroups a unit (the launcher's)
 };
 
 struct PagedScoreArgs {
@@ -83,10 +83,8 @@ struct PagedTail {
 constexpr int kPagedTile = 32;              // positions of a wave's step
 constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
 constexpr int kMaxPagedWgs = 1024;
-#ifndef V_WG
-#define V_WG 2
-#endif
-constexpr int kPagedWgsPerCu = V_WG;
+constexpr int kPagedWgsPerCu = 2;
+constexpr int kReadSlots = 32;              // slots of a reading workgroup
 constexpr int kPagedScoreRows = 512;        // positions of a scoring workgroup
 
 struct PagedAttnArgs {
