@@ -400,11 +400,10 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _call(name: str, t: torch.Tensor, stream, *args) -> None:
+def _call(fn, t: torch.Tensor, stream, *args) -> None:
     """Calls an entry with its last argument, the stream (None: the current one
     of t's device), with t's device current."""
     dev = t.get_device()
-    fn = getattr(_lib, name)
     handle = _raw_stream(dev) if stream is None else _stream(stream)
     if dev == torch.cuda.current_device():
         status = fn(*args, handle)
@@ -412,7 +411,7 @@ def _call(name: str, t: torch.Tensor, stream, *args) -> None:
         with torch.cuda.device(dev):
             status = fn(*args, handle)
     if status:
-        _check(name, status)
+        _check(fn.__name__, status)
 
 
 def _int32(name: str, t: torch.Tensor, n: int) -> None:
@@ -459,6 +458,7 @@ def rows_for(src: torch.Tensor, dst: Optional[torch.Tensor] = None) -> Rows:
     r = Rows(src.data_ptr(), dst.data_ptr(), src.stride(0), src.stride(1), dst.stride(0),
              dst.stride(1), src.shape[1], 0)
     r.keep = (src, dst)
+    r.holds = (src.shape[0], src.shape[2], _ROPE_TYPES.get(src.dtype))
     return r
 
 
@@ -466,10 +466,9 @@ _ROPE_TYPES = {torch.bfloat16: ROPE_BF16, torch.float32: ROPE_F32}
 
 
 def _rows_ok(name: str, rows: Rows, rope: Rope, n: int) -> None:
-    if not hasattr(rows, "keep"):
-        return  # filled in by hand
-    t = rows.keep[0]
-    if t.shape[0] < n or t.shape[2] != rope.head_dim or _ROPE_TYPES.get(t.dtype) != rope.type:
+    holds = getattr(rows, "holds", None)  # None: filled in by hand
+    if holds is not None and (holds[0] < n or holds[1] != rope.head_dim or holds[2] != rope.type):
+        t = rows.keep[0]
         raise ValueError(f"{name}: {n} tokens of rows of {rope.head_dim} elements of the rope's "
                          f"type, not {t.dtype} {tuple(t.shape)}")
 
@@ -482,7 +481,7 @@ def rope_rows(rope: Rope, positions: torch.Tensor, q: Rows, k: Optional[Rows] = 
     _rows_ok("q", q, rope, n)
     if k is not None:
         _rows_ok("k", k, rope, n)
-    _call("ckv_rope_rows", positions, stream, rope, n, positions.data_ptr(), q, k)
+    _call(_lib.ckv_rope_rows, positions, stream, rope, n, positions.data_ptr(), q, k)
 
 
 def paged_cache_for(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
@@ -510,6 +509,7 @@ def paged_cache_for(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: to
                    k_pages.shape[2], k_pages.shape[0],
                    page_table.shape[1] if page_table.shape[0] == 1 else page_table.stride(0))
     c.keep = (k_pages, v_pages, page_table, k_exps, v_exps)
+    c.holds = (k_pages.shape[1], page_table.shape[0])
     return c
 
 
@@ -519,12 +519,10 @@ def _stride(t: torch.Tensor, i: int) -> int:
 
 
 def _cache_ok(shape: Shape, cache: PagedCache) -> None:
-    if not hasattr(cache, "keep"):
-        return  # filled in by hand
-    pages, table = cache.keep[0], cache.keep[2]
-    if pages.shape[1] != shape.num_kv_heads or table.shape[0] < shape.batch:
-        raise ValueError(f"a cache of {pages.shape[1]} heads and {table.shape[0]} requests for a "
-                         f"shape of {shape.num_kv_heads} and {shape.batch}")
+    holds = getattr(cache, "holds", None)  # None: filled in by hand
+    if holds is not None and (holds[0] != shape.num_kv_heads or holds[1] < shape.batch):
+        raise ValueError(f"a cache of {holds[0]} heads and {holds[1]} requests for a shape of "
+                         f"{shape.num_kv_heads} and {shape.batch}")
 
 
 def paged_write(shape: Shape, cache: PagedCache, requests, positions: torch.Tensor,
@@ -537,15 +535,16 @@ def paged_write(shape: Shape, cache: PagedCache, requests, positions: torch.Tens
     _int32("positions", positions, n)
     if requests is not None:
         _int32("requests", requests, n)
-    want = (n, shape.num_kv_heads, 128)
-    if k.shape != want or v.shape != want or k.stride() != v.stride() or k.stride(2) != 1 or \
-            (k.stride(1) != 128 and want[1] > 1) or k.dtype != torch.bfloat16 or \
+    heads = shape.num_kv_heads
+    want, strides = (n, heads, 128), k.stride()
+    if k.shape != want or v.shape != want or strides != v.stride() or strides[2] != 1 or \
+            (strides[1] != 128 and heads > 1) or k.dtype != torch.bfloat16 or \
             v.dtype != torch.bfloat16:
         raise ValueError(f"k, v: bf16 {want} with dense heads, not {k.dtype} {tuple(k.shape)}")
     if q is not None and rope is not None:
         _rows_ok("q", q, rope, n)
-    stride = k.stride(0) if n > 1 else max(k.stride(0), 128 * want[1])
-    _call("ckv_paged_write", positions, stream, shape, cache, n, _ptr(requests),
+    stride = strides[0] if n > 1 else max(strides[0], 128 * heads)
+    _call(_lib.ckv_paged_write, positions, stream, shape, cache, n, _ptr(requests),
           positions.data_ptr(), k.data_ptr(), v.data_ptr(), stride, rope, q)
 
 
@@ -563,7 +562,7 @@ def paged_read(shape: Shape, cache: PagedCache, ctx_lens: torch.Tensor, idx, n_s
     for t in (k_dst, v_dst):
         if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.numel() < units * k * 128:
             raise ValueError(f"k_dst, v_dst: dense bf16 of {units * k * 128} elements")
-    _call("ckv_paged_read", ctx_lens, stream, shape, cache, ctx_lens.data_ptr(), _ptr(idx),
+    _call(_lib.ckv_paged_read, ctx_lens, stream, shape, cache, ctx_lens.data_ptr(), _ptr(idx),
           _ptr(n_sel), k, k_dst.data_ptr(), v_dst.data_ptr())
 
 
@@ -579,7 +578,7 @@ def paged_score_keys(shape: Shape, cache: PagedCache, q: torch.Tensor, ctx_lens:
     _int32("ctx_lens", ctx_lens, shape.batch)
     _dense("q", q, torch.bfloat16, shape.batch * shape.num_q_heads * 128)
     _dense("scores", scores, torch.float32, shape.batch * shape.num_kv_heads * shape.max_ctx)
-    _call("ckv_paged_score_keys", ctx_lens, stream, shape, cache, q.data_ptr(),
+    _call(_lib.ckv_paged_score_keys, ctx_lens, stream, shape, cache, q.data_ptr(),
           ctx_lens.data_ptr(), scale, scores.data_ptr())
 
 
@@ -595,7 +594,7 @@ def paged_decode_attn(shape: Shape, cache: PagedCache, num_tokens: int, q: torch
     _dense("out", out, torch.float32, rows * 128)
     if lse is not None:
         _dense("lse", lse, torch.float32, rows)
-    _call("ckv_paged_decode_attn", ctx_lens, stream, shape, cache, num_tokens, q.data_ptr(),
+    _call(_lib.ckv_paged_decode_attn, ctx_lens, stream, shape, cache, num_tokens, q.data_ptr(),
           ctx_lens.data_ptr(), scale, out.data_ptr(), _ptr(lse), _ptr(ws),
           ws.numel() if ws is not None else 0)
 

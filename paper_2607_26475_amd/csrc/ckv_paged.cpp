@@ -335,10 +335,6 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
   CKV_PTR(q);
   CKV_PTR(ctx_lens);
   CKV_PTR(scores);
-  a.chunks = (d.max_ctx + kPagedScoreRows - 1) / kPagedScoreRows;
-  // work-items per dispatch must stay below 2^32
-  if ((int64_t)d.U * a.chunks >= ((int64_t)1 << 24))
-    return fail(CKV_EUNSUPPORTED, "grid too large for this shape");
   if (d.U == 0) return CKV_OK;
   hipStream_t s = (hipStream_t)stream;
   CKV_RC(debug_check(s, ctx_lens, nullptr, nullptr, d.B, d.Hkv, d.max_ctx, 1));
@@ -348,8 +344,15 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.scores = scores;
   a.scale = scale;
   a.Hq = d.Hq;
+  a.B = d.B;
   a.max_ctx = d.max_ctx;
   a.units = d.U;
+  const int64_t steps = (int64_t)d.U * ((d.max_ctx + kScoreStep - 1) / kScoreStep);
+  const int slots = score_wgs_per_cu(a.pg.shift >= 4) * device_cus();
+  a.direct = steps <= slots;
+  a.nwg = a.direct ? (int)steps : slots;
+  a.piece = a.direct ? kScoreStep : kScorePiece;
+  a.chunks = (d.max_ctx + a.piece - 1) / a.piece;
   CKV_TRY_HIP(launch_paged_score(a, cache->kind == CKV_CACHE_E4M3, d.G, s), "paged score launch");
   return CKV_OK;
 }

@@ -525,6 +525,36 @@ struct KRaw {
     for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
       w[i] = *reinterpret_cast<const uint4*>(row + 64 * i + 16 * g);
   }
+  // The same from whole 128-byte lines, streamed past the caches (rows of one
+  // page from `base`; read in halves, a line is fetched for the first and has to
+  // stay for the second): each load takes both halves of a line of eight rows, the
+  // second half through the lanes of r >= 8; lanes r and r ^ 8 then swap what
+  // belongs to the other's row.
+  __device__ __forceinline__ void load_lines(const uint8_t* base, int32_t row_bytes, int32_t cap,
+                                             int g, int r) {
+    const uint8_t* p = base + 8 * (r & 8) + 16 * g;
+    const uint32_t at[2] = {(uint32_t)min((r & 7) * row_bytes, cap),
+                            (uint32_t)min(((r & 7) + 8) * row_bytes, cap)};
+#pragma unroll
+    for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+      w[i] = ld16_nt(reinterpret_cast<const uint16_t*>(p + at[i & 1] + 128 * (i >> 1)));
+  }
+  __device__ __forceinline__ void swap_halves(int r) {
+    const bool lo = r < 8;
+#pragma unroll
+    for (int l = 0; l < (E4M3 ? 2 : 4); l += 2) {
+      uint32_t a[4] = {w[l].x, w[l].y, w[l].z, w[l].w};
+      uint32_t b[4] = {w[l + 1].x, w[l + 1].y, w[l + 1].z, w[l + 1].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t y = dpp_u32<0x128, 0xF, false>(lo ? b[i] : a[i]);  // row_ror:8
+        if (lo) b[i] = y;
+        else a[i] = y;
+      }
+      w[l] = make_uint4(a[0], a[1], a[2], a[3]);
+      w[l + 1] = make_uint4(b[0], b[1], b[2], b[3]);
+    }
+  }
   __device__ __forceinline__ bf16x8 frag(int f) const {
     if (!E4M3) return as_bf16x8(w[f]);
     const uint4 q = w[f >> 1];
@@ -532,103 +562,51 @@ struct KRaw {
   }
 };
 
-// ---- scores ----------------------------------------------------------------------------
-// Four waves score kPagedScoreRows positions of a unit, 64 a step: queries x
-// keys on 16x16x32 products, heads in the rows, so that the largest over a
-// group's heads is taken over a lane's registers and, past four heads, over
-// lane rows.
-constexpr int kPagedScoreThreads = 256;
-
-template <bool E4M3, bool WIDE, int G>
-__global__ __launch_bounds__(kPagedScoreThreads) void k_paged_score(PagedScoreArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int g = lane >> 4, r = lane & 15;
-  const int unit = blockIdx.x / a.chunks, chunk = blockIdx.x - unit * a.chunks;
-  Ctx x;
-  x.b = unit / a.pg.Hkv;
-  x.h = unit - x.b * a.pg.Hkv;
-  x.n = clamp_len(a.ctx_lens[x.b], a.max_ctx);
-  x.table = table_of(a.pg, x.b);
-  float* scores = a.scores + (int64_t)unit * a.max_ctx;
-  bf16x8 q[4];
-#pragma unroll
-  for (int f = 0; f < 4; ++f)
-    q[f] = as_bf16x8(r < G ? ld16(a.q + ((int64_t)x.b * a.Hq + x.h * G + r) * kD +
-                                  frag_base<E4M3>(f, g))
-                           : make_uint4(0u, 0u, 0u, 0u));
-  constexpr int kRows = kPagedScoreRows / 4;  // of a wave
-  for (int p = chunk * kPagedScoreRows + wave * kRows;
-       p < min((chunk * kPagedScoreRows) + (wave + 1) * kRows, a.max_ctx); p += 64) {
-    float mine = -INFINITY;  // of position p + lane
-    if (p < x.n) {
-      KRaw<E4M3> k[4];
-      int page[4], pos[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        group_row<WIDE>(a.pg, x, p + 16 * i, r, &page[i], &pos[i]);
-        const bool there = (unsigned)page[i] < (unsigned)a.pg.num_pages;
-        if (!there) page[i] = -1;
-        k[i].load(a.pg.k + row_offset(a.pg, max(page[i], 0), x.h, pos[i]), g);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int f = 0; f < 4; ++f) acc = mfma_16x16x32(q[f], k[i].frag(f), acc);
-        // register j of lane (g, r): head 4g + j at position r
-        float best = acc[0];
-#pragma unroll
-        for (int j = 1; j < (G < 4 ? G : 4); ++j) best = fmaxf(best, acc[j]);
-        if (G <= 4) best = __shfl(best, r);  // heads are in lane row 0
-        if (G >= 8) best = fmaxf(best, __shfl_xor(best, 16));
-        if (G == 8) best = __shfl(best, r);
-        if (G == 16) best = fmaxf(best, __shfl_xor(best, 32));
-        best *= a.scale;
-        if (E4M3)
-          best = times_exp(best, a.pg.k_exps[exp_offset(a.pg, max(page[i], 0), x.h, pos[i])]);
-        if (page[i] >= 0 && p + 16 * i + r < x.n && g == i) mine = best;
-      }
-    }
-    if (p + lane < a.max_ctx) scores[p + lane] = mine;
-  }
-}
-
-// ---- attention -----------------------------------------------------------------------
-// Work is counted in steps of kPagedStep positions of a unit (request, KV
-// head), over all units in order: workgroup w of W takes the steps [total * w /
-// W, total * (w + 1) / W), whatever requests they belong to, so that a ragged
-// batch, one long request and many short ones all fill the device evenly, and
-// the division is the device's own (lengths are device data; max_ctx says
-// little about them).  Fewer steps than workgroups: one each for the first ones.  A unit inside one range is finished there; the partials
-// of one that ranges share are joined by k_paged_merge.
+// ---- ranges of work ------------------------------------------------------------------
+// Work is counted in steps of STEP positions of a unit (request, KV head), over
+// all units in order: workgroup w of W takes the steps [total * w / W, total *
+// (w + 1) / W), whatever requests they belong to, so that a ragged batch, one
+// long request and many short ones all fill the device evenly, and the division
+// is the device's own (lengths are device data; max_ctx says little about
+// them).  Fewer steps than workgroups: one each for the first ones.
 __device__ __forceinline__ int64_t range_start(int64_t total, int w, int nwg) {
   return total * w / nwg;
 }
 
-__device__ __forceinline__ int steps_of(const PagedAttnArgs& a, int b) {
-  return (clamp_len(a.ctx_lens[b], a.max_ctx) + kPagedStep - 1) / kPagedStep;
+struct Lens {
+  const int32_t* ctx_lens;
+  int32_t B, Hkv, max_ctx;
+  __device__ __forceinline__ int operator()(int b) const {
+    return clamp_len(ctx_lens[b], max_ctx);
+  }
+};
+
+template <int STEP>
+__device__ __forceinline__ int steps_of(const Lens& n, int b) {
+  return (n(b) + STEP - 1) / STEP;
 }
 
-constexpr int kPagedAttnThreads = 256;
-
-struct PagedAttnLds {
-  float m[4][16], l[4][16];
-  float o[4][16][kPartStride];
+struct RangeLds {
   int64_t wave_sum[4];
-  int64_t off;             // of the range's first step in its request
+  int64_t off;
   int32_t b;
 };
 
-// Steps of all requests; lds.b and lds.off get the request of step `first` and
-// the step's offset there (the range is not empty).
-__device__ __forceinline__ int64_t find_range(const PagedAttnArgs& a, PagedAttnLds& lds,
-                                              int64_t* s0, int64_t* s1) {
+// A workgroup's range and where it begins: step s0's request and head, and its
+// number in that unit.
+struct Range {
+  int64_t s0, s1, total;
+  int32_t b, h, step, steps;  // steps: of the unit
+};
+
+template <int STEP>
+__device__ __forceinline__ Range find_range(const Lens& n, int max_wgs, RangeLds& lds) {
+  constexpr int kThreads = 256;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int per = (a.B + kPagedAttnThreads - 1) / kPagedAttnThreads;
-  const int b0 = min(tid * per, a.B), b1 = min(b0 + per, a.B);
+  const int per = (n.B + kThreads - 1) / kThreads;
+  const int b0 = min(tid * per, n.B), b1 = min(b0 + per, n.B);
   int64_t mine = 0;
-  for (int b = b0; b < b1; ++b) mine += (int64_t)steps_of(a, b) * a.pg.Hkv;
+  for (int b = b0; b < b1; ++b) mine += (int64_t)steps_of<STEP>(n, b) * n.Hkv;
   int64_t incl = mine;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) {
@@ -637,30 +615,220 @@ __device__ __forceinline__ int64_t find_range(const PagedAttnArgs& a, PagedAttnL
   }
   if (lane == 63) lds.wave_sum[wave] = incl;
   __syncthreads();
-  int64_t total = 0;
+  Range r;
+  r.total = 0;
 #pragma unroll
   for (int w = 0; w < 4; ++w) {
     if (w < wave) incl += lds.wave_sum[w];
-    total += lds.wave_sum[w];
+    r.total += lds.wave_sum[w];
   }
-  const int nwg = (int)min((int64_t)a.nwg, total), w = min((int)blockIdx.x, nwg);
-  *s0 = nwg ? range_start(total, w, nwg) : 0;
-  *s1 = nwg ? range_start(total, min(w + 1, nwg), nwg) : 0;
+  const int nwg = (int)min((int64_t)max_wgs, r.total), w = min((int)blockIdx.x, nwg);
+  r.s0 = nwg ? range_start(r.total, w, nwg) : 0;
+  r.s1 = nwg ? range_start(r.total, min(w + 1, nwg), nwg) : 0;
   int64_t at = incl - mine;
-  if (*s0 < *s1 && *s0 >= at && *s0 < incl) {
+  if (r.s0 < r.s1 && r.s0 >= at && r.s0 < incl) {
     for (int b = b0; b < b1; ++b) {
-      const int64_t n = (int64_t)steps_of(a, b) * a.pg.Hkv;
-      if (*s0 < at + n) {
+      const int64_t s = (int64_t)steps_of<STEP>(n, b) * n.Hkv;
+      if (r.s0 < at + s) {
         lds.b = b;
-        lds.off = *s0 - at;
+        lds.off = r.s0 - at;
         break;
       }
-      at += n;
+      at += s;
     }
   }
   __syncthreads();
-  return total;
+  r.b = r.h = r.step = 0;
+  r.steps = 1;
+  if (r.s0 < r.s1) {
+    r.b = __builtin_amdgcn_readfirstlane(lds.b);
+    r.steps = __builtin_amdgcn_readfirstlane(steps_of<STEP>(n, r.b));
+    r.h = __builtin_amdgcn_readfirstlane((int)(lds.off / r.steps));
+    r.step = __builtin_amdgcn_readfirstlane((int)(lds.off % r.steps));
+  }
+  return r;
 }
+
+// The unit after the range's current one.
+template <int STEP>
+__device__ __forceinline__ void next_unit(const Lens& n, int64_t at, Range& r) {
+  r.step = 0;
+  if (++r.h < n.Hkv || at >= r.s1) return;
+  r.h = 0;
+  do {
+    r.steps = __builtin_amdgcn_readfirstlane(steps_of<STEP>(n, ++r.b));
+  } while (r.steps == 0);
+}
+
+// ---- scores ----------------------------------------------------------------------------
+// A workgroup scores a range of steps of kScoreStep positions, 64 a wave, with
+// the next step's keys on their way: queries x keys on 16x16x32 products, heads in the
+// rows (row m: head m % G, so that for up to four heads every lane row has them
+// all) and positions in the columns, so that the largest over a group's heads is
+// taken over a lane's registers and, past four heads, over lane rows.  Lane
+// row i keeps the results of the step's i-th 16 positions: lane l has position
+// p + l.  Scores wait in LDS while keys are loaded: a store between loads would
+// be waited for with them (106 -> 93 us for 0.54 GB of e4m3 keys).
+constexpr int kPagedScoreThreads = 256;
+constexpr int kScoreHold = 16;  // steps whose scores a wave holds
+
+template <bool E4M3>
+struct ScoreStep {
+  KRaw<E4M3> k[4];
+  uint32_t e;   // of the lane's own position
+  bool there;   // likewise
+};
+
+// Pages of a step's 64 positions: four halves of one page each (WIDE, for the
+// whole wave), or the lane's own positions' and its key rows' (page of row 16 i
+// + r in row[i]), looked up a step ahead.
+template <bool WIDE>
+struct ScorePages {
+  int row[4];
+  int own;
+};
+
+template <bool WIDE>
+__device__ __forceinline__ ScorePages<WIDE> score_pages(const PagedPages& pg, const Ctx& x,
+                                                        int p) {
+  const int lane = threadIdx.x & 63, r = lane & 15;
+  ScorePages<WIDE> t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    t.row[i] = x.table[min(p + 16 * i + (WIDE ? 0 : r), x.n - 1) >> pg.shift];
+  if (WIDE) {
+    const int g = lane >> 4;
+    t.own = g & 2 ? (g & 1 ? t.row[3] : t.row[2]) : (g & 1 ? t.row[1] : t.row[0]);
+  } else {
+    t.own = x.table[min(p + lane, x.n - 1) >> pg.shift];
+  }
+  return t;
+}
+
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void load_score_step(const PagedPages& pg, const Ctx& x, int p,
+                                                const ScorePages<WIDE>& t, ScoreStep<E4M3>& s) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  s.there = (unsigned)t.own < (unsigned)pg.num_pages && p + lane < x.n;
+  if (E4M3) s.e = pg.k_exps[exp_offset(pg, s.there ? t.own : 0, x.h, min(p + lane, x.n - 1))];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const bool has = (unsigned)t.row[i] < (unsigned)pg.num_pages;
+    if (WIDE) {
+      const int first = min(p + 16 * i, (x.n - 1) & ~15);
+      const uint8_t* base = pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, first);
+      const int32_t cap = min(x.n - 1 - first, 15) * pg.row_bytes;
+      s.k[i].load_lines(base, pg.row_bytes, cap, g, r);
+    } else {
+      s.k[i].load(pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, min(p + 16 * i + r, x.n - 1)),
+                  g);
+    }
+  }
+}
+
+// Scores of a step: the largest over the group's heads, of position p + lane.
+template <bool E4M3, bool WIDE, int G>
+__device__ __forceinline__ float step_scores(ScoreStep<E4M3>& s, const bf16x8* q, float scale) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  float best[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (WIDE) s.k[i].swap_halves(r);
+#pragma unroll
+    for (int f = 0; f < 4; ++f) acc = mfma_16x16x32(q[f], s.k[i].frag(f), acc);
+    best[i] = acc[0];  // register j of lane (g, r): head (4g + j) % G at position r
+#pragma unroll
+    for (int j = 1; j < (G < 4 ? G : 4); ++j) best[i] = fmaxf(best[i], acc[j]);
+    if (G >= 8) best[i] = fmaxf(best[i], __shfl_xor(best[i], 16));
+    if (G == 16) best[i] = fmaxf(best[i], __shfl_xor(best[i], 32));
+  }
+  float mine = (g & 2 ? (g & 1 ? best[3] : best[2]) : (g & 1 ? best[1] : best[0])) * scale;
+  if (E4M3) mine = times_exp(mine, s.e);
+  return s.there ? mine : -INFINITY;
+}
+
+template <bool E4M3, bool WIDE, int G>
+__global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_paged_score(PagedScoreArgs a) {
+  __shared__ float hold[4][64 * kScoreHold];  // finished scores, stored some steps later
+  __shared__ RangeLds range;
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Lens lens = {a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
+  Range rg;
+  if (a.direct) {  // one step of one unit a workgroup
+    const int unit = blockIdx.x / a.chunks;
+    rg.step = blockIdx.x - unit * a.chunks;
+    rg.b = unit / a.pg.Hkv;
+    rg.h = unit - rg.b * a.pg.Hkv;
+    rg.steps = steps_of<kScoreStep>(lens, rg.b);
+    rg.s0 = 0;
+    rg.s1 = rg.step < rg.steps;
+  } else {
+    rg = find_range<kScoreStep>(lens, a.nwg, range);
+  }
+  for (int64_t at = rg.s0; at < rg.s1;) {
+    const int take = (int)min((int64_t)(rg.steps - rg.step), rg.s1 - at);
+    Ctx x;
+    x.b = rg.b;
+    x.h = rg.h;
+    x.n = lens(rg.b);
+    x.table = table_of(a.pg, rg.b);
+    float* scores = a.scores + ((int64_t)rg.b * a.pg.Hkv + rg.h) * a.max_ctx;
+    const int stop = min((rg.step + take) * kScoreStep, x.n);
+    int p = rg.step * kScoreStep + 64 * wave;
+    if (p < stop) {
+      ScoreStep<E4M3> s;
+      ScorePages<WIDE> pages = score_pages<WIDE>(a.pg, x, p);
+      load_score_step<E4M3, WIDE>(a.pg, x, p, pages, s);
+      pages = score_pages<WIDE>(a.pg, x, min(p + kScoreStep, stop - 1) & ~15);
+      bf16x8 q[4];
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        q[f] = as_bf16x8(ld16(a.q + ((int64_t)x.b * a.Hq + x.h * G + (r & (G - 1))) * kD +
+                              frag_base<E4M3>(f, g)));
+      while (p < stop) {
+        const int held = p;
+        float* mine = hold[wave] + lane;
+        for (int i = 0; i < kScoreHold && p < stop; ++i, p += kScoreStep) {
+          const float best = step_scores<E4M3, WIDE, G>(s, q, a.scale);
+          load_score_step<E4M3, WIDE>(a.pg, x, min(p + kScoreStep, stop - 1) & ~15, pages, s);
+          pages = score_pages<WIDE>(a.pg, x, min(p + 2 * kScoreStep, stop - 1) & ~15);
+          mine[64 * i] = best;
+        }
+        for (int i = 0, w = held; w < p; ++i, w += kScoreStep)
+          if (w + lane < stop) scores[w + lane] = mine[64 * i];
+      }
+    }
+    at += take;
+    next_unit<kScoreStep>(lens, at, rg);
+  }
+  if (a.direct) {  // the same step's
+    static_assert(kScoreStep == kPagedScoreThreads, "a position a thread");
+    const int unit = blockIdx.x / a.chunks;
+    const int p = (blockIdx.x - unit * a.chunks) * kScoreStep + threadIdx.x;
+    if (p >= lens(unit / a.pg.Hkv) && p < a.max_ctx) a.scores[(int64_t)unit * a.max_ctx + p] = -INFINITY;
+    return;
+  }
+  // positions past the contexts' ends, in pieces shared out over the grid
+  const int64_t pieces = (int64_t)a.units * a.chunks;
+  for (int64_t i = blockIdx.x; i < pieces; i += gridDim.x) {
+    const int unit = (int)(i / a.chunks), c = (int)(i - (int64_t)unit * a.chunks);
+    const int from = max(lens(unit / a.pg.Hkv), c * a.piece);
+    const int to = (int)min((int64_t)(c + 1) * a.piece, (int64_t)a.max_ctx);
+    for (int p = from + threadIdx.x; p < to; p += kPagedScoreThreads)
+      a.scores[(int64_t)unit * a.max_ctx + p] = -INFINITY;
+  }
+}
+
+// ---- attention -----------------------------------------------------------------------
+constexpr int kPagedAttnThreads = 256;
+
+struct PagedAttnLds {
+  float m[4][16], l[4][16];
+  float o[4][16][kPartStride];
+  RangeLds range;
+};
 
 // One wave's state over the positions it has seen of a unit: lane (g, r) has
 // query row r's running maximum m (of logits times log2 e, the same in every
@@ -685,9 +853,8 @@ struct WaveState {
 //            row, and picks its operands out of them by byte permutes
 // K of the next step is asked for once this step's logits have taken theirs,
 // V once the products have taken its rows: a wave always has one of them in
-// flight, and none needs a second set of registers.  V rows are streamed past
-// the caches (every load takes whole rows; 4.4 GB of a bf16 batch 745 -> 667
-// us); K lines are read by two loads, half each, and stay.
+// flight, and none needs a second set of registers.  Both are streamed past the
+// caches by loads of whole lines (4.4 GB of a bf16 batch 745 -> 667 us).
 template <bool E4M3>
 struct Tile {
   KRaw<E4M3> k[2];
@@ -733,8 +900,7 @@ __device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (WIDE) {
-      const uint32_t off = min(r * pg.row_bytes, at.cap[i]);
-      t.k[i].load(pg.k + half_base(pg, x, at, i) + off, g);
+      t.k[i].load_lines(pg.k + half_base(pg, x, at, i), pg.row_bytes, at.cap[i], g, r);
     } else {
       const int pos = min(at.first[i] + r, x.n - 1), page = x.table[pos >> pg.shift];
       const bool has = (unsigned)page < (unsigned)pg.num_pages;
@@ -794,10 +960,11 @@ __device__ __forceinline__ float scaled(float x, uint32_t w, int j) {
 
 // Logits of a step for query row r: lg[j] at position p0 + 16 (j / 4) + 4g +
 // j % 4, before the scale.
-template <bool E4M3>
-__device__ __forceinline__ void tile_logits(const Tile<E4M3>& t, const bf16x8* q, float* lg) {
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void tile_logits(Tile<E4M3>& t, const bf16x8* q, float* lg) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
+    if (WIDE) t.k[i].swap_halves(threadIdx.x & 15);
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int f = 0; f < 4; ++f) s = mfma_16x16x32(t.k[i].frag(f), q[f], s);
@@ -922,7 +1089,7 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
   load_v<E4M3, WIDE>(pg, x, at, t);
   if (p + kPagedStep < end) at = tile_at<WIDE>(pg, x, p + kPagedStep);
   for (; p + kPagedStep < end; p += kPagedStep) {
-    tile_logits<E4M3>(t, q, lg);
+    tile_logits<E4M3, WIDE>(t, q, lg);
     load_k<E4M3, WIDE>(pg, x, at, t);
     __builtin_amdgcn_sched_barrier(0);
     const bool masked = WIDE ? t.there != 255u : __any(t.there != 255u);
@@ -931,7 +1098,7 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
     load_v<E4M3, WIDE>(pg, x, at, t);
     at = tile_at<WIDE>(pg, x, min(p + 2 * kPagedStep, end - 1));
   }
-  tile_logits<E4M3>(t, q, lg);
+  tile_logits<E4M3, WIDE>(t, q, lg);
   tile_rest<E4M3>(t, true, p, limit, c, lg, st);
 }
 
@@ -949,9 +1116,10 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
   // e4m3 exponents are taken less 128: one power of two more in the logits'
   // factor and, at the end, in the sums of V
   const float ce = a.scale * (E4M3 ? 2.f : 1.f) * 1.4426950408889634f;
+  const Lens lens = {a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
   // requests without any position: their outputs, shared out over the grid
   for (int u = w; u < a.B; u += a.nwg) {
-    if (steps_of(a, u) != 0) continue;
+    if (lens(u) != 0) continue;
     for (int64_t i = tid; i < (int64_t)a.T * a.Hq * (kD / 4); i += kPagedAttnThreads)
       reinterpret_cast<float4*>(a.out)[(int64_t)u * a.T * a.Hq * (kD / 4) + i] =
           make_float4(0.f, 0.f, 0.f, 0.f);
@@ -959,20 +1127,16 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
       for (int i = tid; i < a.T * a.Hq; i += kPagedAttnThreads)
         a.lse[(int64_t)u * a.T * a.Hq + i] = -INFINITY;
   }
-  int64_t s0, s1;
-  const int64_t total = find_range(a, lds, &s0, &s1);
-  PagedTail tail = {0, total, -1, 0};
-  int64_t at = s0;
-  int b = __builtin_amdgcn_readfirstlane(lds.b);
-  int steps = at < s1 ? steps_of(a, b) : 1;
-  int h = at < s1 ? __builtin_amdgcn_readfirstlane((int)(lds.off / steps)) : 0;
-  int step = at < s1 ? __builtin_amdgcn_readfirstlane((int)(lds.off % steps)) : 0;
-  while (at < s1) {
-    const int take = (int)min((int64_t)(steps - step), s1 - at);
+  Range rg = find_range<kPagedStep>(lens, a.nwg, lds.range);
+  PagedTail tail = {0, rg.total, -1, 0};
+  int64_t at = rg.s0;
+  while (at < rg.s1) {
+    const int b = rg.b, h = rg.h, step = rg.step, steps = rg.steps;
+    const int take = (int)min((int64_t)(steps - step), rg.s1 - at);
     Ctx x;
     x.b = b;
     x.h = h;
-    x.n = clamp_len(a.ctx_lens[b], a.max_ctx);
+    x.n = lens(b);
     x.table = table_of(a.pg, b);
     const int64_t qrow = out_row(a, b, h, r);
     const int limit = r < rows ? x.n - (a.T - 1 - (r >> a.lg)) : 0;
@@ -1004,7 +1168,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
     }
     __syncthreads();
     const bool whole = step == 0 && take == steps;
-    const int slot = at == s0 ? 0 : 1;
+    const int slot = at == rg.s0 ? 0 : 1;
     for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
       const int row = i >> 5, d = 4 * (i & 31);
       float M = -INFINITY;
@@ -1046,14 +1210,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
       tail.slot = slot;
     }
     at += take;
-    step = 0;
-    if (++h == a.pg.Hkv && at < s1) {
-      h = 0;
-      do {
-        ++b;
-        steps = steps_of(a, b);
-      } while (steps == 0);
-    }
+    next_unit<kPagedStep>(lens, at, rg);
   }
   if (tid == 0) a.tail[w] = tail;
 }
@@ -1207,7 +1364,7 @@ hipError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, hipStream_t s) {
 
 template <bool E4M3, bool WIDE>
 static void launch_score_g(const PagedScoreArgs& a, int G, hipStream_t s) {
-  const dim3 grid((unsigned)(a.units * a.chunks)), block(kPagedScoreThreads);
+  const dim3 grid(a.nwg), block(kPagedScoreThreads);
   switch (G) {
     case 1: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 1>, grid, block, s, a); break;
     case 2: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 2>, grid, block, s, a); break;

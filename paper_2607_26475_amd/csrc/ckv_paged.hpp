@@ -68,7 +68,10 @@ struct PagedScoreArgs {
   const int32_t* ctx_lens;
   float* scores;
   float scale;
-  int32_t Hq, max_ctx, chunks, units;
+  int32_t B, Hq, max_ctx, units;
+  int32_t nwg;
+  int32_t direct;          // workgroup (unit, step); else ranges
+  int32_t piece, chunks;   // positions of a piece of a unit (direct: a step), pieces of a unit
 };
 
 // A unit that begins in a workgroup's range and goes on in the next ones:
@@ -85,7 +88,6 @@ constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
 constexpr int kMaxPagedWgs = 1024;
 constexpr int kPagedWgsPerCu = 2;
 constexpr int kReadSlots = 32;              // slots of a reading workgroup
-constexpr int kPagedScoreRows = 512;        // positions of a scoring workgroup
 
 struct PagedAttnArgs {
   PagedPages pg;
@@ -130,6 +132,14 @@ inline int paged_wgs_cap(const Dims& d) {
   const int64_t steps = (int64_t)d.U * ((d.max_ctx + kPagedStep - 1) / kPagedStep);
   return (int)std::max<int64_t>(1, std::min<int64_t>(steps, kMaxPagedWgs));
 }
+
+// Scoring: steps of kScoreStep positions.  While every step can have a
+// workgroup of its own at once they are not cut into ranges (finding a range
+// takes a scan over the batch).
+constexpr int kScoreStep = 256;
+// Workgroups that a CU holds at once (single-row lookups take more registers).
+constexpr int score_wgs_per_cu(bool wide) { return wide ? 4 : 3; }
+constexpr int kScorePiece = 4096;   // positions past the ends that a workgroup fills in turn
 
 inline size_t paged_tail_bytes(const Dims& d) {
   return align256((size_t)paged_wgs_cap(d) * sizeof(PagedTail));
