@@ -88,16 +88,6 @@ using namespace ckv;
 // ckv_set_one_launch_same_step
 std::atomic<int> g_one_launch{CKV_ONE_LAUNCH_ROW_HALVES};
 
-// A tag for one launch of the one-launch same-step kernel: a 32-bit value
-// that is never zero in the high half and its complement in the low half.
-uint64_t next_fused_tag() {
-  static std::atomic<uint32_t> counter{0};
-  uint32_t t = counter.fetch_add(1u, std::memory_order_relaxed) + 1u;
-  t *= 2654435761u;  // spread consecutive calls over the 32 bits
-  t |= 1u;
-  return ((uint64_t)t << 32) | (uint32_t)~t;
-}
-
 int check_rank(int32_t rank) {
   if (rank < 1 || rank > CKV_MAX_RANK)
     return fail(CKV_ESHAPE, "rank %d outside [1, %d]", rank, CKV_MAX_RANK);

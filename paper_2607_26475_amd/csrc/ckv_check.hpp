@@ -3,6 +3,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
+
 #include "ckv.h"
 #include "ckv_launch.hpp"
 
@@ -72,6 +74,16 @@ inline int check_scale(float scale) {
     if (!(p)) return fail(CKV_EINVAL, "%s is NULL", #p);                    \
     if (!aligned16(p)) return fail(CKV_EINVAL, "%s is not 16-byte aligned", #p); \
   } while (0)
+
+// A tag for one launch whose workgroups hand over to each other: a 32-bit value
+// that is never zero in the high half and its complement in the low half.
+inline uint64_t next_fused_tag() {
+  static std::atomic<uint32_t> counter{0};
+  uint32_t t = counter.fetch_add(1u, std::memory_order_relaxed) + 1u;
+  t *= 2654435761u;  // spread consecutive calls over the 32 bits
+  t |= 1u;
+  return ((uint64_t)t << 32) | (uint32_t)~t;
+}
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 

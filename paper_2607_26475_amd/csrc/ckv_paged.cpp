@@ -386,14 +386,23 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.out = out;
   a.lse = lse;
   a.tail = static_cast<PagedTail*>(ws);
-  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + paged_tail_bytes(d));
+  a.flags = reinterpret_cast<uint64_t*>(static_cast<char*>(ws) + paged_tail_bytes(d));
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + paged_tail_bytes(d) +
+                                    paged_flag_bytes(d));
   a.scale = scale;
   a.B = d.B;
   a.Hq = d.Hq;
   a.T = num_tokens;
   a.lg = __builtin_ctz((unsigned)d.G);
   a.max_ctx = d.max_ctx;
-  a.nwg = std::min(paged_wgs_cap(d), kPagedWgsPerCu * device_cus());
+  // every step a workgroup of its own, all at once, and the unit's last one
+  // joins them: one launch, without a scan over the batch
+  const int64_t steps = (d.max_ctx + kPagedStep - 1) / kPagedStep;
+  const int slots = std::min(paged_wgs_cap(d), kPagedWgsPerCu * device_cus());
+  const bool direct = steps <= kMaxDirect && d.U * steps <= slots;
+  a.nwg = direct ? (int)(d.U * steps) : slots;
+  a.chunks = direct ? (int)steps : 0;
+  a.tag = next_fused_tag();
   CKV_TRY_HIP(launch_paged_attn(a, cache->kind == CKV_CACHE_E4M3, s), "paged attention launch");
   return CKV_OK;
 }

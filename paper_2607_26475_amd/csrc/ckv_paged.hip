@@ -827,6 +827,7 @@ constexpr int kPagedAttnThreads = 256;
 struct PagedAttnLds {
   float m[4][16], l[4][16];
   float o[4][16][kPartStride];
+  float jm[16], jl[16];      // direct: the joining workgroup's own partial (and o[0])
   RangeLds range;
 };
 
@@ -1107,100 +1108,131 @@ __device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h,
   return ((int64_t)b * a.T + t) * a.Hq + (h << a.lg) + g;
 }
 
+// A query row's result from its sums.
+__device__ __forceinline__ float inverse_sum(float L) {
+  return L > 0.f ? 1.f / L : L;  // nothing seen: 0; NaN stays
+}
+
+__device__ __forceinline__ float log_sum(float M, float L) {
+  return L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+}
+
+// One piece: positions [step, step + take) * kPagedStep of unit (b, h), the four
+// waves' states left in lds.
+template <bool E4M3, bool WIDE>
+__device__ __forceinline__ void attn_piece(const PagedAttnArgs& a, int b, int h, int n, int step,
+                                           int take, PagedAttnLds& lds) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int rows = a.T << a.lg;
+  // e4m3 exponents are taken less 128: one power of two more in the logits'
+  // factor and, at the end, in the sums of V
+  const float c = a.scale * (E4M3 ? 2.f : 1.f) * 1.4426950408889634f;
+  const Ctx x = {b, h, n, table_of(a.pg, b)};
+  const int64_t qrow = out_row(a, b, h, r);
+  const int limit = r < rows ? n - (a.T - 1 - (r >> a.lg)) : 0;
+  bf16x8 q[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+    q[f] = as_bf16x8(r < rows ? ld16(a.q + qrow * kD + frag_base<E4M3>(f, g))
+                              : make_uint4(0u, 0u, 0u, 0u));
+  WaveState st;
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  attn_steps<E4M3, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
+                         min((step + take) * kPagedStep, n), limit, c, q, st);
+  st.l += __shfl_xor(st.l, 16);
+  st.l += __shfl_xor(st.l, 32);
+  if (g == 0) {
+    lds.m[wave][r] = st.m;
+    lds.l[wave][r] = st.l;
+  }
+  if (r < rows) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float* o = &lds.o[wave][r][8 * (4 * g + j)];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] = E4M3 ? 2.f * st.o[e][j] : st.o[e][j];
+    }
+  }
+  __syncthreads();
+}
+
+// The four waves' sums for query row `row`, channels [d, d + 4).
+struct Partial {
+  float M, L;
+  float4 o;
+};
+
+__device__ __forceinline__ Partial join_waves(const PagedAttnLds& lds, int row, int d) {
+  Partial p;
+  p.M = -INFINITY;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) p.M = fmaxf(p.M, lds.m[k][row]);
+  p.L = 0.f;
+  p.o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float m = lds.m[k][row];
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - p.M);
+    const float4 o = *reinterpret_cast<const float4*>(&lds.o[k][row][d]);
+    p.L = fmaf(f, lds.l[k][row], p.L);
+    p.o.x = fmaf(f, o.x, p.o.x);
+    p.o.y = fmaf(f, o.y, p.o.y);
+    p.o.z = fmaf(f, o.z, p.o.z);
+    p.o.w = fmaf(f, o.w, p.o.w);
+  }
+  return p;
+}
+
+__device__ __forceinline__ void store_result(const PagedAttnArgs& a, int b, int h, int row, int d,
+                                             const Partial& p) {
+  const int64_t at = out_row(a, b, h, row);
+  const float inv = inverse_sum(p.L);
+  *reinterpret_cast<float4*>(a.out + at * kD + d) =
+      make_float4(p.o.x * inv, p.o.y * inv, p.o.z * inv, p.o.w * inv);
+  if (a.lse && d == 0) a.lse[at] = log_sum(p.M, p.L);
+}
+
+// A request without any position.
+__device__ __forceinline__ void store_empty(const PagedAttnArgs& a, int64_t first_row,
+                                            int64_t rows) {
+  for (int64_t i = threadIdx.x; i < rows * (kD / 4); i += kPagedAttnThreads)
+    reinterpret_cast<float4*>(a.out)[first_row * (kD / 4) + i] = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (a.lse)
+    for (int64_t i = threadIdx.x; i < rows; i += kPagedAttnThreads)
+      a.lse[first_row + i] = -INFINITY;
+}
+
 template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
-  const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int rows = a.T << a.lg, w = blockIdx.x;
-  // e4m3 exponents are taken less 128: one power of two more in the logits'
-  // factor and, at the end, in the sums of V
-  const float ce = a.scale * (E4M3 ? 2.f : 1.f) * 1.4426950408889634f;
+  const int tid = threadIdx.x, w = blockIdx.x, rows = a.T << a.lg;
   const Lens lens = {a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
-  // requests without any position: their outputs, shared out over the grid
-  for (int u = w; u < a.B; u += a.nwg) {
-    if (lens(u) != 0) continue;
-    for (int64_t i = tid; i < (int64_t)a.T * a.Hq * (kD / 4); i += kPagedAttnThreads)
-      reinterpret_cast<float4*>(a.out)[(int64_t)u * a.T * a.Hq * (kD / 4) + i] =
-          make_float4(0.f, 0.f, 0.f, 0.f);
-    if (a.lse)
-      for (int i = tid; i < a.T * a.Hq; i += kPagedAttnThreads)
-        a.lse[(int64_t)u * a.T * a.Hq + i] = -INFINITY;
-  }
+  for (int u = w; u < a.B; u += a.nwg)
+    if (lens(u) == 0) store_empty(a, (int64_t)u * a.T * a.Hq, (int64_t)a.T * a.Hq);
   Range rg = find_range<kPagedStep>(lens, a.nwg, lds.range);
   PagedTail tail = {0, rg.total, -1, 0};
   int64_t at = rg.s0;
   while (at < rg.s1) {
     const int b = rg.b, h = rg.h, step = rg.step, steps = rg.steps;
     const int take = (int)min((int64_t)(steps - step), rg.s1 - at);
-    Ctx x;
-    x.b = b;
-    x.h = h;
-    x.n = lens(b);
-    x.table = table_of(a.pg, b);
-    const int64_t qrow = out_row(a, b, h, r);
-    const int limit = r < rows ? x.n - (a.T - 1 - (r >> a.lg)) : 0;
-    bf16x8 q[4];
-#pragma unroll
-    for (int f = 0; f < 4; ++f)
-      q[f] = as_bf16x8(r < rows ? ld16(a.q + qrow * kD + frag_base<E4M3>(f, g))
-                                : make_uint4(0u, 0u, 0u, 0u));
-    WaveState st;
-    st.m = -INFINITY;
-    st.l = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    attn_steps<E4M3, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
-                           min((step + take) * kPagedStep, x.n), limit, ce, q, st);
-    st.l += __shfl_xor(st.l, 16);
-    st.l += __shfl_xor(st.l, 32);
-    if (g == 0) {
-      lds.m[wave][r] = st.m;
-      lds.l[wave][r] = st.l;
-    }
-    if (r < rows) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        float* o = &lds.o[wave][r][8 * (4 * g + j)];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] = E4M3 ? 2.f * st.o[e][j] : st.o[e][j];
-      }
-    }
-    __syncthreads();
-    const bool whole = step == 0 && take == steps;
+    attn_piece<E4M3, WIDE>(a, b, h, lens(b), step, take, lds);
     const int slot = at == rg.s0 ? 0 : 1;
     for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
       const int row = i >> 5, d = 4 * (i & 31);
-      float M = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) M = fmaxf(M, lds.m[k][row]);
-      float L = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float m = lds.m[k][row];
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-        const float4 ok = *reinterpret_cast<const float4*>(&lds.o[k][row][d]);
-        L = fmaf(f, lds.l[k][row], L);
-        o.x = fmaf(f, ok.x, o.x);
-        o.y = fmaf(f, ok.y, o.y);
-        o.z = fmaf(f, ok.z, o.z);
-        o.w = fmaf(f, ok.w, o.w);
+      const Partial p = join_waves(lds, row, d);
+      if (take == steps) {
+        store_result(a, b, h, row, d, p);
+        continue;
       }
-      if (whole) {
-        const int64_t at_row = out_row(a, b, h, row);
-        const float inv = L > 0.f ? 1.f / L : L;  // NaN stays
-        *reinterpret_cast<float4*>(a.out + at_row * kD + d) =
-            make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-        if (a.lse && d == 0)
-          a.lse[at_row] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
-      } else {
-        float* p = a.part + (((int64_t)w * 2 + slot) * rows + row) * kPartStride;
-        *reinterpret_cast<float4*>(p + 4 + d) = o;
-        if (d == 0) {
-          p[0] = M;
-          p[1] = L;
-        }
+      float* part = a.part + (((int64_t)w * 2 + slot) * rows + row) * kPartStride;
+      *reinterpret_cast<float4*>(part + 4 + d) = p.o;
+      if (d == 0) {
+        part[0] = p.M;
+        part[1] = p.L;
       }
     }
     __syncthreads();
@@ -1213,6 +1245,120 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
     next_unit<kPagedStep>(lens, at, rg);
   }
   if (tid == 0) a.tail[w] = tail;
+}
+
+// The same with a workgroup for every step of every unit (workgroup unit *
+// chunks + step) and the join inside the launch, for few steps: each hands its
+// partial over through its flag, which takes the launch's tag once the partial's
+// device-coherent stores are done; the unit's last step's workgroup waits for
+// the flags, clears them and joins.  Only higher-numbered workgroups wait, for
+// lower-numbered ones that never do, and the wait is bounded (kFusedSpinLimit):
+// a broken hand-over leaves outputs undefined but ends.  8 units of 2001
+// positions: 8.1 us, against 10.4 with ranges and a second launch.
+template <bool E4M3, bool WIDE>
+__global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(PagedAttnArgs a) {
+  __shared__ PagedAttnLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, rows = a.T << a.lg;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int unit = blockIdx.x / a.chunks, step = blockIdx.x - unit * a.chunks;
+  const int b = unit / a.pg.Hkv, h = unit - b * a.pg.Hkv;
+  const int n = clamp_len(a.ctx_lens[b], a.max_ctx);
+  const int steps = (n + kPagedStep - 1) / kPagedStep;
+  if (step >= steps) {
+    if (step == 0)  // no positions: this unit's query rows
+      for (int t = 0; t < a.T; ++t)
+        store_empty(a, out_row(a, b, h, t << a.lg), (int64_t)1 << a.lg);
+    return;
+  }
+  attn_piece<E4M3, WIDE>(a, b, h, n, step, 1, lds);
+  const bool last = step == steps - 1;
+  float* part = a.part + (int64_t)blockIdx.x * 2 * rows * kPartStride;
+  for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
+    const int row = i >> 5, d = 4 * (i & 31);
+    const Partial p = join_waves(lds, row, d);
+    if (steps == 1) {
+      store_result(a, b, h, row, d, p);
+    } else if (last) {  // (row, d) of o[0] is read by this thread alone
+      *reinterpret_cast<float4*>(&lds.o[0][row][d]) = p.o;
+      if (d == 0) {
+        lds.jm[row] = p.M;
+        lds.jl[row] = p.L;
+      }
+    } else {
+      uint64_t* o = reinterpret_cast<uint64_t*>(part + row * kPartStride + 4 + d);
+      const uint64_t v[2] = {__float_as_uint(p.o.x) | (uint64_t)__float_as_uint(p.o.y) << 32,
+                             __float_as_uint(p.o.z) | (uint64_t)__float_as_uint(p.o.w) << 32};
+      __hip_atomic_store(o, v[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      __hip_atomic_store(o + 1, v[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (d == 0)
+        __hip_atomic_store(reinterpret_cast<uint64_t*>(part + row * kPartStride),
+                           __float_as_uint(p.M) | (uint64_t)__float_as_uint(p.L) << 32,
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+  }
+  if (steps == 1) return;
+  if (!last) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0)
+      __hip_atomic_store(a.flags + blockIdx.x, a.tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return;
+  }
+  const int64_t first = (int64_t)unit * a.chunks;  // the unit's first workgroup
+  if (tid < steps - 1) {
+    uint64_t* f = a.flags + first + tid;
+    for (uint32_t spin = 0;
+         __hip_atomic_load(f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.tag &&
+         spin < kFusedSpinLimit;
+         ++spin)
+      __builtin_amdgcn_s_sleep(2);
+    __hip_atomic_store(f, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __syncthreads();
+  // a wave a query row: lane i weighs step i, then lanes take two channels each
+  for (int row = wave; row < rows; row += 4) {
+    const uint64_t* p0 =
+        reinterpret_cast<const uint64_t*>(a.part + (first * 2 * rows + row) * kPartStride);
+    const int64_t next = (int64_t)rows * kPartStride;  // 2 * rows * kPartStride floats
+    float m = -INFINITY, l = 0.f;
+    if (lane < steps - 1) {
+      const uint64_t ml = __hip_atomic_load(const_cast<uint64_t*>(p0 + lane * next),
+                                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      m = __uint_as_float((uint32_t)ml);
+      l = __uint_as_float((uint32_t)(ml >> 32));
+    } else if (lane == steps - 1) {
+      m = lds.jm[row];
+      l = lds.jl[row];
+    }
+    const float M = wave_max(m);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
+    const float L = wave_sum(f * l);
+    float2 o = make_float2(0.f, 0.f);
+    constexpr int kAhead = 8;
+    for (int i0 = 0; i0 < steps - 1; i0 += kAhead) {
+      uint64_t x[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        x[k] = __hip_atomic_load(
+            const_cast<uint64_t*>(p0 + min(i0 + k, steps - 2) * next + 2 + lane),
+            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const float fk = i0 + k < steps - 1 ? __shfl(f, i0 + k) : 0.f;
+        if (fk == 0.f) continue;  // nothing there: its sums are not to be looked at
+        o.x = fmaf(fk, __uint_as_float((uint32_t)x[k]), o.x);
+        o.y = fmaf(fk, __uint_as_float((uint32_t)(x[k] >> 32)), o.y);
+      }
+    }
+    const float fk = __shfl(f, steps - 1);
+    const float2 own = *reinterpret_cast<const float2*>(&lds.o[0][row][2 * lane]);
+    o.x = fmaf(fk, own.x, o.x);
+    o.y = fmaf(fk, own.y, o.y);
+    const int64_t at = out_row(a, b, h, row);
+    const float inv = inverse_sum(L);
+    *reinterpret_cast<float2*>(a.out + at * kD + 2 * lane) = make_float2(o.x * inv, o.y * inv);
+    if (a.lse && lane == 0) a.lse[at] = log_sum(M, L);
+  }
 }
 
 // Joins the unit that workgroup blockIdx.x's range left unfinished: query row
@@ -1273,11 +1419,10 @@ __global__ __launch_bounds__(kPagedMergeThreads) void k_paged_merge(PagedAttnArg
   }
   const int b = t.unit / a.pg.Hkv, h = t.unit - b * a.pg.Hkv;
   const int64_t at = out_row(a, b, h, row);
-  const float inv = L > 0.f ? 1.f / L : L;
+  const float inv = inverse_sum(L);
   *reinterpret_cast<float4*>(a.out + at * kD + 4 * d) =
       make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  if (a.lse && d == 0)
-    a.lse[at] = L == 0.f ? -INFINITY : (M + __log2f(L)) * 0.6931471805599453f;
+  if (a.lse && d == 0) a.lse[at] = log_sum(M, L);
 }
 
 // ---- debug mode ------------------------------------------------------------------------
@@ -1384,6 +1529,17 @@ hipError_t launch_paged_score(const PagedScoreArgs& a, bool e4m3, int G, hipStre
 hipError_t launch_paged_attn(const PagedAttnArgs& a, bool e4m3, hipStream_t s) {
   const bool wide = a.pg.shift >= 4;
   const dim3 grid(a.nwg), block(kPagedAttnThreads);
+  if (a.chunks) {
+    if (e4m3 && wide)
+      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<true, true>, grid, block, s, a);
+    else if (e4m3)
+      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<true, false>, grid, block, s, a);
+    else if (wide)
+      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<false, true>, grid, block, s, a);
+    else
+      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<false, false>, grid, block, s, a);
+    return launch_status();
+  }
   if (e4m3 && wide) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<true, true>, grid, block, s, a);
   else if (e4m3) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<true, false>, grid, block, s, a);
   else if (wide) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<false, true>, grid, block, s, a);

@@ -87,6 +87,7 @@ constexpr int kPagedTile = 32;              // positions of a wave's step
 constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
 constexpr int kMaxPagedWgs = 1024;
 constexpr int kPagedWgsPerCu = 2;
+constexpr int kMaxDirect = 64;              // steps of a unit that one wave's lanes can join
 constexpr int kReadSlots = 32;              // slots of a reading workgroup
 
 struct PagedAttnArgs {
@@ -97,9 +98,12 @@ struct PagedAttnArgs {
   float* lse;              // [B][T][Hq] or NULL
   float* part;             // [nwg][2][T*G][kPartStride]
   PagedTail* tail;         // [nwg]
+  uint64_t* flags;         // [nwg], direct calls
+  uint64_t tag;
   float scale;
   int32_t B, Hq, T, lg;    // lg: log2 G
   int32_t max_ctx, nwg;
+  int32_t chunks;          // direct: workgroups (steps) of a unit; else 0
 };
 
 // Debug mode's checks of paged inputs (CheckArgs' codes go on: 4 page_table
@@ -145,8 +149,12 @@ inline size_t paged_tail_bytes(const Dims& d) {
   return align256((size_t)paged_wgs_cap(d) * sizeof(PagedTail));
 }
 
+inline size_t paged_flag_bytes(const Dims& d) {
+  return align256((size_t)paged_wgs_cap(d) * sizeof(uint64_t));
+}
+
 inline size_t paged_attn_ws_bytes(const Dims& d, int32_t tokens) {
-  return paged_tail_bytes(d) +
+  return paged_tail_bytes(d) + paged_flag_bytes(d) +
          align256((size_t)paged_wgs_cap(d) * 2 * tokens * d.G * kPartStride * sizeof(float));
 }
 

@@ -331,15 +331,19 @@ LENS = [0, 1, 2, 15, 16, 17, 31, 33, 127, 128, 129, 300, 1000]
     (16, "rows", 16, 1), (32, "pairs", 4, 4), (64, "heads", 8, 1), (128, "rows", 1, 16),
     (1024, "heads", 2, 2)])
 def test_paged_attention(kind, page, order, G, T):
+    """In one launch (a workgroup for every step), and, for the same lengths in
+    longer tables, by ranges with a join of their own."""
     _log("attention", kind, page, order, G, T)
-    pool = Pool(LENS, 2, page, kind, seed=G + T, order=order, max_ctx=1100)
-    q, out, lse = _attend(pool, G, T)
-    _check_attention(pool, q, out, lse, T)
+    for max_ctx in (1100, 9000):
+        pool = Pool(LENS, 2, page, kind, seed=G + T, order=order, max_ctx=max_ctx)
+        q, out, lse = _attend(pool, G, T)
+        _check_attention(pool, q, out, lse, T)
 
 
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 @pytest.mark.parametrize("page", [4, 16, 64])
-def test_paged_attention_with_evicted_pages(kind, page):
+@pytest.mark.parametrize("max_ctx", [700, 9000])
+def test_paged_attention_with_evicted_pages(kind, page, max_ctx):
     """Pages missing at the front, in the middle, over whole steps, everywhere,
     and the page of the newest position."""
     _log("evicted", kind, page)
@@ -347,7 +351,7 @@ def test_paged_attention_with_evicted_pages(kind, page):
     per = lambda n: -(-n // page)  # noqa: E731
     holes = [(0, s) for s in range(1, per(500))] + [(1, s) for s in range(per(300))] + \
             [(2, 0)] + [(3, per(64) - 1)]
-    pool = Pool(lens, 2, page, kind, seed=page, holes=holes)
+    pool = Pool(lens, 2, page, kind, seed=page, holes=holes, max_ctx=max_ctx)
     q, out, lse = _attend(pool, 4, 2)
     _check_attention(pool, q, out, lse, 2)
     assert torch.all(out[1] == 0)
@@ -509,11 +513,31 @@ def test_captured_step_follows_growing_contexts():
 
 
 def test_kernel_classes_are_timed():
-    pool = Pool([300], 1, 16, "bf16")
-    ckv.profile_begin(["paged_attn", "paged_merge"])
-    _attend(pool, 1, 1)
-    seen = ckv.profile_end()
-    assert seen["paged_attn"][0] == 1 and seen["paged_merge"][0] == 1
+    for lens, merges in (([300], 0), ([9000], 1)):   # one launch; ranges and their join
+        pool = Pool(lens, 1, 16, "bf16")
+        ckv.profile_begin(["paged_attn", "paged_merge"])
+        _attend(pool, 1, 1)
+        seen = ckv.profile_end()
+        assert seen["paged_attn"][0] == 1 and seen.get("paged_merge", (0,))[0] == merges
+
+
+def test_direct_join_over_and_over():
+    """The hand-over flags are clear again after every call: the same workspace,
+    calls back to back of growing and shrinking contexts, two shapes in turn."""
+    pools = [Pool([2000, 64, 700], 2, 16, "bf16", seed=1), Pool([1, 500], 4, 32, "e4m3", seed=2)]
+    first = [_attend(p, 2, 1, seed=3)[1:] for p in pools]
+    ws = ckv.workspace(pools[0].shape(2), 1, ckv.ENTRY_PAGED_DECODE_ATTN)
+    assert ws.numel() >= ckv.workspace_bytes(pools[1].shape(2), 1, ckv.ENTRY_PAGED_DECODE_ATTN)
+    for i in range(30):
+        for p, want in zip(pools, first):
+            full = p.ctx.clone()
+            if i % 3 == 1:
+                p.ctx.copy_(torch.clamp(full - 100 * i, min=0))
+            got = _attend(p, 2, 1, seed=3, ws=ws)[1:]
+            if i % 3 == 1:
+                p.ctx.copy_(full)
+            else:
+                assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
 # ---- debug mode --------------------------------------------------------------------------
