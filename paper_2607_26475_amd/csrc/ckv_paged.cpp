@@ -399,7 +399,8 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   // joins them: one launch, without a scan over the batch
   const int64_t steps = (d.max_ctx + kPagedStep - 1) / kPagedStep;
   const int slots = std::min(paged_wgs_cap(d), kPagedWgsPerCu * device_cus());
-  const bool direct = steps <= kMaxDirect && d.U * steps <= slots;
+  const bool direct = steps <= kMaxDirect && steps * num_tokens * d.G <= kMaxDirectRows &&
+                      d.U * steps <= slots;
   a.nwg = direct ? (int)(d.U * steps) : slots;
   a.chunks = direct ? (int)steps : 0;
   a.tag = next_fused_tag();

@@ -241,6 +241,9 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int per) {
   rope_copy<T, WHOLE>(a.r, a.k, t0, tokens);
 }
 
+// What a kernel only reads, for scalar loads where the index is the wave's.
+typedef const __attribute__((address_space(4))) int32_t* TablePtr;
+
 // ---- writing -----------------------------------------------------------------------
 // Row of position pos in its page, or a page of -1 where it is not there.
 __device__ __forceinline__ int page_of(const PagedPages& pg, int b, int pos) {
@@ -424,8 +427,8 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
   const bool is_v = threadIdx.x & 16;
   const int unit = blockIdx.x / a.chunks, first = (blockIdx.x - unit * a.chunks) * kReadSlots;
   const int b = unit / a.pg.Hkv, h = unit - b * a.pg.Hkv;
-  const int n = clamp_len(a.ctx_lens[b], a.max_ctx);
-  const int count = a.idx ? clamp_len(a.n_sel[unit], a.k) : min(a.k, n);
+  const int n = clamp_len(((TablePtr)(uintptr_t)a.ctx_lens)[b], a.max_ctx);
+  const int count = a.idx ? clamp_len(((TablePtr)(uintptr_t)a.n_sel)[unit], a.k) : min(a.k, n);
   const int64_t slot0 = (int64_t)unit * a.k;
   const int32_t* table = a.pg.table + (int64_t)b * a.pg.table_stride;
   const uint8_t* pages = (is_v ? a.pg.v : a.pg.k) + h * a.pg.head_bytes + (E4M3 ? 8 : 16) * c;
@@ -482,8 +485,6 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
 // the whole wave; else every lane looks its rows' pages up.  Rows at or past
 // the context's end are read as its last row (rows there may hold anything, and
 // a weight of zero times a NaN is a NaN).
-typedef const __attribute__((address_space(4))) int32_t* TablePtr;  // read-only: scalar loads
-
 __device__ __forceinline__ TablePtr table_of(const PagedPages& pg, int b) {
   return (TablePtr)(uintptr_t)(pg.table + (int64_t)b * pg.table_stride);
 }
@@ -574,7 +575,7 @@ __device__ __forceinline__ int64_t range_start(int64_t total, int w, int nwg) {
 }
 
 struct Lens {
-  const int32_t* ctx_lens;
+  TablePtr ctx_lens;
   int32_t B, Hkv, max_ctx;
   __device__ __forceinline__ int operator()(int b) const {
     return clamp_len(ctx_lens[b], max_ctx);
@@ -599,8 +600,13 @@ struct Range {
   int32_t b, h, step, steps;  // steps: of the unit
 };
 
+// Ranges of that many steps (at least `least` each while there are several).
+__device__ __forceinline__ int ranges_of(int64_t total, int max_wgs, int least) {
+  return (int)min((int64_t)max_wgs, (total + least - 1) / least);
+}
+
 template <int STEP>
-__device__ __forceinline__ Range find_range(const Lens& n, int max_wgs, RangeLds& lds) {
+__device__ __forceinline__ Range find_range(const Lens& n, int max_wgs, int least, RangeLds& lds) {
   constexpr int kThreads = 256;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int per = (n.B + kThreads - 1) / kThreads;
@@ -622,7 +628,7 @@ __device__ __forceinline__ Range find_range(const Lens& n, int max_wgs, RangeLds
     if (w < wave) incl += lds.wave_sum[w];
     r.total += lds.wave_sum[w];
   }
-  const int nwg = (int)min((int64_t)max_wgs, r.total), w = min((int)blockIdx.x, nwg);
+  const int nwg = ranges_of(r.total, max_wgs, least), w = min((int)blockIdx.x, nwg);
   r.s0 = nwg ? range_start(r.total, w, nwg) : 0;
   r.s1 = nwg ? range_start(r.total, min(w + 1, nwg), nwg) : 0;
   int64_t at = incl - mine;
@@ -754,7 +760,7 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
   __shared__ RangeLds range;
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Lens lens = {a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
+  const Lens lens = {(TablePtr)(uintptr_t)a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
   Range rg;
   if (a.direct) {  // one step of one unit a workgroup
     const int unit = blockIdx.x / a.chunks;
@@ -765,7 +771,7 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
     rg.s0 = 0;
     rg.s1 = rg.step < rg.steps;
   } else {
-    rg = find_range<kScoreStep>(lens, a.nwg, range);
+    rg = find_range<kScoreStep>(lens, a.nwg, 1, range);
   }
   for (int64_t at = rg.s0; at < rg.s1;) {
     const int take = (int)min((int64_t)(rg.steps - rg.step), rg.s1 - at);
@@ -823,6 +829,11 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
 
 // ---- attention -----------------------------------------------------------------------
 constexpr int kPagedAttnThreads = 256;
+// Least steps of a range: one step is a chain of latencies and a partial to
+// join.  Against ranges of one, us: 8 units of 16 rows and 8192 positions 24.4 ->
+// 19.6, 16384 28.7 -> 25.4; one unit of 4 rows and 65536 39.3 -> 22.7 (of 16384
+// 16.3 -> 16.5).
+constexpr int kLeastSteps = 4;
 
 struct PagedAttnLds {
   float m[4][16], l[4][16];
@@ -1210,10 +1221,10 @@ template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, w = blockIdx.x, rows = a.T << a.lg;
-  const Lens lens = {a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
+  const Lens lens = {(TablePtr)(uintptr_t)a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
   for (int u = w; u < a.B; u += a.nwg)
     if (lens(u) == 0) store_empty(a, (int64_t)u * a.T * a.Hq, (int64_t)a.T * a.Hq);
-  Range rg = find_range<kPagedStep>(lens, a.nwg, lds.range);
+  Range rg = find_range<kPagedStep>(lens, a.nwg, kLeastSteps, lds.range);
   PagedTail tail = {0, rg.total, -1, 0};
   int64_t at = rg.s0;
   while (at < rg.s1) {
@@ -1247,6 +1258,74 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
   if (tid == 0) a.tail[w] = tail;
 }
 
+// Joins a unit's steps: partials 0 .. steps - 2 handed over in memory, before
+// `part` (where the last step's would be), the last one's in lds.  Wave w takes
+// query rows w, w + 4, ... (at most ROWS of them; those past the last are the last
+// again), all of whose loads are asked for together: lane i weighs step i, then
+// lanes take two channels each.
+template <int ROWS>
+__device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h, int steps,
+                                           const float* part, const PagedAttnLds& lds) {
+  const int lane = threadIdx.x & 63, rows = a.T << a.lg;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave >= rows) return;
+  const int64_t next = (int64_t)rows * kPartStride;  // in pairs of floats: 2 * rows partial rows
+  uint64_t* base = reinterpret_cast<uint64_t*>(const_cast<float*>(part)) - (steps - 1) * next;
+  uint64_t* p0[ROWS];
+  int row[ROWS];
+  float f[ROWS], M[ROWS], L[ROWS];
+  float2 o[ROWS];
+  uint64_t ml[ROWS];
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    row[k] = min(wave + 4 * k, rows - 1);
+    p0[k] = base + row[k] * (kPartStride / 2);
+    ml[k] = __hip_atomic_load(p0[k] + min(lane, steps - 2) * next, __ATOMIC_RELAXED,
+                              __HIP_MEMORY_SCOPE_AGENT);
+  }
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    const bool own = lane == steps - 1, past = lane >= steps;
+    const float m = own ? lds.jm[row[k]] : past ? -INFINITY : __uint_as_float((uint32_t)ml[k]);
+    const float l = own ? lds.jl[row[k]] : __uint_as_float((uint32_t)(ml[k] >> 32));
+    M[k] = wave_max(m);
+    f[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M[k]);
+    L[k] = wave_sum(f[k] == 0.f ? 0.f : f[k] * l);
+    o[k] = make_float2(0.f, 0.f);
+  }
+  constexpr int kAhead = ROWS == 1 ? 8 : 4;
+  for (int i0 = 0; i0 < steps - 1; i0 += kAhead) {
+    uint64_t x[kAhead][ROWS];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k)
+        x[i][k] = __hip_atomic_load(p0[k] + min(i0 + i, steps - 2) * next + 2 + lane,
+                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) {
+        const float fk = i0 + i < steps - 1 ? __shfl(f[k], i0 + i) : 0.f;
+        o[k].x = fmaf(fk, __uint_as_float((uint32_t)x[i][k]), o[k].x);
+        o[k].y = fmaf(fk, __uint_as_float((uint32_t)(x[i][k] >> 32)), o[k].y);
+      }
+  }
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    if (wave + 4 * k >= rows) break;
+    const float fk = __shfl(f[k], steps - 1);
+    const float2 own = *reinterpret_cast<const float2*>(&lds.o[0][row[k]][2 * lane]);
+    o[k].x = fmaf(fk, own.x, o[k].x);
+    o[k].y = fmaf(fk, own.y, o[k].y);
+    const int64_t at = out_row(a, b, h, row[k]);
+    const float inv = inverse_sum(L[k]);
+    *reinterpret_cast<float2*>(a.out + at * kD + 2 * lane) =
+        make_float2(o[k].x * inv, o[k].y * inv);
+    if (a.lse && lane == 0) a.lse[at] = log_sum(M[k], L[k]);
+  }
+}
+
 // The same with a workgroup for every step of every unit (workgroup unit *
 // chunks + step) and the join inside the launch, for few steps: each hands its
 // partial over through its flag, which takes the launch's tag once the partial's
@@ -1258,11 +1337,10 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
 template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
-  const int tid = threadIdx.x, lane = tid & 63, rows = a.T << a.lg;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tid = threadIdx.x, rows = a.T << a.lg;
   const int unit = blockIdx.x / a.chunks, step = blockIdx.x - unit * a.chunks;
   const int b = unit / a.pg.Hkv, h = unit - b * a.pg.Hkv;
-  const int n = clamp_len(a.ctx_lens[b], a.max_ctx);
+  const int n = clamp_len(((TablePtr)(uintptr_t)a.ctx_lens)[b], a.max_ctx);
   const int steps = (n + kPagedStep - 1) / kPagedStep;
   if (step >= steps) {
     if (step == 0)  // no positions: this unit's query rows
@@ -1315,50 +1393,9 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
     __hip_atomic_store(f, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
   __syncthreads();
-  // a wave a query row: lane i weighs step i, then lanes take two channels each
-  for (int row = wave; row < rows; row += 4) {
-    const uint64_t* p0 =
-        reinterpret_cast<const uint64_t*>(a.part + (first * 2 * rows + row) * kPartStride);
-    const int64_t next = (int64_t)rows * kPartStride;  // 2 * rows * kPartStride floats
-    float m = -INFINITY, l = 0.f;
-    if (lane < steps - 1) {
-      const uint64_t ml = __hip_atomic_load(const_cast<uint64_t*>(p0 + lane * next),
-                                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-      m = __uint_as_float((uint32_t)ml);
-      l = __uint_as_float((uint32_t)(ml >> 32));
-    } else if (lane == steps - 1) {
-      m = lds.jm[row];
-      l = lds.jl[row];
-    }
-    const float M = wave_max(m);
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M);
-    const float L = wave_sum(f * l);
-    float2 o = make_float2(0.f, 0.f);
-    constexpr int kAhead = 8;
-    for (int i0 = 0; i0 < steps - 1; i0 += kAhead) {
-      uint64_t x[kAhead];
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k)
-        x[k] = __hip_atomic_load(
-            const_cast<uint64_t*>(p0 + min(i0 + k, steps - 2) * next + 2 + lane),
-            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const float fk = i0 + k < steps - 1 ? __shfl(f, i0 + k) : 0.f;
-        if (fk == 0.f) continue;  // nothing there: its sums are not to be looked at
-        o.x = fmaf(fk, __uint_as_float((uint32_t)x[k]), o.x);
-        o.y = fmaf(fk, __uint_as_float((uint32_t)(x[k] >> 32)), o.y);
-      }
-    }
-    const float fk = __shfl(f, steps - 1);
-    const float2 own = *reinterpret_cast<const float2*>(&lds.o[0][row][2 * lane]);
-    o.x = fmaf(fk, own.x, o.x);
-    o.y = fmaf(fk, own.y, o.y);
-    const int64_t at = out_row(a, b, h, row);
-    const float inv = inverse_sum(L);
-    *reinterpret_cast<float2*>(a.out + at * kD + 2 * lane) = make_float2(o.x * inv, o.y * inv);
-    if (a.lse && lane == 0) a.lse[at] = log_sum(M, L);
-  }
+  if (rows <= 4) join_steps<1>(a, b, h, steps, part, lds);
+  else if (rows <= 8) join_steps<2>(a, b, h, steps, part, lds);
+  else join_steps<4>(a, b, h, steps, part, lds);
 }
 
 // Joins the unit that workgroup blockIdx.x's range left unfinished: query row
@@ -1374,7 +1411,7 @@ __global__ __launch_bounds__(kPagedMergeThreads) void k_paged_merge(PagedAttnArg
   const PagedTail t = a.tail[w];
   if (t.unit < 0) return;
   // the last range that begins before the unit's end: total * i / nwg < end
-  const int64_t nwg = min((int64_t)a.nwg, t.total);
+  const int64_t nwg = ranges_of(t.total, a.nwg, kLeastSteps);
   const int n = (int)((t.end * nwg - 1) / t.total) - w + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto partial = [&](int i) {
     return a.part + (((int64_t)(w + i) * 2 + (i == 0 ? t.slot : 0)) * rows + row) * kPartStride;
@@ -1402,13 +1439,22 @@ __global__ __launch_bounds__(kPagedMergeThreads) void k_paged_merge(PagedAttnArg
   for (int i = 0; i < kPagedMergeThreads / 64; ++i) L += red[i];
   const int d = tid & 31, part = tid >> 5;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = part; i < n; i += kPagedMergeThreads / 32) {
-    const float4 x = *reinterpret_cast<const float4*>(partial(i) + 4 + 4 * d);
-    const float f = weight[i];
-    o.x = fmaf(f, x.x, o.x);
-    o.y = fmaf(f, x.y, o.y);
-    o.z = fmaf(f, x.z, o.z);
-    o.w = fmaf(f, x.w, o.w);
+  constexpr int kGroups = kPagedMergeThreads / 32, kAhead = 8;
+  for (int i0 = part; i0 < n; i0 += kAhead * kGroups) {
+    f32x4 x[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      x[k] = *reinterpret_cast<const f32x4*>(partial(min(i0 + k * kGroups, n - 1)) + 4 + 4 * d);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int i = i0 + k * kGroups;
+      if (i >= n) break;
+      const float f = weight[i];
+      o.x = fmaf(f, x[k][0], o.x);
+      o.y = fmaf(f, x[k][1], o.y);
+      o.z = fmaf(f, x[k][2], o.z);
+      o.w = fmaf(f, x[k][3], o.w);
+    }
   }
   sums[part][d] = o;
   __syncthreads();

@@ -87,7 +87,12 @@ constexpr int kPagedTile = 32;              // positions of a wave's step
 constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
 constexpr int kMaxPagedWgs = 1024;
 constexpr int kPagedWgsPerCu = 2;
-constexpr int kMaxDirect = 64;              // steps of a unit that one wave's lanes can join
+// The attention in one launch: at most so many steps a unit (one wave's lanes
+// weigh them) and partial rows (its 4 waves load them).  8 units, one launch
+// against ranges and a join, us: 4 rows a unit, 256 positions 7.5 / 10.4, 4096
+// 9.6 / 12.5, 8192 14.4 / 17.4; 16 rows, 256 positions 9.9 / 10.9, 2048 12.5 /
+// 13.5, 8192 27.5 / 24.1; 1 unit of 16 rows, 2048 11.6 / 11.3, 4096 13.5 / 12.3.
+constexpr int kMaxDirect = 64, kMaxDirectRows = 256;
 constexpr int kReadSlots = 32;              // slots of a reading workgroup
 
 struct PagedAttnArgs {
