@@ -875,92 +875,114 @@ struct Tile {
   uint32_t there;                   // bit j: position j of the lane's rows has a page
 };
 
-// Where a step's two halves lie: with WIDE pages the same for every lane.  Rows
-// past the context's end are read as its last row, so a row's offset from the
-// half's first is the smaller of its own and the last one's (cap).
+// Where a step's two halves lie, looked up a step ahead (a lookup between row
+// loads would wait for those before it).  Rows past the context's end are read as
+// its last row.  With WIDE pages a half's page is the same for every lane, and a
+// row's offset from the half's first is the smaller of its own and the last
+// row's (cap); else every row has its page.  Pages that are not there are -1.
+template <bool WIDE>
 struct TileAt {
   int first[2];
-  int page[2];      // WIDE: -1 where the half's page is not there
+  int page[2];      // WIDE: of the halves; else of the lane's K rows
+  int v_page[WIDE ? 1 : 8];
   int32_t cap[2];   // WIDE: bytes
 };
 
+__device__ __forceinline__ int page_at(const PagedPages& pg, const Ctx& x, int pos) {
+  const int page = x.table[pos >> pg.shift];
+  return (unsigned)page < (unsigned)pg.num_pages ? page : -1;
+}
+
 template <bool WIDE>
-__device__ __forceinline__ TileAt tile_at(const PagedPages& pg, const Ctx& x, int p0) {
-  TileAt t;
+__device__ __forceinline__ TileAt<WIDE> tile_at(const PagedPages& pg, const Ctx& x, int p0) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  TileAt<WIDE> t;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     t.first[i] = min(p0 + 16 * i, (x.n - 1) & ~15);
     if (WIDE) {
-      const int page = x.table[t.first[i] >> pg.shift];
-      t.page[i] = (unsigned)page < (unsigned)pg.num_pages ? page : -1;
+      t.page[i] = page_at(pg, x, t.first[i]);
       t.cap[i] = min(x.n - 1 - t.first[i], 15) * pg.row_bytes;
+    } else {
+      t.page[i] = page_at(pg, x, min(t.first[i] + r, x.n - 1));
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        t.v_page[WIDE ? 0 : 4 * i + j] =
+            page_at(pg, x, min(t.first[i] + 4 * g + j, x.n - 1));
     }
   }
   return t;
 }
 
 // First byte of a half's first row, for the whole wave.
-__device__ __forceinline__ int64_t half_base(const PagedPages& pg, const Ctx& x, const TileAt& at,
-                                             int i) {
+__device__ __forceinline__ int64_t half_base(const PagedPages& pg, const Ctx& x,
+                                             const TileAt<true>& at, int i) {
   return row_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
 }
 
 template <bool E4M3, bool WIDE>
-__device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TileAt& at,
+__device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TileAt<WIDE>& at,
                                        Tile<E4M3>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if (WIDE) {
+    if constexpr (WIDE)
       t.k[i].load_lines(pg.k + half_base(pg, x, at, i), pg.row_bytes, at.cap[i], g, r);
-    } else {
-      const int pos = min(at.first[i] + r, x.n - 1), page = x.table[pos >> pg.shift];
-      const bool has = (unsigned)page < (unsigned)pg.num_pages;
-      t.k[i].load(pg.k + row_offset(pg, has ? page : 0, x.h, pos), g);
-    }
+    else
+      t.k[i].load(
+          pg.k + row_offset(pg, max(at.page[i], 0), x.h, min(at.first[i] + r, x.n - 1)), g);
   }
 }
 
 template <bool E4M3, bool WIDE>
-__device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TileAt& at,
+__device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TileAt<WIDE>& at,
                                        Tile<E4M3>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   t.there = 0;
+  if constexpr (WIDE) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    if (E4M3 && WIDE) {  // four positions' bytes at once: rows of one page, a multiple of 4
-      const int64_t e = exp_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
-      t.ke[i] = *reinterpret_cast<const uint32_t*>(pg.k_exps + e + 4 * g);
-      t.ve[i] = *reinterpret_cast<const uint32_t*>(pg.v_exps + e + 4 * g);
+    for (int i = 0; i < 2; ++i) {
+      if (at.page[i] >= 0) t.there |= 15u << (4 * i);
+      if (E4M3) {  // four positions' bytes at once: rows of one page, a multiple of 4
+        const int64_t e = exp_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
+        t.ke[i] = *reinterpret_cast<const uint32_t*>(pg.k_exps + e + 4 * g);
+        t.ve[i] = *reinterpret_cast<const uint32_t*>(pg.v_exps + e + 4 * g);
+      }
     }
-    if (E4M3 && !WIDE) t.ke[i] = t.ve[i] = 0;
-    if (WIDE && at.page[i] >= 0) t.there |= 15u << (4 * i);
+  } else {
+    uint32_t ke[8], ve[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint8_t* p;
-      if (WIDE) {
-        const uint32_t off = min((4 * g + j) * pg.row_bytes, at.cap[i]);
-        p = pg.v + half_base(pg, x, at, i) + off;
-      } else {
-        const int pos = min(at.first[i] + 4 * g + j, x.n - 1);
-        int page = x.table[pos >> pg.shift];
-        if ((unsigned)page < (unsigned)pg.num_pages) t.there |= 1u << (4 * i + j);
-        else page = 0;
-        if (E4M3) {
-          const int64_t e = exp_offset(pg, page, x.h, pos);
-          t.ke[i] |= (uint32_t)pg.k_exps[e] << (8 * j);
-          t.ve[i] |= (uint32_t)pg.v_exps[e] << (8 * j);
-        }
-        p = pg.v + row_offset(pg, page, x.h, pos);
-      }
-      uint32_t* v = t.v[4 * i + j];
+    for (int j = 0; j < 8; ++j) {
+      if (at.v_page[j] >= 0) t.there |= 1u << j;
       if (E4M3) {
-        const uint2 w = ld8_nt(p + 8 * r);
-        v[0] = w.x, v[1] = w.y;
-      } else {
-        const uint4 w = ld16_nt(reinterpret_cast<const uint16_t*>(p) + 8 * r);
-        v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
+        const int pos = min(at.first[j >> 2] + 4 * g + (j & 3), x.n - 1);
+        const int64_t e = exp_offset(pg, max(at.v_page[j], 0), x.h, pos);
+        ke[j] = pg.k_exps[e];
+        ve[j] = pg.v_exps[e];
       }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (E4M3) {
+        t.ke[i] = ke[4 * i] | ke[4 * i + 1] << 8 | ke[4 * i + 2] << 16 | ke[4 * i + 3] << 24;
+        t.ve[i] = ve[4 * i] | ve[4 * i + 1] << 8 | ve[4 * i + 2] << 16 | ve[4 * i + 3] << 24;
+      }
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint8_t* p;
+    const int i = j >> 2, row = 4 * g + (j & 3);
+    if constexpr (WIDE)
+      p = pg.v + half_base(pg, x, at, i) + (uint32_t)min(row * pg.row_bytes, at.cap[i]);
+    else
+      p = pg.v + row_offset(pg, max(at.v_page[j], 0), x.h, min(at.first[i] + row, x.n - 1));
+    uint32_t* v = t.v[j];
+    if (E4M3) {
+      const uint2 w = ld8_nt(p + 8 * r);
+      v[0] = w.x, v[1] = w.y;
+    } else {
+      const uint4 w = ld16_nt(reinterpret_cast<const uint16_t*>(p) + 8 * r);
+      v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
     }
   }
 }
@@ -1096,7 +1118,7 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
   const PagedPages& pg = a.pg;
   Tile<E4M3> t;
   float lg[8];
-  TileAt at = tile_at<WIDE>(pg, x, p);
+  TileAt<WIDE> at = tile_at<WIDE>(pg, x, p);
   load_k<E4M3, WIDE>(pg, x, at, t);
   load_v<E4M3, WIDE>(pg, x, at, t);
   if (p + kPagedStep < end) at = tile_at<WIDE>(pg, x, p + kPagedStep);
