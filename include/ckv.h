@@ -389,8 +389,9 @@ typedef struct ckv_rope {
 
 /* Head rows of num_tokens tokens: row (token, head) at element token *
  * token_stride + head * head_stride, its elements adjacent.  Strides are
- * multiples of 16 bytes, so rows may be slices of one projection's output.
- * dst is src (in place, the same strides) or does not overlap it. */
+ * multiples of 16 bytes, so rows may be slices of one projection's output
+ * (source strides may be 0: one row for all).  dst is src (in place, the same
+ * strides) or does not overlap it; its rows do not overlap each other. */
 typedef struct ckv_rows {
   const void* src;
   void* dst;
@@ -454,7 +455,7 @@ int ckv_rope_frequencies(int32_t rot_dim, double base, const ckv_rope_scaling* s
  *   CKV_CACHE_E4M3    8-bit e4m3 codes (no infinities; 0x7f and 0xff are NaN)
  *                     with one exponent byte a row, k_exps / v_exps
  *                     [num_pages][Hkv][page_size]: an element is code *
- *                     2^(byte - 127)
+ *                     2^(byte - 127), byte in [0, 254]
  * Strides are multiples of 16 bytes and at least 128 elements; page_size is a
  * power of two up to 65536, and page_size * row_stride elements take less than
  * 2^31 bytes.  Entries of page_table past ceil(n_b / page_size) are not used.
@@ -525,8 +526,10 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
  * q [B][T][Hq][d] bf16, out [B][T][Hq][d] fp32, lse [B][T][Hq] fp32.  A token
  * with nothing to attend to gets out = 0 and lse = -inf.  Logits, weights and
  * sums are fp32.  T >= 1 and T * G <= 16.  The positions of all units are cut
- * into equal ranges, one a workgroup; a unit that ranges share is joined by a
- * second launch, in a fixed order: the same call gives the same bits.
+ * into equal ranges, one a workgroup, and a unit that ranges share is joined by a
+ * second launch; where the stored positions (max_ctx) are few, every 128 of them
+ * have a workgroup and the join is inside the one launch.  Joins go in a fixed
+ * order: the same call gives the same bits.
  * Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
 int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
                           int32_t num_tokens, const uint16_t* q, const int32_t* ctx_lens,

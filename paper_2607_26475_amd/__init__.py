@@ -400,10 +400,11 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
-def _call(fn, t: torch.Tensor, stream, *args) -> None:
+def _call(fn, dev: int, stream, *args) -> None:
     """Calls an entry with its last argument, the stream (None: the current one
-    of t's device), with t's device current."""
-    dev = t.get_device()
+    of device dev), with dev current."""
+    if dev < 0:
+        raise ValueError("the tensors have to be on a GPU")
     handle = _raw_stream(dev) if stream is None else _stream(stream)
     if dev == torch.cuda.current_device():
         status = fn(*args, handle)
@@ -414,11 +415,12 @@ def _call(fn, t: torch.Tensor, stream, *args) -> None:
         _check(fn.__name__, status)
 
 
-def _int32(name: str, t: torch.Tensor, n: int) -> None:
-    """What the kernels index by has to be int32, dense and long enough."""
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.numel() < n:
-        raise ValueError(f"{name}: a dense int32 tensor of {n} elements, not {t.dtype} "
-                         f"{tuple(t.shape)}")
+def _dense(name: str, t: torch.Tensor, dtype, n: int, dev: int) -> None:
+    """What kernels read and write has to be there: dense, of its type, long
+    enough, on the device of the call."""
+    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n or t.get_device() != dev:
+        raise ValueError(f"{name}: a dense {dtype} tensor of {n} elements on device {dev}, not "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
 
 
 def rope_frequencies(rot_dim: int, base: float, kind: int = ROPE_PLAIN, factor: float = 1.0,
@@ -443,7 +445,7 @@ def rope_for(inv_freq: torch.Tensor, head_dim: int = 128, rot_dim: Optional[int]
             2 * inv_freq.numel() < rot:
         raise ValueError(f"inv_freq: {rot // 2} dense float64 frequencies")
     r = Rope(inv_freq.data_ptr(), head_dim, rot, layout, dtype, int(inverse), scale)
-    r.keep = inv_freq
+    r.keep, r.dev = inv_freq, inv_freq.get_device()
     return r
 
 
@@ -452,36 +454,44 @@ def rows_for(src: torch.Tensor, dst: Optional[torch.Tensor] = None) -> Rows:
     into those of another of the same shape, or in place."""
     dst = src if dst is None else dst
     if src.dim() != 3 or src.shape != dst.shape or src.dtype != dst.dtype or \
+            src.device != dst.device or \
             src.stride(2) != 1 or dst.stride(2) != 1:
         raise ValueError(f"rows: [tokens][heads][d] with adjacent elements, the same twice, not "
                          f"{tuple(src.shape)} and {tuple(dst.shape)}")
     r = Rows(src.data_ptr(), dst.data_ptr(), src.stride(0), src.stride(1), dst.stride(0),
              dst.stride(1), src.shape[1], 0)
     r.keep = (src, dst)
-    r.holds = (src.shape[0], src.shape[2], _ROPE_TYPES.get(src.dtype))
+    r.holds = (src.shape[0], src.shape[2], _ROPE_TYPES.get(src.dtype), src.get_device())
     return r
 
 
 _ROPE_TYPES = {torch.bfloat16: ROPE_BF16, torch.float32: ROPE_F32}
 
 
-def _rows_ok(name: str, rows: Rows, rope: Rope, n: int) -> None:
+def _rows_ok(name: str, rows: Rows, rope: Rope, n: int, dev: int) -> None:
     holds = getattr(rows, "holds", None)  # None: filled in by hand
-    if holds is not None and (holds[0] < n or holds[1] != rope.head_dim or holds[2] != rope.type):
+    if holds is not None and (holds[0] < n or holds[1] != rope.head_dim or
+                              holds[2] != rope.type or holds[3] != dev):
         t = rows.keep[0]
         raise ValueError(f"{name}: {n} tokens of rows of {rope.head_dim} elements of the rope's "
-                         f"type, not {t.dtype} {tuple(t.shape)}")
+                         f"type on device {dev}, not {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _rope_ok(rope: Rope, dev: int) -> None:
+    if getattr(rope, "dev", dev) != dev:
+        raise ValueError(f"the rope's frequencies are on {rope.keep.device}, not on device {dev}")
 
 
 def rope_rows(rope: Rope, positions: torch.Tensor, q: Rows, k: Optional[Rows] = None,
               stream=None) -> None:
     """Rotates the head rows of q (and k) by their tokens' positions."""
-    n = positions.numel()
-    _int32("positions", positions, n)
-    _rows_ok("q", q, rope, n)
+    n, dev = positions.numel(), positions.get_device()
+    _dense("positions", positions, torch.int32, n, dev)
+    _rope_ok(rope, dev)
+    _rows_ok("q", q, rope, n, dev)
     if k is not None:
-        _rows_ok("k", k, rope, n)
-    _call(_lib.ckv_rope_rows, positions, stream, rope, n, positions.data_ptr(), q, k)
+        _rows_ok("k", k, rope, n, dev)
+    _call(_lib.ckv_rope_rows, dev, stream, rope, n, positions.data_ptr(), q, k)
 
 
 def paged_cache_for(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
@@ -509,7 +519,11 @@ def paged_cache_for(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: to
                    k_pages.shape[2], k_pages.shape[0],
                    page_table.shape[1] if page_table.shape[0] == 1 else page_table.stride(0))
     c.keep = (k_pages, v_pages, page_table, k_exps, v_exps)
-    c.holds = (k_pages.shape[1], page_table.shape[0])
+    tensors = [x for x in c.keep if x is not None]
+    if any(x.device != k_pages.device for x in tensors):
+        raise ValueError("a cache's tensors on different devices")
+    c.holds = (k_pages.shape[1], page_table.shape[0], page_table.shape[1] * k_pages.shape[2],
+               k_pages.get_device())
     return c
 
 
@@ -518,11 +532,13 @@ def _stride(t: torch.Tensor, i: int) -> int:
     return t.stride(i) if t.shape[i] > 1 else max(t.stride(i), t.shape[3])
 
 
-def _cache_ok(shape: Shape, cache: PagedCache) -> None:
+def _cache_ok(shape: Shape, cache: PagedCache, dev: int) -> None:
     holds = getattr(cache, "holds", None)  # None: filled in by hand
-    if holds is not None and (holds[0] != shape.num_kv_heads or holds[1] < shape.batch):
-        raise ValueError(f"a cache of {holds[0]} heads and {holds[1]} requests for a shape of "
-                         f"{shape.num_kv_heads} and {shape.batch}")
+    if holds is not None and (holds[0] != shape.num_kv_heads or holds[1] < shape.batch or
+                              holds[2] < shape.max_ctx or holds[3] != dev):
+        raise ValueError(f"a cache of {holds[0]} heads, {holds[1]} requests and {holds[2]} "
+                         f"positions on device {holds[3]} for a shape of {shape.num_kv_heads}, "
+                         f"{shape.batch} and {shape.max_ctx} on {dev}")
 
 
 def paged_write(shape: Shape, cache: PagedCache, requests, positions: torch.Tensor,
@@ -530,21 +546,24 @@ def paged_write(shape: Shape, cache: PagedCache, requests, positions: torch.Tens
                 q: Optional[Rows] = None, stream=None) -> None:
     """Writes k, v [tokens][Hkv][128] into their pages (requests None: token t
     is request t's); with rope, keys (and the rows of q) are rotated."""
-    n = positions.numel()
-    _cache_ok(shape, cache)
-    _int32("positions", positions, n)
+    n, dev = positions.numel(), positions.get_device()
+    _cache_ok(shape, cache, dev)
+    _dense("positions", positions, torch.int32, n, dev)
     if requests is not None:
-        _int32("requests", requests, n)
+        _dense("requests", requests, torch.int32, n, dev)
     heads = shape.num_kv_heads
     want, strides = (n, heads, 128), k.stride()
     if k.shape != want or v.shape != want or strides != v.stride() or strides[2] != 1 or \
             (strides[1] != 128 and heads > 1) or k.dtype != torch.bfloat16 or \
-            v.dtype != torch.bfloat16:
-        raise ValueError(f"k, v: bf16 {want} with dense heads, not {k.dtype} {tuple(k.shape)}")
-    if q is not None and rope is not None:
-        _rows_ok("q", q, rope, n)
+            v.dtype != torch.bfloat16 or k.get_device() != dev or v.get_device() != dev:
+        raise ValueError(f"k, v: bf16 {want} with dense heads on device {dev}, not {k.dtype} "
+                         f"{tuple(k.shape)} on {k.device}")
+    if rope is not None:
+        _rope_ok(rope, dev)
+        if q is not None:
+            _rows_ok("q", q, rope, n, dev)
     stride = strides[0] if n > 1 else max(strides[0], 128 * heads)
-    _call(_lib.ckv_paged_write, positions, stream, shape, cache, n, _ptr(requests),
+    _call(_lib.ckv_paged_write, dev, stream, shape, cache, n, _ptr(requests),
           positions.data_ptr(), k.data_ptr(), v.data_ptr(), stride, rope, q)
 
 
@@ -552,33 +571,27 @@ def paged_read(shape: Shape, cache: PagedCache, ctx_lens: torch.Tensor, idx, n_s
                k_dst: torch.Tensor, v_dst: torch.Tensor, stream=None) -> None:
     """Rows idx of the pages (idx None: positions 0 .. k - 1) into k_dst, v_dst
     [B][Hkv][k][128] bf16."""
-    _cache_ok(shape, cache)
-    _int32("ctx_lens", ctx_lens, shape.batch)
-    units = shape.batch * shape.num_kv_heads
+    dev, units = ctx_lens.get_device(), shape.batch * shape.num_kv_heads
+    _cache_ok(shape, cache, dev)
+    _dense("ctx_lens", ctx_lens, torch.int32, shape.batch, dev)
     if idx is not None:
-        _int32("idx", idx, units * k)
+        _dense("idx", idx, torch.int32, units * k, dev)
     if n_sel is not None:
-        _int32("n_sel", n_sel, units)
-    for t in (k_dst, v_dst):
-        if t.dtype != torch.bfloat16 or not t.is_contiguous() or t.numel() < units * k * 128:
-            raise ValueError(f"k_dst, v_dst: dense bf16 of {units * k * 128} elements")
-    _call(_lib.ckv_paged_read, ctx_lens, stream, shape, cache, ctx_lens.data_ptr(), _ptr(idx),
+        _dense("n_sel", n_sel, torch.int32, units, dev)
+    _dense("k_dst", k_dst, torch.bfloat16, units * k * 128, dev)
+    _dense("v_dst", v_dst, torch.bfloat16, units * k * 128, dev)
+    _call(_lib.ckv_paged_read, dev, stream, shape, cache, ctx_lens.data_ptr(), _ptr(idx),
           _ptr(n_sel), k, k_dst.data_ptr(), v_dst.data_ptr())
-
-
-def _dense(name: str, t: torch.Tensor, dtype, n: int) -> None:
-    if t.dtype != dtype or not t.is_contiguous() or t.numel() < n:
-        raise ValueError(f"{name}: a dense {dtype} tensor of {n} elements, not {t.dtype} "
-                         f"{tuple(t.shape)}")
 
 
 def paged_score_keys(shape: Shape, cache: PagedCache, q: torch.Tensor, ctx_lens: torch.Tensor,
                      scale: float, scores: torch.Tensor, stream=None) -> None:
-    _cache_ok(shape, cache)
-    _int32("ctx_lens", ctx_lens, shape.batch)
-    _dense("q", q, torch.bfloat16, shape.batch * shape.num_q_heads * 128)
-    _dense("scores", scores, torch.float32, shape.batch * shape.num_kv_heads * shape.max_ctx)
-    _call(_lib.ckv_paged_score_keys, ctx_lens, stream, shape, cache, q.data_ptr(),
+    dev = ctx_lens.get_device()
+    _cache_ok(shape, cache, dev)
+    _dense("ctx_lens", ctx_lens, torch.int32, shape.batch, dev)
+    _dense("q", q, torch.bfloat16, shape.batch * shape.num_q_heads * 128, dev)
+    _dense("scores", scores, torch.float32, shape.batch * shape.num_kv_heads * shape.max_ctx, dev)
+    _call(_lib.ckv_paged_score_keys, dev, stream, shape, cache, q.data_ptr(),
           ctx_lens.data_ptr(), scale, scores.data_ptr())
 
 
@@ -587,14 +600,16 @@ def paged_decode_attn(shape: Shape, cache: PagedCache, num_tokens: int, q: torch
                       stream=None) -> None:
     """Attention of the last num_tokens tokens (q [B][T][Hq][128]) over the
     paged cache into out (fp32, like q) and, unless None, lse [B][T][Hq]."""
-    _cache_ok(shape, cache)
-    _int32("ctx_lens", ctx_lens, shape.batch)
-    rows = shape.batch * num_tokens * shape.num_q_heads
-    _dense("q", q, torch.bfloat16, rows * 128)
-    _dense("out", out, torch.float32, rows * 128)
+    dev, rows = ctx_lens.get_device(), shape.batch * num_tokens * shape.num_q_heads
+    _cache_ok(shape, cache, dev)
+    _dense("ctx_lens", ctx_lens, torch.int32, shape.batch, dev)
+    _dense("q", q, torch.bfloat16, rows * 128, dev)
+    _dense("out", out, torch.float32, rows * 128, dev)
     if lse is not None:
-        _dense("lse", lse, torch.float32, rows)
-    _call(_lib.ckv_paged_decode_attn, ctx_lens, stream, shape, cache, num_tokens, q.data_ptr(),
+        _dense("lse", lse, torch.float32, rows, dev)
+    if ws is not None:
+        _dense("ws", ws, torch.uint8, 0, dev)
+    _call(_lib.ckv_paged_decode_attn, dev, stream, shape, cache, num_tokens, q.data_ptr(),
           ctx_lens.data_ptr(), scale, out.data_ptr(), _ptr(lse), _ptr(ws),
           ws.numel() if ws is not None else 0)
 

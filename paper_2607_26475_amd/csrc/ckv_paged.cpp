@@ -36,7 +36,8 @@ int check_rope(const ckv_rope* r, RopeSpec* s) {
   return CKV_OK;
 }
 
-int check_rows(const char* what, const ckv_rows* rows, const RopeSpec& r, RopeRows* out) {
+int check_rows(const char* what, const ckv_rows* rows, int32_t tokens, const RopeSpec& r,
+               RopeRows* out) {
   if (!rows) return fail(CKV_EINVAL, "%s is NULL", what);
   if (!rows->src || !rows->dst || !aligned16(rows->src) || !aligned16(rows->dst))
     return fail(CKV_EINVAL, "%s.src and .dst must be 16-byte aligned pointers", what);
@@ -52,8 +53,12 @@ int check_rows(const char* what, const ckv_rows* rows, const RopeSpec& r, RopeRo
                   (long long)x);
   if (rows->src == rows->dst && (strides[0] != strides[2] || strides[1] != strides[3]))
     return fail(CKV_EINVAL, "%s: in place with different strides", what);
-  if (strides[3] < r.head_dim && rows->heads > 1)
-    return fail(CKV_ESHAPE, "%s: destination rows overlap", what);
+  // destination rows apart: heads within a token, or tokens within a head
+  const int64_t tok = strides[2], head = strides[3], d = r.head_dim, h = rows->heads;
+  const bool many = tokens > 1, by_token = (h == 1 || head >= d) &&
+                                           (!many || tok >= (h - 1) * head + d);
+  const bool by_head = many && tok >= d && (h == 1 || head >= (tokens - 1) * tok + d);
+  if (!by_token && !by_head) return fail(CKV_ESHAPE, "%s: destination rows overlap", what);
   out->src = rows->src;
   out->dst = rows->dst;
   out->src_tok = strides[0];
@@ -183,8 +188,8 @@ int ckv_rope_rows(const ckv_rope* rope, int32_t num_tokens, const int32_t* posit
   RopeArgs a = {};
   CKV_RC(check_rope(rope, &a.r));
   CKV_RC(check_num_tokens(num_tokens));
-  CKV_RC(check_rows("q", q, a.r, &a.q));
-  if (k) CKV_RC(check_rows("k", k, a.r, &a.k));
+  CKV_RC(check_rows("q", q, num_tokens, a.r, &a.q));
+  if (k) CKV_RC(check_rows("k", k, num_tokens, a.r, &a.k));
   if (a.q.heads + a.k.heads > 4096)
     return fail(CKV_ESHAPE, "%d heads in q and k (at most 4096)", a.q.heads + a.k.heads);
   CKV_PTR(positions);
@@ -268,7 +273,7 @@ int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_
     CKV_RC(check_rope(rope, &a.rope.r));
     if (a.rope.r.head_dim != kD || a.rope.r.f32)
       return fail(CKV_EUNSUPPORTED, "a cache's rope has bf16 rows of %d elements", kD);
-    if (q) CKV_RC(check_rows("q", q, a.rope.r, &a.rope.q));
+    if (q) CKV_RC(check_rows("q", q, num_tokens, a.rope.r, &a.rope.q));
   } else if (q) {
     return fail(CKV_EINVAL, "q without rope");
   }

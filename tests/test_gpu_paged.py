@@ -96,6 +96,20 @@ def test_rope_inverse_is_the_gradient():
         assert abs(diff - float(xx.grad[1, 1, 5])) <= slack
 
 
+def test_rope_of_one_row_for_all():
+    """A source of strides 0 and a destination with heads outermost."""
+    freq, _ = ckv.rope_frequencies(128, 10000.0)
+    x = torch.randn((1, 1, 128), generator=torch.Generator().manual_seed(6)).to(DEV)
+    y = torch.empty((3, 7, 128), device=DEV).transpose(0, 1)
+    pos = torch.arange(7, dtype=torch.int32)
+    ckv.rope_rows(ckv.rope_for(freq.to(DEV), dtype=ckv.ROPE_F32), pos.to(DEV),
+                  ckv.rows_for(x.expand(7, 3, 128), y))
+    src = x.cpu().expand(7, 3, 128)
+    want = rope64(src, pos, freq, 128, False)
+    assert torch.all((y.cpu().double() - want).abs() <=
+                     rope_slack(src, 128, False) + U24 * want.abs())
+
+
 def test_rope_undone():
     g = torch.Generator().manual_seed(4)
     freq, _ = ckv.rope_frequencies(128, 10000.0)
@@ -293,6 +307,31 @@ def test_paged_scores(kind, page, order, G):
     got = scores.cpu().double()
     assert torch.all(got[~there] == -math.inf)
     assert torch.all((got - want)[there].abs() <= tol[there])
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,Hkv,page,G,max_ctx", [
+    ([1, 20000, 0, 64, 513], 2, 16, 4, 30000), ([1, 20000, 0, 64, 513], 2, 4, 8, 30000),
+    ([900, 0, 7] * 110, 1, 64, 16, 1000), ([400] * 300, 1, 2, 1, 1100)])
+def test_paged_scores_by_ranges(kind, lens, Hkv, page, G, max_ctx):
+    """More steps than workgroups: ranges over requests and heads, tails filled
+    in pieces."""
+    _log("scores by ranges", kind, len(lens), page, G)
+    B = len(lens)
+    pool = Pool(lens, Hkv, page, kind, seed=3, holes=[(0, 0), (1, 3)], max_ctx=max_ctx)
+    q = torch.randn((B, Hkv * G, D), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    scores = torch.full((B, Hkv, max_ctx), 9.0, device=DEV)
+    ckv.paged_score_keys(pool.shape(G), pool.cache, q.to(DEV), pool.ctx, SCALE, scores)
+    got = scores.cpu().double()
+    for b, n in enumerate(lens):
+        x, k = q[b].double().view(Hkv, G, D), pool.K[b, :, :n]
+        want = torch.matmul(x, k.transpose(1, 2)).amax(1) * SCALE if n else torch.zeros(Hkv, 0)
+        tol = 130 * U24 * SCALE * torch.matmul(x.abs(), k.abs().transpose(1, 2)).amax(1) \
+            if n else torch.zeros(Hkv, 0)
+        there = pool.there[b, :n]
+        assert torch.all((got[b, :, :n] - want)[:, there].abs() <= tol[:, there]), b
+        assert torch.all(got[b, :, :n][:, ~there] == -math.inf), b
+        assert torch.all(got[b, :, n:] == -math.inf), b
 
 
 # ---- attention -------------------------------------------------------------------------

@@ -112,7 +112,9 @@ def test_rope_refusals(kw, status):
     (dict(src=None), "EINVAL"), (dict(dst=None), "EINVAL"), (dict(src=FAKE + 2), "EINVAL"),
     (dict(dst=FAKE + 4104), "EINVAL"), (dict(reserved=1), "EINVAL"), (dict(heads=0), "ESHAPE"),
     (dict(heads=4097), "ESHAPE"), (dict(st=1020), "ESHAPE"), (dict(sh=-128), "ESHAPE"),
-    (dict(dt=1 << 40), "ESHAPE"), (dict(dst=FAKE, dt=2048), "EINVAL"), (dict(dh=64), "ESHAPE")])
+    (dict(dt=1 << 40), "ESHAPE"), (dict(dst=FAKE, dt=2048), "EINVAL"), (dict(dh=64), "ESHAPE"),
+    (dict(dt=0), "ESHAPE"), (dict(dt=512), "ESHAPE"), (dict(dt=128, dh=128), "ESHAPE"),
+    (dict(heads=1, dt=64), "ESHAPE")])
 def test_rows_refusals(kw, status):
     assert call_rope(q=rows(**kw)) == STATUS[status]
     assert call_rope(k=rows(**kw)) == STATUS[status]
@@ -129,6 +131,8 @@ def test_rope_call_refusals():
     assert ckv._lib.ckv_rope_rows(None, 1, FAKE, rows(), None, None) == STATUS["EINVAL"]
     assert ckv._lib.ckv_rope_rows(rope(), 1, FAKE, None, None, None) == STATUS["EINVAL"]
     assert call_rope(n=0) == 0
+    # heads outermost; one row for every token and head as the source
+    assert call_rope(n=0, q=rows(dt=128, dh=5 * 128, st=0, sh=0)) == 0
     # fp32 rows: strides of 16 bytes are 4 elements
     assert call_rope(rope(type=1), n=0, q=rows(st=1020, dt=1020)) == 0
 
@@ -237,7 +241,12 @@ def test_binding_refuses_what_kernels_would_misread():
         ckv.rope_rows(r, torch.zeros(4, dtype=torch.int32), x)   # more tokens than rows
     with pytest.raises(ValueError):
         ckv.rope_rows(r, torch.zeros(3, dtype=torch.int32), ckv.rows_for(torch.zeros(3, 2, 128)))
+    with pytest.raises(ValueError, match="GPU"):                 # all as it should be, but here
+        ckv.rope_rows(r, torch.zeros(3, dtype=torch.int32), x)
     s = shape()
+    with pytest.raises(ValueError):                              # 5 pages a request, 4 in the table
+        ckv.paged_score_keys(shape(max_ctx=65), c, torch.zeros(2, 8, 128).bfloat16(),
+                             torch.zeros(2, dtype=torch.int32), 0.1, torch.zeros(2, 2, 65))
     pos, lens = torch.zeros(2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
     kv = torch.zeros((2, 2, 128), dtype=torch.bfloat16)
     with pytest.raises(ValueError):
