@@ -47,8 +47,7 @@ __device__ __forceinline__ uint2 ld8_nt(const uint8_t* p) {
 
 // ---- rotary positions ------------------------------------------------------------
 // (cos, sin) of pos * inv_freq.  The angle is formed in quarter turns in fp64
-// (a position of 2^20 leaves fp32 5 correct bits of a radian's fraction), its
-// whole quarters are taken off there, and what is left, |x| <= pi/4, goes through
+// (an fp32 angle of 2^20 radians is off by up to 1/16), its whole quarters are taken off there, and what is left, |x| <= pi/4, goes through
 // the Taylor series of sine (to x^9, remainder below 1.8e-9) and cosine (to
 // x^10, below 1.2e-10) in fp32.
 __device__ __forceinline__ float2 cos_sin(double quarters) {
@@ -493,21 +492,6 @@ struct Ctx {
   int b, h, n;            // request, KV head, positions (> 0 where rows are read)
   TablePtr table;         // the request's
 };
-
-// Page of a group's row `i` (0 .. 15) of the group that begins at p0, and the
-// row's position after clamping.
-template <bool WIDE>
-__device__ __forceinline__ void group_row(const PagedPages& pg, const Ctx& x, int p0, int i,
-                                          int* page, int* pos) {
-  if (WIDE) {
-    const int first = min(p0, (x.n - 1) & ~15);
-    *page = x.table[first >> pg.shift];
-    *pos = min(first + i, x.n - 1);
-  } else {
-    *pos = min(p0 + i, x.n - 1);
-    *page = x.table[*pos >> pg.shift];
-  }
-}
 
 // Position i of a group in the order that feeds a product's K operand: lane
 // (g, r) = (lane / 16, lane % 16) holds row r, in the fragments f = 0 .. 3 the
@@ -1298,6 +1282,16 @@ __device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h,
   float f[ROWS], M[ROWS], L[ROWS];
   float2 o[ROWS];
   uint64_t ml[ROWS];
+  constexpr int kAhead = 16 / ROWS;
+  uint64_t x[kAhead][ROWS];
+  auto load = [&](int i0) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k)
+        x[i][k] = __hip_atomic_load(p0[k] + min(i0 + i, steps - 2) * next + 2 + lane,
+                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  };
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) {
     row[k] = min(wave + 4 * k, rows - 1);
@@ -1305,6 +1299,7 @@ __device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h,
     ml[k] = __hip_atomic_load(p0[k] + min(lane, steps - 2) * next, __ATOMIC_RELAXED,
                               __HIP_MEMORY_SCOPE_AGENT);
   }
+  load(0);
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) {
     const bool own = lane == steps - 1, past = lane >= steps;
@@ -1312,18 +1307,11 @@ __device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h,
     const float l = own ? lds.jl[row[k]] : __uint_as_float((uint32_t)(ml[k] >> 32));
     M[k] = wave_max(m);
     f[k] = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - M[k]);
-    L[k] = wave_sum(f[k] == 0.f ? 0.f : f[k] * l);
+    L[k] = wave_sum(f[k] == 0.f && !own ? 0.f : f[k] * l);
     o[k] = make_float2(0.f, 0.f);
   }
-  constexpr int kAhead = ROWS == 1 ? 8 : 4;
   for (int i0 = 0; i0 < steps - 1; i0 += kAhead) {
-    uint64_t x[kAhead][ROWS];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i)
-#pragma unroll
-      for (int k = 0; k < ROWS; ++k)
-        x[i][k] = __hip_atomic_load(p0[k] + min(i0 + i, steps - 2) * next + 2 + lane,
-                                    __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (i0 > 0) load(i0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
 #pragma unroll
@@ -1353,9 +1341,12 @@ __device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h,
 // partial over through its flag, which takes the launch's tag once the partial's
 // device-coherent stores are done; the unit's last step's workgroup waits for
 // the flags, clears them and joins.  Only higher-numbered workgroups wait, for
-// lower-numbered ones that never do, and the wait is bounded (kFusedSpinLimit):
-// a broken hand-over leaves outputs undefined but ends.  8 units of 2001
-// positions: 8.1 us, against 10.4 with ranges and a second launch.
+// lower-numbered ones that never do, and the wait is bounded all the same: one
+// that ends without its flags (lower-numbered workgroups kept from the device
+// for that long) leaves NaN.  8 units of 2001 positions: 8.1 us, against 10.4
+// with ranges and a second launch.
+constexpr uint32_t kJoinSpinLimit = 1u << 24;  // about 20 s
+
 template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
@@ -1404,16 +1395,19 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
       __hip_atomic_store(a.flags + blockIdx.x, a.tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return;
   }
-  const int64_t first = (int64_t)unit * a.chunks;  // the unit's first workgroup
+  bool late = false;
   if (tid < steps - 1) {
-    uint64_t* f = a.flags + first + tid;
-    for (uint32_t spin = 0;
-         __hip_atomic_load(f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.tag &&
-         spin < kFusedSpinLimit;
-         ++spin)
+    uint64_t* f = a.flags + (int64_t)unit * a.chunks + tid;
+    uint32_t spin = 0;
+    while (__hip_atomic_load(f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.tag &&
+           spin < kJoinSpinLimit) {
       __builtin_amdgcn_s_sleep(2);
+      ++spin;
+    }
+    late = spin == kJoinSpinLimit;
     __hip_atomic_store(f, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   }
+  if (__syncthreads_or(late) && tid < rows) lds.jl[tid] = NAN;  // every output of the unit
   __syncthreads();
   if (rows <= 4) join_steps<1>(a, b, h, steps, part, lds);
   else if (rows <= 8) join_steps<2>(a, b, h, steps, part, lds);
