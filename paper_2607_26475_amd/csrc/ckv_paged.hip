@@ -777,17 +777,19 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
       for (int f = 0; f < 4; ++f)
         q[f] = as_bf16x8(ld16(a.q + ((int64_t)x.b * a.Hq + x.h * G + (r & (G - 1))) * kD +
                               frag_base<E4M3>(f, g)));
-      while (p < stop) {
-        const int held = p;
-        float* mine = hold[wave] + lane;
-        for (int i = 0; i < kScoreHold && p < stop; ++i, p += kScoreStep) {
-          const float best = step_scores<E4M3, WIDE, G>(s, q, a.scale);
-          load_score_step<E4M3, WIDE>(a.pg, x, min(p + kScoreStep, stop - 1) & ~15, pages, s);
-          pages = score_pages<WIDE>(a.pg, x, min(p + 2 * kScoreStep, stop - 1) & ~15);
-          mine[64 * i] = best;
+      float* mine = hold[wave] + lane;
+      for (int i = 0;;) {
+        mine[64 * i++] = step_scores<E4M3, WIDE, G>(s, q, a.scale);
+        p += kScoreStep;
+        const bool more = p < stop;
+        if (!more || i == kScoreHold) {
+          for (int w = p - i * kScoreStep, k = 0; k < i; ++k, w += kScoreStep)
+            if (w + lane < stop) scores[w + lane] = mine[64 * k];
+          i = 0;
         }
-        for (int i = 0, w = held; w < p; ++i, w += kScoreStep)
-          if (w + lane < stop) scores[w + lane] = mine[64 * i];
+        if (!more) break;
+        load_score_step<E4M3, WIDE>(a.pg, x, p, pages, s);
+        pages = score_pages<WIDE>(a.pg, x, min(p + kScoreStep, stop - 1) & ~15);
       }
     }
     at += take;
