@@ -403,10 +403,11 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   // every step a workgroup of its own, all at once, and the unit's last one
   // joins them: one launch, without a scan over the batch
   const int64_t steps = (d.max_ctx + kPagedStep - 1) / kPagedStep;
-  const int slots = std::min(paged_wgs_cap(d), kPagedWgsPerCu * device_cus());
+  const int cap = paged_wgs_cap(d), held = kPagedWgsPerCu * device_cus();
   const bool direct = steps <= kMaxDirect && steps * num_tokens * d.G <= kMaxDirectRows &&
-                      d.U * steps <= slots;
-  a.nwg = direct ? (int)(d.U * steps) : slots;
+                      d.U * steps <= std::min(cap, held);
+  a.nwg = direct ? (int)(d.U * steps)
+                 : std::min(cap, d.U < kFewUnits ? device_cus() : held);
   a.chunks = direct ? (int)steps : 0;
   a.tag = next_fused_tag();
   CKV_TRY_HIP(launch_paged_attn(a, cache->kind == CKV_CACHE_E4M3, s), "paged attention launch");

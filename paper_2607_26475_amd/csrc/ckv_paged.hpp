@@ -86,7 +86,11 @@ struct PagedTail {
 constexpr int kPagedTile = 32;              // positions of a wave's step
 constexpr int kPagedStep = 4 * kPagedTile;  // and of its workgroup's
 constexpr int kMaxPagedWgs = 1024;
-constexpr int kPagedWgsPerCu = 2;
+// Ranges of the attention: two a CU, which it holds at once; one where few units
+// mean that many would have to be joined (1 unit of 262144 bf16 positions 43.9 ->
+// 35.4 us, 2 65.9 -> 54.1, 4 98.6 -> 92.3; 16 units of 200 k e4m3 positions would
+// go 127 -> 135).
+constexpr int kPagedWgsPerCu = 2, kFewUnits = 8;
 // The attention in one launch: at most so many steps a unit (one wave's lanes
 // weigh them) and partial rows (its 4 waves load them).  8 units, one launch
 // against ranges and a join, us: 4 rows a unit, 256 positions 7.5 / 10.4, 4096
