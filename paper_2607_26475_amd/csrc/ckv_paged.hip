@@ -194,36 +194,45 @@ __device__ __forceinline__ void rope_turn(const RopeSpec& r, const RopeRows& row
   }
 }
 
-// Copies what lies past rot_dim: nothing in place.
-template <typename T, bool WHOLE>
-__device__ __forceinline__ void rope_copy(const RopeSpec& r, const RopeRows& rows, int t0,
-                                          int tokens) {
-  constexpr int N = WHOLE ? RopeVec<T>::kN : 1;
-  const int per_row = (r.head_dim - r.rot) / N;
-  if (rows.src == rows.dst || per_row == 0) return;
-  const int n = tokens * rows.heads * per_row;
+// Copies elements [from, to) of every row, in vectors (both multiples of them)
+// or one by one.
+template <typename T, bool VECTORS>
+__device__ __forceinline__ void copy_part(const RopeRows& rows, int t0, int tokens, int from,
+                                          int to) {
+  constexpr int N = VECTORS ? RopeVec<T>::kN : 1;
+  const int per_row = (to - from) / N, n = tokens * rows.heads * per_row;
   for (int e0 = threadIdx.x; e0 < n; e0 += kRopeBatch * kRopeThreads) {
     u32x4 x[kRopeBatch];
     T* dst[kRopeBatch];
 #pragma unroll
     for (int i = 0; i < kRopeBatch; ++i) {
       const int e = min(e0 + i * kRopeThreads, n - 1);
-      const int row = e / per_row, at = r.rot + N * (e - row * per_row);
+      const int row = e / per_row, at = from + N * (e - row * per_row);
       const int t = row / rows.heads, head = row - t * rows.heads;
       const T* src = static_cast<const T*>(rows.src) + (int64_t)(t0 + t) * rows.src_tok +
                      head * rows.src_head + at;
       dst[i] = static_cast<T*>(rows.dst) + (int64_t)(t0 + t) * rows.dst_tok +
                head * rows.dst_head + at;
-      if constexpr (WHOLE) x[i] = *reinterpret_cast<const u32x4*>(src);
+      if constexpr (VECTORS) x[i] = *reinterpret_cast<const u32x4*>(src);
       else x[i][0] = __builtin_bit_cast(typename RopeVec<T>::Bits, *src);
     }
 #pragma unroll
     for (int i = 0; i < kRopeBatch; ++i) {
       if (e0 + i * kRopeThreads >= n) break;
-      if constexpr (WHOLE) *reinterpret_cast<u32x4*>(dst[i]) = x[i];
+      if constexpr (VECTORS) *reinterpret_cast<u32x4*>(dst[i]) = x[i];
       else *dst[i] = __builtin_bit_cast(T, (typename RopeVec<T>::Bits)x[i][0]);
     }
   }
+}
+
+// Copies what lies past rot_dim: nothing in place.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void rope_copy(const RopeSpec& r, const RopeRows& rows, int t0,
+                                          int tokens) {
+  if (rows.src == rows.dst) return;
+  const int whole = (r.rot + RopeVec<T>::kN - 1) / RopeVec<T>::kN * RopeVec<T>::kN;
+  if (!WHOLE && whole > r.rot) copy_part<T, false>(rows, t0, tokens, r.rot, whole);
+  if (whole < r.head_dim) copy_part<T, true>(rows, t0, tokens, whole, r.head_dim);
 }
 
 template <typename T, bool HALF, bool WHOLE>
