@@ -94,9 +94,12 @@ template <>
 struct RopeVec<uint16_t> {
   using Bits = uint16_t;
   static constexpr int kN = 8;
-  static __device__ __forceinline__ void load(const uint16_t* p, float* x) { unpack8(ld16(p), x); }
-  static __device__ __forceinline__ void store(uint16_t* p, const float* y) {
-    *reinterpret_cast<uint4*>(p) = pack8_bf16(y);
+  static __device__ __forceinline__ void open(u32x4 v, float* x) {
+    unpack8(make_uint4(v[0], v[1], v[2], v[3]), x);
+  }
+  static __device__ __forceinline__ u32x4 close(const float* y) {
+    const uint4 v = pack8_bf16(y);
+    return u32x4{v.x, v.y, v.z, v.w};
   }
   static __device__ __forceinline__ float one(const uint16_t* p) {
     return __uint_as_float((uint32_t)*p << 16);
@@ -107,23 +110,25 @@ template <>
 struct RopeVec<float> {
   using Bits = uint32_t;
   static constexpr int kN = 4;
-  static __device__ __forceinline__ void load(const float* p, float* x) {
-    const float4 v = *reinterpret_cast<const float4*>(p);
-    x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+  static __device__ __forceinline__ void open(u32x4 v, float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = __uint_as_float(v[i]);
   }
-  static __device__ __forceinline__ void store(float* p, const float* y) {
-    *reinterpret_cast<float4*>(p) = make_float4(y[0], y[1], y[2], y[3]);
+  static __device__ __forceinline__ u32x4 close(const float* y) {
+    return u32x4{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]),
+                 __float_as_uint(y[3])};
   }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float y) { *p = y; }
 };
 
 // A row's work in items that each own what they read, so that a row may be
-// rotated in place.  WHOLE, where vectors of 16 bytes hold whole pairs or whole
-// runs of first elements (rot_dim a multiple of 16 bytes, of 32 for HALF): an
-// item is a vector of first elements with the vector of their partners, or a
-// vector of neighbouring pairs; else an item is one pair.  A thread asks for the
-// rows of kRopeBatch items before it turns the first.
+// rotated in place.  Where vectors of 16 bytes hold whole pairs or whole runs of
+// first elements (rot_dim a multiple of 16 bytes, of 32 for HALF) an item is a
+// vector of first elements with the vector of their partners, a vector of
+// neighbouring pairs, or (not in place) a vector past rot_dim; else an item is
+// one pair.  A thread asks for the rows of kRopeBatch items before it turns the
+// first.
 constexpr int kRopeBatch = 4;
 
 template <typename T>
@@ -132,64 +137,95 @@ __host__ __device__ __forceinline__ bool rope_whole(int rot, int layout) {
   return rot % (layout == CKV_ROPE_HALF ? 2 * n : n) == 0;
 }
 
-// Rotates `tokens` tokens' rows from token t0 on; tab as rope_table leaves it.
-template <typename T, bool HALF, bool WHOLE>
-__device__ __forceinline__ void rope_turn(const RopeSpec& r, const RopeRows& rows, int t0,
-                                          int tokens, const float2* tab) {
+// Rotates `tokens` tokens' rows from token t0 on, in vectors, and copies the
+// rest of them; tab as rope_table leaves it.
+template <typename T, bool HALF>
+__device__ __forceinline__ void rope_vectors(const RopeSpec& r, const RopeRows& rows, int t0,
+                                             int tokens, const float2* tab) {
   using V = RopeVec<T>;
-  constexpr int N = WHOLE ? V::kN : 1;
-  const int pairs = r.rot >> 1;
-  const int per_row = WHOLE && !HALF ? r.rot / N : pairs / N;
+  constexpr int N = V::kN;
+  const int pairs = r.rot >> 1, turn = (HALF ? pairs : r.rot) / N;
+  const int per_row = turn + (rows.src == rows.dst ? 0 : (r.head_dim - r.rot) / N);
   const int n = tokens * rows.heads * per_row;
   for (int e0 = threadIdx.x; e0 < n; e0 += kRopeBatch * kRopeThreads) {
-    float x1[kRopeBatch][N], x2[kRopeBatch][N];
+    u32x4 v1[kRopeBatch], v2[kRopeBatch];
     T* dst[kRopeBatch];
-    int pair[kRopeBatch], first[kRopeBatch];  // in the table, in the row
+    int pair[kRopeBatch];  // the item's first one in the table; -1: copied
 #pragma unroll
     for (int i = 0; i < kRopeBatch; ++i) {
       const int e = min(e0 + i * kRopeThreads, n - 1);  // past the end: loaded, not stored
       const int row = e / per_row, item = e - row * per_row;
       const int t = row / rows.heads, head = row - t * rows.heads;
+      const bool turned = item < turn;
+      const int first = turned ? N * item : r.rot + N * (item - turn);
       const T* src = static_cast<const T*>(rows.src) + (int64_t)(t0 + t) * rows.src_tok +
-                     head * rows.src_head;
-      dst[i] = static_cast<T*>(rows.dst) + (int64_t)(t0 + t) * rows.dst_tok + head * rows.dst_head;
-      first[i] = HALF ? N * item : WHOLE ? N * item : 2 * item;
-      pair[i] = t * pairs + (HALF ? N * item : WHOLE ? N / 2 * item : item);
-      if constexpr (WHOLE) {
-        V::load(src + first[i], x1[i]);
-        if (HALF) V::load(src + first[i] + pairs, x2[i]);
-      } else {
-        x1[i][0] = V::one(src + first[i]);
-        x2[i][0] = V::one(src + first[i] + (HALF ? pairs : 1));
-      }
+                     head * rows.src_head + first;
+      dst[i] = static_cast<T*>(rows.dst) + (int64_t)(t0 + t) * rows.dst_tok +
+               head * rows.dst_head + first;
+      pair[i] = turned ? t * pairs + (HALF ? N : N / 2) * item : -1;
+      v1[i] = *reinterpret_cast<const u32x4*>(src);
+      if (HALF) v2[i] = *reinterpret_cast<const u32x4*>(src + (turned ? pairs : 0));
     }
 #pragma unroll
     for (int i = 0; i < kRopeBatch; ++i) {
       if (e0 + i * kRopeThreads >= n) break;
-      float y1[N], y2[N];
-      if constexpr (WHOLE && !HALF) {
-#pragma unroll
-        for (int j = 0; j < N; j += 2) {
-          const float2 c = tab[pair[i] + j / 2];
-          y1[j] = x1[i][j] * c.x - x1[i][j + 1] * c.y;
-          y1[j + 1] = x1[i][j + 1] * c.x + x1[i][j] * c.y;
-        }
-        V::store(dst[i] + first[i], y1);
-      } else {
+      if (pair[i] < 0) {
+        *reinterpret_cast<u32x4*>(dst[i]) = v1[i];
+        continue;
+      }
+      const float2* c = tab + pair[i];
+      float x1[N], y1[N];
+      V::open(v1[i], x1);
+      if constexpr (HALF) {
+        float x2[N], y2[N];
+        V::open(v2[i], x2);
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          const float2 c = tab[pair[i] + j];
-          y1[j] = x1[i][j] * c.x - x2[i][j] * c.y;
-          y2[j] = x2[i][j] * c.x + x1[i][j] * c.y;
+          y1[j] = x1[j] * c[j].x - x2[j] * c[j].y;
+          y2[j] = x2[j] * c[j].x + x1[j] * c[j].y;
         }
-        if constexpr (WHOLE) {
-          V::store(dst[i] + first[i], y1);
-          V::store(dst[i] + first[i] + pairs, y2);
-        } else {
-          V::put(dst[i] + first[i], y1[0]);
-          V::put(dst[i] + first[i] + (HALF ? pairs : 1), y2[0]);
+        *reinterpret_cast<u32x4*>(dst[i] + pairs) = V::close(y2);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; j += 2) {
+          y1[j] = x1[j] * c[j / 2].x - x1[j + 1] * c[j / 2].y;
+          y1[j + 1] = x1[j + 1] * c[j / 2].x + x1[j] * c[j / 2].y;
         }
       }
+      *reinterpret_cast<u32x4*>(dst[i]) = V::close(y1);
+    }
+  }
+}
+
+// The same pair by pair.
+template <typename T, bool HALF>
+__device__ __forceinline__ void rope_pairs(const RopeSpec& r, const RopeRows& rows, int t0,
+                                           int tokens, const float2* tab) {
+  using V = RopeVec<T>;
+  const int pairs = r.rot >> 1, n = tokens * rows.heads * pairs;
+  for (int e0 = threadIdx.x; e0 < n; e0 += kRopeBatch * kRopeThreads) {
+    float x1[kRopeBatch], x2[kRopeBatch];
+    T* dst[kRopeBatch];
+    int pair[kRopeBatch];
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      const int e = min(e0 + i * kRopeThreads, n - 1);
+      const int row = e / pairs, item = e - row * pairs, first = HALF ? item : 2 * item;
+      const int t = row / rows.heads, head = row - t * rows.heads;
+      const T* src = static_cast<const T*>(rows.src) + (int64_t)(t0 + t) * rows.src_tok +
+                     head * rows.src_head + first;
+      dst[i] = static_cast<T*>(rows.dst) + (int64_t)(t0 + t) * rows.dst_tok +
+               head * rows.dst_head + first;
+      pair[i] = t * pairs + item;
+      x1[i] = V::one(src);
+      x2[i] = V::one(src + (HALF ? pairs : 1));
+    }
+#pragma unroll
+    for (int i = 0; i < kRopeBatch; ++i) {
+      if (e0 + i * kRopeThreads >= n) break;
+      const float2 c = tab[pair[i]];
+      V::put(dst[i], x1[i] * c.x - x2[i] * c.y);
+      V::put(dst[i] + (HALF ? pairs : 1), x2[i] * c.x + x1[i] * c.y);
     }
   }
 }
@@ -225,14 +261,19 @@ __device__ __forceinline__ void copy_part(const RopeRows& rows, int t0, int toke
   }
 }
 
-// Copies what lies past rot_dim: nothing in place.
-template <typename T, bool WHOLE>
-__device__ __forceinline__ void rope_copy(const RopeSpec& r, const RopeRows& rows, int t0,
-                                          int tokens) {
-  if (rows.src == rows.dst) return;
-  const int whole = (r.rot + RopeVec<T>::kN - 1) / RopeVec<T>::kN * RopeVec<T>::kN;
-  if (!WHOLE && whole > r.rot) copy_part<T, false>(rows, t0, tokens, r.rot, whole);
-  if (whole < r.head_dim) copy_part<T, true>(rows, t0, tokens, whole, r.head_dim);
+template <typename T, bool HALF, bool WHOLE>
+__device__ __forceinline__ void rope_rows(const RopeSpec& r, const RopeRows& rows, int t0,
+                                          int tokens, const float2* tab) {
+  if constexpr (WHOLE) {
+    rope_vectors<T, HALF>(r, rows, t0, tokens, tab);
+  } else {
+    rope_pairs<T, HALF>(r, rows, t0, tokens, tab);
+    if (rows.src == rows.dst) return;
+    constexpr int N = RopeVec<T>::kN;
+    const int whole = (r.rot + N - 1) / N * N;  // the next vector
+    if (whole > r.rot) copy_part<T, false>(rows, t0, tokens, r.rot, whole);
+    if (whole < r.head_dim) copy_part<T, true>(rows, t0, tokens, whole, r.head_dim);
+  }
 }
 
 template <typename T, bool HALF, bool WHOLE>
@@ -242,11 +283,8 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int per) {
   const int tokens = min(per, a.tokens - t0);
   rope_table(a.r, a.pos, t0, tokens, tab);
   __syncthreads();
-  rope_turn<T, HALF, WHOLE>(a.r, a.q, t0, tokens, tab);
-  rope_copy<T, WHOLE>(a.r, a.q, t0, tokens);
-  if (a.k.heads == 0) return;
-  rope_turn<T, HALF, WHOLE>(a.r, a.k, t0, tokens, tab);
-  rope_copy<T, WHOLE>(a.r, a.k, t0, tokens);
+  rope_rows<T, HALF, WHOLE>(a.r, a.q, t0, tokens, tab);
+  if (a.k.heads) rope_rows<T, HALF, WHOLE>(a.r, a.k, t0, tokens, tab);
 }
 
 // What a kernel only reads, for scalar loads where the index is the wave's.
@@ -408,15 +446,14 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
   }
   if (TURN == Turn::kNone || a.rope.q.heads == 0) return;
   if (TURN == Turn::kHalf) {
-    rope_turn<uint16_t, true, true>(r, a.rope.q, t0, tokens, tab);
+    rope_rows<uint16_t, true, true>(r, a.rope.q, t0, tokens, tab);
   } else if (TURN == Turn::kPairs) {
-    rope_turn<uint16_t, false, true>(r, a.rope.q, t0, tokens, tab);
+    rope_rows<uint16_t, false, true>(r, a.rope.q, t0, tokens, tab);
   } else if (r.layout == CKV_ROPE_HALF) {
-    rope_turn<uint16_t, true, false>(r, a.rope.q, t0, tokens, tab);
+    rope_rows<uint16_t, true, false>(r, a.rope.q, t0, tokens, tab);
   } else {
-    rope_turn<uint16_t, false, false>(r, a.rope.q, t0, tokens, tab);
+    rope_rows<uint16_t, false, false>(r, a.rope.q, t0, tokens, tab);
   }
-  rope_copy<uint16_t, TURN != Turn::kEach>(r, a.rope.q, t0, tokens);
 }
 
 // ---- reading back --------------------------------------------------------------------
