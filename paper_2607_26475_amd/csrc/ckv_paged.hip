@@ -1139,6 +1139,28 @@ __device__ __forceinline__ void tile_rest(Tile<E4M3>& t, bool masked, int p, int
   tile_output<E4M3>(t, part, st);
 }
 
+// The next step from `next` on that has a page, with its lookup.  Steps whose
+// whole pages are gone are passed over, 64 lookups at a time, so that a context's
+// time goes by what eviction left of it: 150000 to 200001 positions, of which the
+// first page and the last 1024 are kept, 98 -> 34 us (e4m3, two sequences); with
+// every page there the same.  The steps of small pages are all taken.
+template <bool WIDE>
+__device__ __forceinline__ int with_pages(const PagedPages& pg, const Ctx& x, int next, int end,
+                                          TileAt<WIDE>* at) {
+  if (WIDE)
+    while (next < end && (at->page[0] & at->page[1]) < 0) {  // 64 steps at a time
+      const int p = next + (int)(threadIdx.x & 63) * kPagedStep;
+      const int last = min(end, x.n) - 1;
+      bool any = false;
+      if (p <= last)
+        any = page_at(pg, x, p) >= 0 || page_at(pg, x, min(p + 16, x.n - 1)) >= 0;
+      const uint64_t mask = __ballot(any) & ~1ull;  // `next` itself has none
+      next += (mask ? __builtin_ctzll(mask) : 64) * kPagedStep;
+      *at = tile_at<WIDE>(pg, x, min(next, end - 1));
+    }
+  return next;
+}
+
 // A wave's steps of a piece: positions [p, end) in strides of kPagedStep.  Only
 // the last one can meet the end of a query row's positions (T <= 16 of them are
 // not seen by all); the loop's loads are unconditional, so that each wait is
@@ -1151,18 +1173,26 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
   Tile<E4M3> t;
   float lg[8];
   TileAt<WIDE> at = tile_at<WIDE>(pg, x, p);
+  p = with_pages<WIDE>(pg, x, p, end, &at);
+  if (p >= end) return;
   load_k<E4M3, WIDE>(pg, x, at, t);
   load_v<E4M3, WIDE>(pg, x, at, t);
-  if (p + kPagedStep < end) at = tile_at<WIDE>(pg, x, p + kPagedStep);
-  for (; p + kPagedStep < end; p += kPagedStep) {
+  int next = p + kPagedStep;
+  at = tile_at<WIDE>(pg, x, min(next, end - 1));
+  next = with_pages<WIDE>(pg, x, next, end, &at);
+  while (next < end) {
     tile_logits<E4M3, WIDE>(t, q, lg);
     load_k<E4M3, WIDE>(pg, x, at, t);
     __builtin_amdgcn_sched_barrier(0);
+    TileAt<WIDE> then = at;
+    if (WIDE) then = tile_at<WIDE>(pg, x, min(next + kPagedStep, end - 1));
     const bool masked = WIDE ? t.there != 255u : __any(t.there != 255u);
     tile_rest<E4M3>(t, masked, p, limit, c, lg, st);
     __builtin_amdgcn_sched_barrier(0);
     load_v<E4M3, WIDE>(pg, x, at, t);
-    at = tile_at<WIDE>(pg, x, min(p + 2 * kPagedStep, end - 1));
+    p = next;
+    at = WIDE ? then : tile_at<WIDE>(pg, x, min(next + kPagedStep, end - 1));
+    next = with_pages<WIDE>(pg, x, next + kPagedStep, end, &at);
   }
   tile_logits<E4M3, WIDE>(t, q, lg);
   tile_rest<E4M3>(t, true, p, limit, c, lg, st);
