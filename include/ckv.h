@@ -402,8 +402,8 @@ typedef struct ckv_rows {
 } ckv_rows;
 
 /* Rotates the rows of q and, if k is not NULL, of k, token t by positions[t]
- * (int32, device), in one launch.  0 <= num_tokens <= 2^24; at most 4096
- * heads in q and k together. */
+ * (int32, device), in one launch.  0 <= num_tokens <= 2^24 (without
+ * tokens addresses may be NULL); at most 4096 heads in q and k together. */
 int ckv_rope_rows(const ckv_rope* rope, int32_t num_tokens, const int32_t* positions,
                   const ckv_rows* q, const ckv_rows* k, void* stream);
 
@@ -480,9 +480,9 @@ typedef struct ckv_paged_cache {
 /* Writes the K and V rows of num_tokens tokens into their pages: token t goes
  * to position positions[t] of request requests[t] (NULL: request t).  k, v:
  * [num_tokens][Hkv][d] bf16 at token stride kv_token_stride elements (a
- * multiple of 8, at least Hkv * d).  A token whose position is outside
- * [0, max_ctx) (-1: padding), whose request is outside [0, B) or whose page is
- * not there is not written.  Positions written by one call are distinct (the
+ * multiple of 8, at least Hkv * d); without tokens they may be NULL.
+ * A token whose position is outside [0, max_ctx) (-1: padding), whose request is
+ * outside [0, B) or whose page is not there is not written.  Positions written by one call are distinct (the
  * bytes of a row written twice are unspecified, inside the row).  All other
  * rows keep their bytes.
  *   With rope (bf16, head_dim 128), K rows are turned by their positions on the

@@ -39,7 +39,7 @@ int check_rope(const ckv_rope* r, RopeSpec* s) {
 int check_rows(const char* what, const ckv_rows* rows, int32_t tokens, const RopeSpec& r,
                RopeRows* out) {
   if (!rows) return fail(CKV_EINVAL, "%s is NULL", what);
-  if (!rows->src || !rows->dst || !aligned16(rows->src) || !aligned16(rows->dst))
+  if (tokens > 0 && (!rows->src || !rows->dst || !aligned16(rows->src) || !aligned16(rows->dst)))
     return fail(CKV_EINVAL, "%s.src and .dst must be 16-byte aligned pointers", what);
   if (rows->reserved != 0) return fail(CKV_EINVAL, "%s.reserved must be 0", what);
   if (rows->heads < 1 || rows->heads > 4096)
@@ -192,8 +192,8 @@ int ckv_rope_rows(const ckv_rope* rope, int32_t num_tokens, const int32_t* posit
   if (k) CKV_RC(check_rows("k", k, num_tokens, a.r, &a.k));
   if (a.q.heads + a.k.heads > 4096)
     return fail(CKV_ESHAPE, "%d heads in q and k (at most 4096)", a.q.heads + a.k.heads);
+  if (num_tokens == 0) return CKV_OK;  // without rows their addresses may be NULL
   CKV_PTR(positions);
-  if (num_tokens == 0) return CKV_OK;
   a.pos = positions;
   a.tokens = num_tokens;
   CKV_TRY_HIP(launch_rope(a, (hipStream_t)stream), "rope launch");
@@ -259,10 +259,6 @@ int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_
   CKV_RC(check_shape(shape, &d));
   CKV_RC(check_cache(cache, d, &a.pg));
   CKV_RC(check_num_tokens(num_tokens));
-  if (requests) CKV_PTR(requests);
-  CKV_PTR(positions);
-  CKV_PTR(k);
-  CKV_PTR(v);
   if ((kv_token_stride & 7) || kv_token_stride < (int64_t)d.Hkv * kD ||
       kv_token_stride > ((int64_t)1 << 38))
     return fail(CKV_ESHAPE, "kv_token_stride %lld (>= Hkv * 128, a multiple of 8)",
@@ -277,7 +273,12 @@ int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_
   } else if (q) {
     return fail(CKV_EINVAL, "q without rope");
   }
-  if (num_tokens == 0 || d.U == 0) return CKV_OK;
+  if (num_tokens == 0) return CKV_OK;  // without rows their addresses may be NULL
+  if (requests) CKV_PTR(requests);
+  CKV_PTR(positions);
+  CKV_PTR(k);
+  CKV_PTR(v);
+  if (d.U == 0 && !q) return CKV_OK;  // no requests: all tokens are padding
   hipStream_t s = (hipStream_t)stream;
   CKV_RC(debug_check_paged(s, a.pg, nullptr, requests, positions, d.B, d.max_ctx, num_tokens));
   a.rope.pos = positions;

@@ -213,3 +213,26 @@ def test_two_streams_with_a_workspace_each(lens, max_ctx):
                                   spaces[j], stream=streams[j])
     torch.cuda.synchronize()
     assert torch.equal(outs, alone.expand_as(outs))
+
+
+def test_no_tokens_and_no_requests():
+    """Empty tensors, and a batch without requests whose queries are rotated all
+    the same."""
+    pool = Pool([40], 2, 16, "bf16", seed=1)
+    was = [t.clone() for t in (pool.k, pool.v)]
+    freq, _ = ckv.rope_frequencies(D, 10000.0)
+    r = ckv.rope_for(freq.to(DEV))
+    none = torch.empty((0, 2, D), dtype=torch.bfloat16, device=DEV)
+    pos = torch.empty(0, dtype=torch.int32, device=DEV)
+    ckv.rope_rows(r, pos, ckv.rows_for(none))
+    ckv.paged_write(pool.shape(1), pool.cache, None, pos, none, none, r, ckv.rows_for(none))
+    x = torch.randn((3, 2, D), generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    pos = torch.tensor([7, 0, 39], dtype=torch.int32, device=DEV)
+    xd, out = x.to(DEV), torch.zeros((3, 2, D), dtype=torch.bfloat16, device=DEV)
+    want = torch.zeros_like(out)
+    ckv.paged_write(ckv.shape_for(0, 2, 2, 40), pool.cache, torch.zeros_like(pos), pos, xd, xd, r,
+                    ckv.rows_for(xd, out))
+    ckv.rope_rows(r, pos, ckv.rows_for(xd, want))
+    assert torch.equal(out, want) and bool((out != 0).any())
+    for t, old in zip((pool.k, pool.v), was):
+        assert torch.equal(t.view(torch.int16), old.view(torch.int16))

@@ -334,3 +334,18 @@ def test_plain_e4m3_against_torch():
     codes, e = e4m3_64(v * 2.0 ** -30)
     assert torch.equal(codes[0], every) and int(e[0]) == 97
     assert torch.equal(values(codes, e), v * 2.0 ** -30)
+
+
+def test_no_tokens():
+    """Empty tensors have no address; all else is checked as ever."""
+    lib, r = ckv._lib, rope()
+    none = rows(src=None, dst=None)
+    assert lib.ckv_rope_rows(r, 0, None, none, none, None) == 0
+    assert lib.ckv_rope_rows(r, 1, FAKE, none, None, None) == STATUS["EINVAL"]
+    assert lib.ckv_rope_rows(rope(rot_dim=3), 0, None, none, None, None) == STATUS["ESHAPE"]
+    s, c = shape(), cache()
+    write = lambda n, stride: lib.ckv_paged_write(  # noqa: E731
+        s, c, n, None, None, None, None, stride, r, none, None)
+    wide = s.num_kv_heads * 128
+    assert write(0, wide) == 0
+    assert write(0, wide - 8) == STATUS["ESHAPE"] and write(1, wide) == STATUS["EINVAL"]
