@@ -398,6 +398,7 @@ CACHE_BF16, CACHE_E4M3 = 0, 1
 # 8 us call).
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def _call(fn, dev: int, stream, *args) -> None:
@@ -406,7 +407,7 @@ def _call(fn, dev: int, stream, *args) -> None:
     if dev < 0:
         raise ValueError("the tensors have to be on a GPU")
     handle = _raw_stream(dev) if stream is None else _stream(stream)
-    if dev == torch.cuda.current_device():
+    if dev == _current_device():
         status = fn(*args, handle)
     else:
         with torch.cuda.device(dev):
