@@ -528,7 +528,7 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
  * sums are fp32.  T >= 1 and T * G <= 16.  The positions of all units are cut
  * into equal ranges, one a workgroup, and a unit that ranges share is joined by a
  * second launch; where the stored positions (max_ctx) are few, every 128 of them
- * have a workgroup and the join is inside the one launch.  Joins go in a fixed
+ * (up to 1024) have a workgroup and the join is inside the one launch.  Joins go in a fixed
  * order: the same call gives the same bits.
  * Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
 int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,

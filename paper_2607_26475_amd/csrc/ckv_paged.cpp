@@ -401,15 +401,20 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.T = num_tokens;
   a.lg = __builtin_ctz((unsigned)d.G);
   a.max_ctx = d.max_ctx;
-  // every step a workgroup of its own, all at once, and the unit's last one
-  // joins them: one launch, without a scan over the batch
+  // pieces of few steps, a workgroup each and all at once (or whole units), whose
+  // last one in a unit joins them: one launch, without a scan over the batch
   const int64_t steps = (d.max_ctx + kPagedStep - 1) / kPagedStep;
   const int cap = paged_wgs_cap(d), held = kPagedWgsPerCu * device_cus();
-  const bool direct = steps <= kMaxDirect && steps * num_tokens * d.G <= kMaxDirectRows &&
-                      d.U * steps <= std::min(cap, held);
-  a.nwg = direct ? (int)(d.U * steps)
-                 : std::min(cap, d.U < kFewUnits ? device_cus() : held);
-  a.chunks = direct ? (int)steps : 0;
+  const int64_t most = std::min(cap, held);
+  auto pieces = [&](int lg) { return ((steps - 1) >> lg) + 1; };
+  int lg = 0;
+  while (lg < kMaxPiece && d.U * pieces(lg) > most) ++lg;
+  const int64_t n = pieces(lg), wgs = d.U * n;
+  const bool direct = n <= kMaxDirect && n * num_tokens * d.G <= kMaxDirectRows &&
+                      (wgs <= most || (n == 1 && wgs < ((int64_t)1 << 23)));
+  a.nwg = direct ? (int)wgs : std::min(cap, d.U < kFewUnits ? device_cus() : held);
+  a.chunks = direct ? (int)n : 0;
+  a.piece = lg;
   a.tag = next_fused_tag();
   CKV_TRY_HIP(launch_paged_attn(a, cache->kind == CKV_CACHE_E4M3, s), "paged attention launch");
   return CKV_OK;

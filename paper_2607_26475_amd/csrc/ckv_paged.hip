@@ -1423,39 +1423,40 @@ __device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h,
   }
 }
 
-// The same with a workgroup for every step of every unit (workgroup unit *
-// chunks + step) and the join inside the launch, for few steps: each hands its
-// partial over through its flag, which takes the launch's tag once the partial's
-// device-coherent stores are done; the unit's last step's workgroup waits for
-// the flags, clears them and joins.  Only higher-numbered workgroups wait, for
-// lower-numbered ones that never do, and the wait is bounded all the same: one
-// that ends without its flags (lower-numbered workgroups kept from the device
-// for that long) leaves NaN.  8 units of 2001 positions: 7.6 us, against 10.4
-// with ranges and a second launch; a chain of latencies (length, page, rows,
-// hand-over, join), which 8 MB of rows hardly lengthen.
+// The same with a workgroup for every piece of 2^piece steps of every unit
+// (workgroup unit * chunks + piece) and the join inside the launch, for few
+// steps: each hands its partial over through its flag, which takes the launch's
+// tag once the partial's device-coherent stores are done; the workgroup of the
+// unit's last piece waits for the flags, clears them and joins.  Only
+// higher-numbered workgroups wait, for lower-numbered ones that never do, and the
+// wait is bounded all the same: one that ends without its flags (lower-numbered
+// workgroups kept from the device for that long) leaves NaN.  8 units of 2001
+// positions: 7.6 us, against 10.4 with ranges and a second launch; a chain of
+// latencies (length, page, rows, hand-over, join), which 8 MB of rows hardly
+// lengthen.
 constexpr uint32_t kJoinSpinLimit = 1u << 24;  // about 20 s
 
 template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, rows = a.T << a.lg;
-  const int unit = blockIdx.x / a.chunks, step = blockIdx.x - unit * a.chunks;
+  const int unit = blockIdx.x / a.chunks, piece = blockIdx.x - unit * a.chunks;
   const int b = unit / a.pg.Hkv, h = unit - b * a.pg.Hkv;
   const int n = clamp_len(((TablePtr)(uintptr_t)a.ctx_lens)[b], a.max_ctx);
-  const int steps = (n + kPagedStep - 1) / kPagedStep;
-  if (step >= steps) {
-    if (step == 0)  // no positions: this unit's query rows
+  const int pieces = (n + (kPagedStep << a.piece) - 1) / kPagedStep >> a.piece;
+  if (piece >= pieces) {
+    if (piece == 0)  // no positions: this unit's query rows
       for (int t = 0; t < a.T; ++t)
         store_empty(a, out_row(a, b, h, t << a.lg), (int64_t)1 << a.lg);
     return;
   }
-  attn_piece<E4M3, WIDE>(a, b, h, n, step, 1, lds);
-  const bool last = step == steps - 1;
+  attn_piece<E4M3, WIDE>(a, b, h, n, piece << a.piece, 1 << a.piece, lds);
+  const bool last = piece == pieces - 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * rows * kPartStride;
   for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
     const int row = i >> 5, d = 4 * (i & 31);
     const Partial p = join_waves(lds, row, d);
-    if (steps == 1) {
+    if (pieces == 1) {
       store_result(a, b, h, row, d, p);
     } else if (last) {  // (row, d) of o[0] is read by this thread alone
       *reinterpret_cast<float4*>(&lds.o[0][row][d]) = p.o;
@@ -1475,7 +1476,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
                            __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
   }
-  if (steps == 1) return;
+  if (pieces == 1) return;
   if (!last) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
@@ -1484,7 +1485,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
     return;
   }
   bool late = false;
-  if (tid < steps - 1) {
+  if (tid < pieces - 1) {
     uint64_t* f = a.flags + (int64_t)unit * a.chunks + tid;
     uint32_t spin = 0;
     while (__hip_atomic_load(f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.tag &&
@@ -1497,9 +1498,9 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
   }
   if (__syncthreads_or(late) && tid < rows) lds.jl[tid] = NAN;  // every output of the unit
   __syncthreads();
-  if (rows <= 4) join_steps<1>(a, b, h, steps, part, lds);
-  else if (rows <= 8) join_steps<2>(a, b, h, steps, part, lds);
-  else join_steps<4>(a, b, h, steps, part, lds);
+  if (rows <= 4) join_steps<1>(a, b, h, pieces, part, lds);
+  else if (rows <= 8) join_steps<2>(a, b, h, pieces, part, lds);
+  else join_steps<4>(a, b, h, pieces, part, lds);
 }
 
 // Joins the unit that workgroup blockIdx.x's range left unfinished: query row

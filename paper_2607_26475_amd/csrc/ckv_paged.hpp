@@ -91,12 +91,19 @@ constexpr int kMaxPagedWgs = 1024;
 // 35.4 us, 2 65.9 -> 54.1, 4 98.6 -> 92.3; 16 units of 200 k e4m3 positions would
 // go 127 -> 135).
 constexpr int kPagedWgsPerCu = 2, kFewUnits = 8;
-// The attention in one launch: at most so many steps a unit (one wave's lanes
+// The attention in one launch: at most so many pieces a unit (one wave's lanes
 // weigh them) and partial rows (its 4 waves load them).  8 units, one launch
 // against ranges and a join, us: 4 rows a unit, 256 positions 7.5 / 10.4, 4096
 // 9.6 / 12.5, 8192 14.4 / 17.4; 16 rows, 256 positions 9.9 / 10.9, 2048 12.5 /
 // 13.5, 8192 27.5 / 24.1; 1 unit of 16 rows, 2048 11.6 / 11.3, 4096 13.5 / 12.3.
 constexpr int kMaxDirect = 64, kMaxDirectRows = 256;
+// Where a step each would be more workgroups than the device holds, pieces of up
+// to 2^3 steps, or whole units that short, however many.  Against ranges, us: 64
+// e4m3 units of 2048 positions 18.1 -> 13.5, 512 bf16 units of 100 to 1000 38.1 ->
+// 29.8, 78 of 2397 28.1 -> 22.4, 8 of 32768 33.1 -> 29.7.  Pieces of 16 would give
+// a batch of even lengths up to 12 % more and cost one of 32 with a single long
+// sequence 20.1 -> 28.4.
+constexpr int kMaxPiece = 3;
 constexpr int kReadSlots = 32;              // slots of a reading workgroup
 
 struct PagedAttnArgs {
@@ -112,7 +119,8 @@ struct PagedAttnArgs {
   float scale;
   int32_t B, Hq, T, lg;    // lg: log2 G
   int32_t max_ctx, nwg;
-  int32_t chunks;          // direct: workgroups (steps) of a unit; else 0
+  int32_t chunks;          // direct: workgroups (pieces) of a unit; else 0
+  int32_t piece;           // direct: a piece has 2^piece steps
 };
 
 // Debug mode's checks of paged inputs (CheckArgs' codes go on: 4 page_table

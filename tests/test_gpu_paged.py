@@ -408,6 +408,25 @@ def test_units_over_many_ranges(kind, lens, Hkv, G, T):
     _check_attention(pool, q, out, lse, T)
 
 
+EDGES = [0, 1, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 5, 640]
+
+
+@pytest.mark.parametrize("kind,page", [("bf16", 16), ("e4m3", 64), ("bf16", 4)])
+@pytest.mark.parametrize("B,Hkv,G,T", [(40, 2, 2, 1), (75, 2, 1, 3), (130, 2, 4, 1), (300, 2, 1, 2),
+                                       (20, 2, 16, 1)])
+def test_pieces_of_several_steps(kind, page, B, Hkv, G, T):
+    """A workgroup for 2, 4 and 8 steps, and for whole units, more of them than
+    the device holds at once; lengths about the pieces' ends."""
+    _log("pieces", kind, page, B, Hkv, G, T)
+    lens = [EDGES[(5 * i + i // 14) % 14] for i in range(B)]
+    holes = [(3, 0), (4, 1), (9, 0), (9, 1)]
+    pool = Pool(lens, Hkv, page, kind, seed=B, holes=holes, max_ctx=1000)
+    q, out, lse = _attend(pool, G, T)
+    _check_attention(pool, q, out, lse, T)
+    _, again, _ = _attend(pool, G, T)
+    assert torch.equal(out, again)
+
+
 def test_shared_pages_and_no_lse():
     pool = Pool([100, 90], 2, 32, "bf16", seed=3, share=True)
     q, out, _ = _attend(pool, 4, 1, lse=False)
