@@ -407,11 +407,14 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   const int cap = paged_wgs_cap(d), held = kPagedWgsPerCu * device_cus();
   const int64_t most = std::min(cap, held);
   auto pieces = [&](int lg) { return ((steps - 1) >> lg) + 1; };
+  const int64_t joined = std::min<int64_t>(kMaxDirect, kMaxDirectRows / (num_tokens * d.G));
+  auto fits = [&](int64_t n) {
+    return n <= joined && (d.U * n <= most || (n == 1 && d.U < (1 << 23)));
+  };
   int lg = 0;
-  while (lg < kMaxPiece && d.U * pieces(lg) > most) ++lg;
+  while (!fits(pieces(lg)) && lg < (d.U * pieces(lg) > most ? kMaxPiece : kMaxJoinPiece)) ++lg;
+  const bool direct = fits(pieces(lg));
   const int64_t n = pieces(lg), wgs = d.U * n;
-  const bool direct = n <= kMaxDirect && n * num_tokens * d.G <= kMaxDirectRows &&
-                      (wgs <= most || (n == 1 && wgs < ((int64_t)1 << 23)));
   a.nwg = direct ? (int)wgs : std::min(cap, d.U < kFewUnits ? device_cus() : held);
   a.chunks = direct ? (int)n : 0;
   a.piece = lg;

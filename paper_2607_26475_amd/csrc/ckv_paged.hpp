@@ -92,18 +92,21 @@ constexpr int kMaxPagedWgs = 1024;
 // go 127 -> 135).
 constexpr int kPagedWgsPerCu = 2, kFewUnits = 8;
 // The attention in one launch: at most so many pieces a unit (one wave's lanes
-// weigh them) and partial rows (its 4 waves load them).  8 units, one launch
-// against ranges and a join, us: 4 rows a unit, 256 positions 7.5 / 10.4, 4096
-// 9.6 / 12.5, 8192 14.4 / 17.4; 16 rows, 256 positions 9.9 / 10.9, 2048 12.5 /
-// 13.5, 8192 27.5 / 24.1; 1 unit of 16 rows, 2048 11.6 / 11.3, 4096 13.5 / 12.3.
+// weigh them) and partial rows (its 4 waves load them).  8 units, one launch of
+// single steps against ranges and a join, us: 4 rows a unit, 256 positions 7.5 /
+// 10.4, 4096 9.6 / 12.5, 8192 14.4 / 17.4; 16 rows, 256 positions 9.9 / 10.9, 2048
+// 12.5 / 13.5, 8192 27.5 / 24.1 (of 64 pieces, which the limits leave out).
 constexpr int kMaxDirect = 64, kMaxDirectRows = 256;
-// Where a step each would be more workgroups than the device holds, pieces of up
-// to 2^3 steps, or whole units that short, however many.  Against ranges, us: 64
-// e4m3 units of 2048 positions 18.1 -> 13.5, 512 bf16 units of 100 to 1000 38.1 ->
-// 29.8, 78 of 2397 28.1 -> 22.4, 8 of 32768 33.1 -> 29.7.  Pieces of 16 would give
-// a batch of even lengths up to 12 % more and cost one of 32 with a single long
-// sequence 20.1 -> 28.4.
-constexpr int kMaxPiece = 3;
+// Where steps are more than that, or than the workgroups that the device holds,
+// pieces of up to 2^3 steps, or whole units that short, however many.  Against
+// ranges, us: 64 e4m3 units of 2048 positions 18.1 -> 13.5, 512 bf16 units of 100
+// to 1000 38.1 -> 29.8, 78 of 2397 28.1 -> 22.4, 8 of 32768 33.1 -> 29.7.  Pieces
+// of 16 would give a batch of even lengths up to 12 % more and cost one of 32 with
+// a single long sequence 20.1 -> 28.4.  For the join's sake alone up to 2^2: 8
+// units of 8 rows and 8192 positions 17.9 -> 13.6, of 16 rows 20.1 -> 17.3; 2^3
+// would leave too much of the device idle (1 unit of 16 rows and 16384 positions
+// 18.3 -> 21.6, of 4 rows and 60000 19.0 -> 20.6).
+constexpr int kMaxPiece = 3, kMaxJoinPiece = 2;
 constexpr int kReadSlots = 32;              // slots of a reading workgroup
 
 struct PagedAttnArgs {

@@ -68,7 +68,7 @@ class Pool:
     ORDERS = ("heads", "rows", "pairs")  # [page][head][row], [page][row][head], K|V interleaved
 
     def __init__(self, lens, Hkv, page, kind, seed=0, order="heads", holes=(), spare=2,
-                 max_ctx=None, share=False):
+                 max_ctx=None, share=False, rows=None):
         g = torch.Generator().manual_seed(seed)
         dev = torch.device("cuda:0")
         self.lens = list(lens)
@@ -96,7 +96,7 @@ class Pool:
             (k, ke), (v, ve) = e4m3_64(k.double() * r), e4m3_64(v.double() / r)
             kd, vd = values(k, ke), values(v, ve)
         # what each request's positions hold, and which positions are there
-        pos = torch.arange(self.max_ctx)
+        pos = torch.arange(rows or self.max_ctx)   # (of long tables only the first)
         pg = table[:, pos // page].long()
         self.there = (pg >= 0) & (pos < torch.tensor(self.lens)[:, None])
         at = (pg.clamp(min=0), slice(None), (pos % page).expand(B, -1))
@@ -138,7 +138,7 @@ class Pool:
         for b in range(B):
             for t in range(T):
                 n = self.lens[b] - (T - 1 - t)
-                ok = self.there[b] & (torch.arange(self.max_ctx) < n)
+                ok = self.there[b] & (torch.arange(self.there.shape[1]) < n)
                 if not ok.any():
                     continue
                 for h in range(H):

@@ -427,6 +427,35 @@ def test_pieces_of_several_steps(kind, page, B, Hkv, G, T):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("kind,page", [("bf16", 16), ("e4m3", 64), ("bf16", 4)])
+@pytest.mark.parametrize("lens,G,T", [([4096, 1, 0, 511, 2049], 16, 1), ([8192, 3900], 4, 2),
+                                      ([9000], 4, 1)])
+def test_pieces_for_the_join(kind, page, lens, G, T):
+    """Few units whose steps are too many to be joined one by one."""
+    _log("pieces for the join", kind, page, lens, G, T)
+    pool = Pool(lens, 2, page, kind, seed=G, holes=[(0, 1), (0, 2)])
+    q, out, lse = _attend(pool, G, T)
+    _check_attention(pool, q, out, lse, T)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page,order,G,T", [
+    (1, "heads", 4, 1), (2, "rows", 2, 3), (8, "pairs", 8, 2), (16, "heads", 1, 1),
+    (16, "rows", 16, 1), (32, "pairs", 4, 4), (64, "heads", 8, 1), (128, "rows", 1, 16),
+    (1024, "heads", 2, 2)])
+def test_ranges_of_ragged_batches(kind, page, order, G, T):
+    """Short contexts in long tables, more units than pieces are made for: ranges
+    over requests and heads, pages missing, a join of their own."""
+    _log("ragged ranges", kind, page, order, G, T)
+    lens = [EDGES[i % 14] for i in range(24)] + [3000, 0, 1777, 128, 1, 2999]
+    per = lambda n: -(-n // page)  # noqa: E731
+    holes = [(24, s) for s in range(1, per(2000))] + [(26, s) for s in range(per(1600))] + \
+            [(11, s) for s in range(per(1000))] + [(3, 0), (29, per(2999) - 1)]
+    pool = Pool(lens, 2, page, kind, seed=G + T, order=order, holes=holes, max_ctx=40000, rows=3000)
+    q, out, lse = _attend(pool, G, T)
+    _check_attention(pool, q, out, lse, T)
+
+
 def test_shared_pages_and_no_lse():
     pool = Pool([100, 90], 2, 32, "bf16", seed=3, share=True)
     q, out, _ = _attend(pool, 4, 1, lse=False)
@@ -571,7 +600,7 @@ def test_captured_step_follows_growing_contexts():
 
 
 def test_kernel_classes_are_timed():
-    for lens, merges in (([300], 0), ([9000], 1)):   # one launch; ranges and their join
+    for lens, merges in (([300], 0), ([9000], 0), ([70000], 1)):  # one launch; ranges, their join
         pool = Pool(lens, 1, 16, "bf16")
         ckv.profile_begin(["paged_attn", "paged_merge"])
         _attend(pool, 1, 1)
