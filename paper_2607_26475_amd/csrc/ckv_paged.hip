@@ -1144,25 +1144,57 @@ __device__ __forceinline__ void tile_rest(Tile<E4M3>& t, bool masked, int p, int
   tile_output<E4M3>(t, part, st);
 }
 
+// Whether a step has no page at all (for the whole wave).
+__device__ __forceinline__ bool no_pages(const TileAt<true>& at) {
+  return (at.page[0] & at.page[1]) < 0;
+}
+
+__device__ __forceinline__ bool no_pages(const TileAt<false>& at) {
+  int all = -1;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) all &= at.v_page[j];
+  return !__any(all >= 0);
+}
+
 // The next step from `next` on that has a page, with its lookup.  Steps whose
-// whole pages are gone are passed over, 64 lookups at a time, so that a context's
-// time goes by what eviction left of it: 150000 to 200001 positions, of which the
-// first page and the last 1024 are kept, 98 -> 34 us (e4m3, two sequences); with
-// every page there the same.  The steps of small pages are all taken.
+// pages are all gone are passed over, 64 lookups at a time (of small pages 8
+// times 64 positions'), so that a context's time goes by what eviction left of it:
+// 150000 to 200001 positions, of which the first page and the last 1024 are kept,
+// 98 -> 34 us (e4m3, two sequences), with every page there the same; pages of 4
+// and 20000 to 32768 positions 139 -> 46 (bf16, 16 sequences), with every page there
+// 283 -> 294.  Called once the step's logits are taken, when the lookup has come.
 template <bool WIDE>
 __device__ __forceinline__ int with_pages(const PagedPages& pg, const Ctx& x, int next, int end,
                                           TileAt<WIDE>* at) {
-  if (WIDE)
-    while (next < end && (at->page[0] & at->page[1]) < 0) {  // 64 steps at a time
-      const int p = next + (int)(threadIdx.x & 63) * kPagedStep;
-      const int last = min(end, x.n) - 1;
+  while (next < end && no_pages(*at)) {
+    const int lane = threadIdx.x & 63;
+    int skip;
+    if (WIDE) {
+      const int p = next + lane * kPagedStep;
       bool any = false;
-      if (p <= last)
-        any = page_at(pg, x, p) >= 0 || page_at(pg, x, min(p + 16, x.n - 1)) >= 0;
+      if (p < end) any = page_at(pg, x, p) >= 0 || page_at(pg, x, min(p + 16, x.n - 1)) >= 0;
       const uint64_t mask = __ballot(any) & ~1ull;  // `next` itself has none
-      next += (mask ? __builtin_ctzll(mask) : 64) * kPagedStep;
-      *at = tile_at<WIDE>(pg, x, min(next, end - 1));
+      skip = mask ? __builtin_ctzll(mask) : 64;
+    } else {
+      int page[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {  // steps 2j and 2j + 1, a lane a position
+        const int p = next + (2 * j + (lane >> 5)) * kPagedStep + (lane & 31);
+        page[j] = page_at(pg, x, min(p, end - 1));
+        if (p >= end) page[j] = -1;
+      }
+      uint32_t mask = 0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint64_t any = __ballot(page[j] >= 0);
+        mask |= (uint32_t)((uint32_t)any != 0) << 2 * j | (uint32_t)(any >> 32 != 0) << (2 * j + 1);
+      }
+      mask &= ~1u;
+      skip = mask ? __builtin_ctz(mask) : 16;
     }
+    next += skip * kPagedStep;
+    *at = tile_at<WIDE>(pg, x, min(next, end - 1));
+  }
   return next;
 }
 
@@ -1184,21 +1216,20 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
   load_v<E4M3, WIDE>(pg, x, at, t);
   int next = p + kPagedStep;
   at = tile_at<WIDE>(pg, x, min(next, end - 1));
-  next = with_pages<WIDE>(pg, x, next, end, &at);
   while (next < end) {
     tile_logits<E4M3, WIDE>(t, q, lg);
+    next = with_pages<WIDE>(pg, x, next, end, &at);  // from end on: rows that nobody uses
     load_k<E4M3, WIDE>(pg, x, at, t);
     __builtin_amdgcn_sched_barrier(0);
-    TileAt<WIDE> then = at;
-    if (WIDE) then = tile_at<WIDE>(pg, x, min(next + kPagedStep, end - 1));
     const bool masked = WIDE ? t.there != 255u : __any(t.there != 255u);
     tile_rest<E4M3>(t, masked, p, limit, c, lg, st);
     __builtin_amdgcn_sched_barrier(0);
     load_v<E4M3, WIDE>(pg, x, at, t);
     p = next;
-    at = WIDE ? then : tile_at<WIDE>(pg, x, min(next + kPagedStep, end - 1));
-    next = with_pages<WIDE>(pg, x, next + kPagedStep, end, &at);
+    next += kPagedStep;
+    at = tile_at<WIDE>(pg, x, min(next, end - 1));
   }
+  if (p >= end) return;
   tile_logits<E4M3, WIDE>(t, q, lg);
   tile_rest<E4M3>(t, true, p, limit, c, lg, st);
 }
