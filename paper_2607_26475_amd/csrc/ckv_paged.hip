@@ -756,9 +756,9 @@ __device__ __forceinline__ void load_score_step(const PagedPages& pg, const Ctx&
   for (int i = 0; i < 4; ++i) {
     const bool has = (unsigned)t.row[i] < (unsigned)pg.num_pages;
     if (WIDE) {
-      const int first = min(p + 16 * i, (x.n - 1) & ~15);
+      const int first = half_first(p, i, x.n);
       const uint8_t* base = pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, first);
-      const int32_t cap = min(x.n - 1 - first, 15) * pg.row_bytes;
+      const int32_t cap = half_last(first, x.n) * pg.row_bytes;
       s.k[i].load_lines(base, pg.row_bytes, cap, g, r);
     } else {
       s.k[i].load(pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, min(p + 16 * i + r, x.n - 1)),
@@ -822,7 +822,7 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
       ScoreStep<E4M3> s;
       ScorePages<WIDE> pages = score_pages<WIDE>(a.pg, x, p);
       load_score_step<E4M3, WIDE>(a.pg, x, p, pages, s);
-      pages = score_pages<WIDE>(a.pg, x, min(p + kScoreStep, stop - 1) & ~15);
+      pages = score_pages<WIDE>(a.pg, x, lookup_at(p + kScoreStep, stop));
       bf16x8 q[4];
 #pragma unroll
       for (int f = 0; f < 4; ++f)
@@ -840,7 +840,7 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
         }
         if (!more) break;
         load_score_step<E4M3, WIDE>(a.pg, x, p, pages, s);
-        pages = score_pages<WIDE>(a.pg, x, min(p + kScoreStep, stop - 1) & ~15);
+        pages = score_pages<WIDE>(a.pg, x, lookup_at(p + kScoreStep, stop));
       }
     }
     at += take;
@@ -936,10 +936,10 @@ __device__ __forceinline__ TileAt<WIDE> tile_at(const PagedPages& pg, const Ctx&
   TileAt<WIDE> t;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    t.first[i] = min(p0 + 16 * i, (x.n - 1) & ~15);
+    t.first[i] = half_first(p0, i, x.n);
     if (WIDE) {
       t.page[i] = page_at(pg, x, t.first[i]);
-      t.cap[i] = min(x.n - 1 - t.first[i], 15) * pg.row_bytes;
+      t.cap[i] = half_last(t.first[i], x.n) * pg.row_bytes;
     } else {
       t.page[i] = page_at(pg, x, min(t.first[i] + r, x.n - 1));
 #pragma unroll
@@ -1193,7 +1193,7 @@ __device__ __forceinline__ int with_pages(const PagedPages& pg, const Ctx& x, in
       skip = mask ? __builtin_ctz(mask) : 16;
     }
     next += skip * kPagedStep;
-    *at = tile_at<WIDE>(pg, x, min(next, end - 1));
+    *at = tile_at<WIDE>(pg, x, lookup_at(next, end));
   }
   return next;
 }
@@ -1215,7 +1215,7 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
   load_k<E4M3, WIDE>(pg, x, at, t);
   load_v<E4M3, WIDE>(pg, x, at, t);
   int next = p + kPagedStep;
-  at = tile_at<WIDE>(pg, x, min(next, end - 1));
+  at = tile_at<WIDE>(pg, x, lookup_at(next, end));
   while (next < end) {
     tile_logits<E4M3, WIDE>(t, q, lg);
     next = with_pages<WIDE>(pg, x, next, end, &at);  // from end on: rows that nobody uses
@@ -1227,7 +1227,7 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
     load_v<E4M3, WIDE>(pg, x, at, t);
     p = next;
     next += kPagedStep;
-    at = tile_at<WIDE>(pg, x, min(next, end - 1));
+    at = tile_at<WIDE>(pg, x, lookup_at(next, end));
   }
   if (p >= end) return;
   tile_logits<E4M3, WIDE>(t, q, lg);

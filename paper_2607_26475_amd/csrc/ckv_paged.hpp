@@ -109,6 +109,28 @@ constexpr int kMaxDirect = 64, kMaxDirectRows = 256;
 constexpr int kMaxPiece = 3, kMaxJoinPiece = 2;
 constexpr int kReadSlots = 32;              // slots of a reading workgroup
 
+// A wave's step is two halves of 16 positions.  First position of half i of the
+// step at p0 in a context of n positions: its own, or that of the last 16 where
+// the half is past the context's end.  p0 is a multiple of 16, and so is the
+// result: a half's rows never leave a page of 16 or more.
+__host__ __device__ inline int half_first(int p0, int i, int n) {
+  const int own = p0 + 16 * i, last = (n - 1) & ~15;
+  return own < last ? own : last;
+}
+
+// A half's last row, counted from its first.
+__host__ __device__ inline int half_last(int first, int n) {
+  return n - 1 - first < 15 ? n - 1 - first : 15;
+}
+
+// Where a wave whose next step is at `next` looks and loads: there or, once that
+// is past the piece's end, at the piece's last 16 positions (rows that nobody
+// uses).  A multiple of 16 whatever `end` is.
+__host__ __device__ inline int lookup_at(int next, int end) {
+  const int last = (end - 1) & ~15;
+  return next < last ? next : last;
+}
+
 struct PagedAttnArgs {
   PagedPages pg;
   const uint16_t* q;       // [B][T][Hq][d]
