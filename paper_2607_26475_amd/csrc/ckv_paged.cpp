@@ -153,6 +153,7 @@ int debug_check_paged(hipStream_t s, const PagedPages& pg, const int32_t* ctx_le
   a.B = B;
   a.max_ctx = max_ctx;
   a.tokens = tokens;
+  a.slots = (int32_t)(((int64_t)max_ctx + (1 << pg.shift) - 1) >> pg.shift);
   unsigned long long got = 0;
   if ((e = launch_fill(a.flag, 16, 0xffffffffu, s)) != hipSuccess ||
       (e = launch_paged_check(a, s)) != hipSuccess ||
@@ -164,7 +165,7 @@ int debug_check_paged(hipStream_t s, const PagedPages& pg, const int32_t* ctx_le
   const long long item = (long long)(got & ((1ull << 56) - 1));
   if (kind == 4)
     return fail(CKV_EINVAL, "debug check: page_table[%lld][%lld] is neither -1 nor below %d",
-                item / pg.table_stride, item % pg.table_stride, pg.num_pages);
+                item / a.slots, item % a.slots, pg.num_pages);
   if (kind == 5)
     return fail(CKV_EINVAL, "debug check: positions[%lld] is neither -1 nor in [0, %d)", item,
                 max_ctx);

@@ -294,12 +294,6 @@ __global__ __launch_bounds__(kRopeThreads) void k_rope(RopeArgs a, int per) {
 typedef const __attribute__((address_space(4))) int32_t* TablePtr;
 
 // ---- writing -----------------------------------------------------------------------
-// Row of position pos in its page, or a page of -1 where it is not there.
-__device__ __forceinline__ int page_of(const PagedPages& pg, int b, int pos) {
-  const int page = pg.table[(int64_t)b * pg.table_stride + (pos >> pg.shift)];
-  return (unsigned)page < (unsigned)pg.num_pages ? page : -1;
-}
-
 __device__ __forceinline__ int64_t row_offset(const PagedPages& pg, int page, int h, int pos) {
   const int row = pos & ((1 << pg.shift) - 1);
   return page * pg.page_bytes + h * pg.head_bytes + (int64_t)row * pg.row_bytes;
@@ -1611,22 +1605,9 @@ __global__ __launch_bounds__(kPagedMergeThreads) void k_paged_merge(PagedAttnArg
 // ---- debug mode ------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void k_paged_check(PagedCheckArgs a) {
   const int64_t stride = (int64_t)gridDim.x * blockDim.x;
-  const int64_t total = a.ctx_lens ? (int64_t)a.B * a.pg.table_stride : a.tokens;
+  const int64_t total = paged_check_items(a);
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < total; i += stride) {
-    unsigned long long kind = 0;
-    if (a.ctx_lens) {
-      const int b = (int)(i / a.pg.table_stride), s = (int)(i - (int64_t)b * a.pg.table_stride);
-      const int n = clamp_len(a.ctx_lens[b], a.max_ctx);
-      const int page = a.pg.table[i];
-      if (((int64_t)s << a.pg.shift) < n && page != -1 &&
-          (unsigned)page >= (unsigned)a.pg.num_pages)
-        kind = 4;
-    } else if (a.pos[i] != -1) {
-      const int b = a.req ? a.req[i] : (int)i;
-      if ((unsigned)a.pos[i] >= (unsigned)a.max_ctx) kind = 5;
-      else if ((unsigned)b >= (unsigned)a.B) kind = 6;
-      else if (page_of(a.pg, b, a.pos[i]) < 0) kind = 7;
-    }
+    const unsigned long long kind = paged_check_item(a, i);
     if (kind) atomicMin(a.flag, kind << 56 | (unsigned long long)i);
   }
 }
@@ -1735,7 +1716,7 @@ hipError_t launch_paged_attn(const PagedAttnArgs& a, bool e4m3, hipStream_t s) {
 }
 
 hipError_t launch_paged_check(const PagedCheckArgs& a, hipStream_t s) {
-  const int64_t total = a.ctx_lens ? (int64_t)a.B * a.pg.table_stride : a.tokens;
+  const int64_t total = paged_check_items(a);
   hipLaunchKernelGGL(k_paged_check, dim3(grid_for(total, 256, 4096)), dim3(256), 0, s, a);
   return hipGetLastError();
 }

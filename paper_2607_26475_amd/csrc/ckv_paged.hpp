@@ -148,8 +148,15 @@ struct PagedAttnArgs {
   int32_t piece;           // direct: a piece has 2^piece steps
 };
 
+// Page of position pos of request b, or -1 where it is not there.
+__host__ __device__ inline int page_of(const PagedPages& pg, int b, int pos) {
+  const int page = pg.table[(int64_t)b * pg.table_stride + (pos >> pg.shift)];
+  return (unsigned)page < (unsigned)pg.num_pages ? page : -1;
+}
+
 // Debug mode's checks of paged inputs (CheckArgs' codes go on: 4 page_table
-// entry, 5 positions[t], 6 requests[t], 7 the page of a written token).
+// entry b * slots + s, 5 positions[t], 6 requests[t], 7 the page of a written
+// token).
 struct PagedCheckArgs {
   PagedPages pg;
   const int32_t* ctx_lens; // reading entries
@@ -157,7 +164,30 @@ struct PagedCheckArgs {
   const int32_t* pos;
   unsigned long long* flag;
   int32_t B, max_ctx, tokens;
+  int32_t slots;           // table entries of max_ctx positions
 };
+
+__host__ __device__ inline int64_t paged_check_items(const PagedCheckArgs& a) {
+  return a.ctx_lens ? (int64_t)a.B * a.slots : a.tokens;
+}
+
+// What is wrong with item i (0: nothing).  Table entries past a context's end are
+// not looked at: a table may be some columns of a wider one, whose last row ends
+// before table_stride entries.
+__host__ __device__ inline unsigned paged_check_item(const PagedCheckArgs& a, int64_t i) {
+  if (a.ctx_lens) {
+    const int b = (int)(i / a.slots), s = (int)(i - (int64_t)b * a.slots);
+    const int len = a.ctx_lens[b], n = len < a.max_ctx ? len : a.max_ctx;
+    if (((int64_t)s << a.pg.shift) >= n) return 0;
+    const int page = a.pg.table[(int64_t)b * a.pg.table_stride + s];
+    return page != -1 && (unsigned)page >= (unsigned)a.pg.num_pages ? 4 : 0;
+  }
+  if (a.pos[i] == -1) return 0;
+  const int b = a.req ? a.req[i] : (int)i;
+  if ((unsigned)a.pos[i] >= (unsigned)a.max_ctx) return 5;
+  if ((unsigned)b >= (unsigned)a.B) return 6;
+  return page_of(a.pg, b, a.pos[i]) < 0 ? 7 : 0;
+}
 
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
 hipError_t launch_paged_write(const PagedWriteArgs& a, bool e4m3, hipStream_t s);

@@ -1,6 +1,10 @@
 // C entries to the paged cache's index arithmetic, for the tests without a GPU.
 #include "ckv_paged.hpp"
 
+#include <sys/mman.h>
+
+#include <cstring>
+
 namespace {
 
 // Whether any of the step's pages is there (`there`: of each table entry).
@@ -33,6 +37,33 @@ int t_attn_halves(int n, int shift, const uint8_t* there, int step, int take, in
     next += ckv::kPagedStep;
   }
   return count;
+}
+// Debug mode's check of a reading call whose table is the columns from `col` on
+// of [B][stride] entries that end where readable memory ends: the smallest
+// finding (kind << 56 | item, all ones: none).
+uint64_t t_check_table(int B, int max_ctx, int shift, int num_pages, const int32_t* lens,
+                       const int32_t* wide, int stride, int col, int* slots) {
+  const size_t bytes = (size_t)B * stride * 4, guard = 1 << 16;
+  const size_t room = (bytes + guard - 1) / guard * guard;
+  char* m = static_cast<char*>(mmap(nullptr, room + guard, PROT_READ | PROT_WRITE,
+                                    MAP_PRIVATE | MAP_ANONYMOUS, -1, 0));
+  if (m == MAP_FAILED || mprotect(m + room, guard, PROT_NONE)) return 0;
+  int32_t* t = reinterpret_cast<int32_t*>(m + room - bytes);
+  std::memcpy(t, wide, bytes);
+  ckv::PagedCheckArgs a = {};
+  a.pg.table = t + col;
+  a.pg.shift = shift;
+  a.pg.num_pages = num_pages;
+  a.pg.table_stride = stride;
+  a.ctx_lens = lens;
+  a.B = B;
+  a.max_ctx = max_ctx;
+  a.slots = *slots = (max_ctx + (1 << shift) - 1) >> shift;
+  uint64_t got = ~0ull;
+  for (int64_t i = 0; i < ckv::paged_check_items(a); ++i)
+    if (const uint64_t kind = ckv::paged_check_item(a, i)) got = std::min(got, kind << 56 | i);
+  munmap(m, room + guard);
+  return got;
 }
 int t_half_last(int first, int n) { return ckv::half_last(first, n); }
 }

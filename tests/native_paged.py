@@ -31,4 +31,6 @@ def lib() -> ctypes.CDLL:
         capture_output=True, text=True, timeout=300)
     assert r.returncode == 0, r.stderr[-3000:]
     os.replace(tmp, out)
-    return ctypes.CDLL(out)
+    so = ctypes.CDLL(out)
+    so.t_check_table.restype = ctypes.c_uint64
+    return so

@@ -3,10 +3,14 @@ from __future__ import annotations
 
 import ctypes
 
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 
-from native_paged import lib
+from native_paged import HERE, lib
 
 
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
@@ -34,3 +38,35 @@ def test_loaded_halves_stay_in_their_pages(page, n):
                         last = f + so.t_half_last(f, n)
                         assert f % 16 == 0 and 0 <= f <= last < n, (f, last)
                         assert f // page == last // page, (f, last)
+
+
+def check_table(lens, max_ctx, page, wide, col, num_pages=8):
+    """Debug mode's finding about columns col .. of `wide`: None or (kind, request,
+    entry)."""
+    lens, wide = np.asarray(lens, np.int32), np.ascontiguousarray(wide, np.int32)
+    slots = ctypes.c_int()
+    got = lib().t_check_table(len(lens), max_ctx, page.bit_length() - 1, num_pages,
+                              lens.ctypes.data_as(ctypes.c_void_p),
+                              wide.ctypes.data_as(ctypes.c_void_p), wide.shape[1], col,
+                              ctypes.byref(slots))
+    if got == 2 ** 64 - 1:
+        return None
+    item = got & (2 ** 56 - 1)
+    return got >> 56, item // slots.value, item % slots.value
+
+
+def test_checked_table_entries_belong_to_positions():
+    """Columns of a wider table whose last row ends where memory ends: no entry
+    past the columns is read, and only those of positions are judged."""
+    code = ("import numpy as np, test_paged_math as t\n"
+            "w = np.full((3, 11), 99); w[:, 6:] = 3\n"
+            "assert t.check_table([80, 0, 65], 80, 16, w, 6) is None\n"
+            "w[2, 8] = 8\n"
+            "assert t.check_table([80, 0, 65], 80, 16, w, 6) == (4, 2, 2)\n"
+            "assert t.check_table([80, 0, 32], 80, 16, w, 6) is None\n"
+            "w[0, 10] = -2\n"
+            "assert t.check_table([80, 0, 65], 80, 16, w, 6) == (4, 0, 4)\n"
+            "assert t.check_table([64, -5, 32], 80, 16, w, 6) is None\n")
+    r = subprocess.run([sys.executable, "-c", code], cwd=HERE, capture_output=True, text=True,
+                       env=dict(os.environ, PYTHONPATH=os.path.dirname(HERE)), timeout=120)
+    assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
