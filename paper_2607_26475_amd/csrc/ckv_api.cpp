@@ -6,7 +6,6 @@
 #include <atomic>
 #include <cstdarg>
 #include <cstdio>
-#include <mutex>
 #include <string>
 
 #include "ckv.h"
@@ -40,33 +39,23 @@ const char* last_detail() { return g_detail.c_str(); }
 int debug_check(hipStream_t s, const int32_t* ctx_lens, const int32_t* idx,
                 const int32_t* n_sel, int B, int Hkv, int max_ctx, int k) {
   if (!debug_on() || B == 0 || (!ctx_lens && !idx && !n_sel)) return CKV_OK;
-  // one 16-byte flag per device, kept until the process ends (debug mode only)
-  static std::mutex mu;
-  static unsigned long long* flags[256] = {};
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_fail(e, "debug check");
-  if (dev < 0 || dev >= 256) return fail(CKV_EUNSUPPORTED, "device %d", dev);
-  {
-    std::lock_guard<std::mutex> lk(mu);
-    if (!flags[dev] && (e = hipMalloc(&flags[dev], 16)) != hipSuccess)
-      return hip_fail(e, "debug check flag");
-  }
   CheckArgs a;
   a.ctx_lens = ctx_lens;
   a.idx = idx;
   a.n_sel = n_sel;
-  a.flag = flags[dev];
   a.B = B;
   a.Hkv = Hkv;
   a.max_ctx = max_ctx;
   a.k = k;
   unsigned long long got = 0;
-  if ((e = launch_fill(a.flag, 16, 0xffffffffu, s)) != hipSuccess ||
-      (e = launch_check(a, s)) != hipSuccess ||
-      (e = hipMemcpyAsync(&got, a.flag, 8, hipMemcpyDeviceToHost, s)) != hipSuccess ||
-      (e = hipStreamSynchronize(s)) != hipSuccess)
-    return hip_fail(e, "debug check");
+  const int rc = debug_run(
+      s,
+      [&](unsigned long long* flag) {
+        a.flag = flag;
+        return launch_check(a, s);
+      },
+      &got);
+  if (rc) return rc;
   if (got == ~0ull) return CKV_OK;
   const unsigned kind = (unsigned)(got >> 40);
   const long long item = (long long)(got & ((1ull << 40) - 1));

@@ -4,6 +4,8 @@
 #include <hip/hip_runtime.h>
 
 #include <atomic>
+#include <mutex>
+#include <new>
 
 #include "ckv.h"
 #include "ckv_launch.hpp"
@@ -83,6 +85,67 @@ inline uint64_t next_fused_tag() {
   t *= 2654435761u;  // spread consecutive calls over the 32 bits
   t |= 1u;
   return ((uint64_t)t << 32) | (uint32_t)~t;
+}
+
+// Words that are each held by one call at a time and kept until the process ends.
+class FlagPool {
+ public:
+  struct Flag {
+    unsigned long long* word;
+    Flag* next;
+  };
+  // A free flag, or a new one whose word make(&word) gives (true: it did); NULL if
+  // there is none to be had.
+  template <class Make>
+  Flag* take(Make make) {
+    {
+      std::lock_guard<std::mutex> lk(mu_);
+      if (Flag* f = free_) {
+        free_ = f->next;
+        return f;
+      }
+    }
+    Flag* f = new (std::nothrow) Flag{nullptr, nullptr};
+    if (f && !make(&f->word)) {
+      delete f;
+      f = nullptr;
+    }
+    return f;
+  }
+  void give(Flag* f) {
+    std::lock_guard<std::mutex> lk(mu_);
+    f->next = free_;
+    free_ = f;
+  }
+
+ private:
+  std::mutex mu_;
+  Flag* free_ = nullptr;
+};
+
+// Debug mode: runs launch(flag) on the stream, a check that leaves the smallest code
+// of what it finds in *flag (all ones: nothing), and waits for it.  The flag is
+// this call's own, so that calls of other threads and streams do not meet; one
+// whose call failed is not used again (the device may still write it).
+template <class Launch>
+inline int debug_run(hipStream_t s, Launch launch, unsigned long long* got) {
+  static FlagPool pools[256];
+  int dev = 0;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return hip_fail(e, "debug check");
+  if (dev < 0 || dev >= 256) return fail(CKV_EUNSUPPORTED, "device %d", dev);
+  FlagPool::Flag* f = pools[dev].take([&](unsigned long long** word) {
+    e = hipMalloc(word, 16);
+    return e == hipSuccess;
+  });
+  if (!f) return hip_fail(e != hipSuccess ? e : hipErrorOutOfMemory, "debug check flag");
+  if ((e = launch_fill(f->word, 16, 0xffffffffu, s)) != hipSuccess ||
+      (e = launch(f->word)) != hipSuccess ||
+      (e = hipMemcpyAsync(got, f->word, 8, hipMemcpyDeviceToHost, s)) != hipSuccess ||
+      (e = hipStreamSynchronize(s)) != hipSuccess)
+    return hip_fail(e, "debug check");
+  pools[dev].give(f);
+  return CKV_OK;
 }
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }

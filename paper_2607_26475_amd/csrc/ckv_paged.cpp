@@ -3,7 +3,6 @@
 #include "ckv_paged.hpp"
 
 #include <cmath>
-#include <mutex>
 
 #include "ckv_profile.hpp"
 
@@ -133,33 +132,24 @@ int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p) {
 int debug_check_paged(hipStream_t s, const PagedPages& pg, const int32_t* ctx_lens,
                       const int32_t* req, const int32_t* pos, int B, int max_ctx, int tokens) {
   if (!debug_on()) return CKV_OK;
-  static std::mutex mu;  // one 16-byte flag per device, kept until the process ends
-  static unsigned long long* flags[256] = {};
-  int dev = 0;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return hip_fail(e, "debug check");
-  if (dev < 0 || dev >= 256) return fail(CKV_EUNSUPPORTED, "device %d", dev);
-  {
-    std::lock_guard<std::mutex> lk(mu);
-    if (!flags[dev] && (e = hipMalloc(&flags[dev], 16)) != hipSuccess)
-      return hip_fail(e, "debug check flag");
-  }
   PagedCheckArgs a;
   a.pg = pg;
   a.ctx_lens = ctx_lens;
   a.req = req;
   a.pos = pos;
-  a.flag = flags[dev];
   a.B = B;
   a.max_ctx = max_ctx;
   a.tokens = tokens;
   a.slots = (int32_t)(((int64_t)max_ctx + (1 << pg.shift) - 1) >> pg.shift);
   unsigned long long got = 0;
-  if ((e = launch_fill(a.flag, 16, 0xffffffffu, s)) != hipSuccess ||
-      (e = launch_paged_check(a, s)) != hipSuccess ||
-      (e = hipMemcpyAsync(&got, a.flag, 8, hipMemcpyDeviceToHost, s)) != hipSuccess ||
-      (e = hipStreamSynchronize(s)) != hipSuccess)
-    return hip_fail(e, "debug check");
+  const int rc = debug_run(
+      s,
+      [&](unsigned long long* flag) {
+        a.flag = flag;
+        return launch_paged_check(a, s);
+      },
+      &got);
+  if (rc) return rc;
   if (got == ~0ull) return CKV_OK;
   const unsigned kind = (unsigned)(got >> 56);
   const long long item = (long long)(got & ((1ull << 56) - 1));

@@ -3,7 +3,10 @@
 
 #include <sys/mman.h>
 
+#include <atomic>
 #include <cstring>
+#include <thread>
+#include <vector>
 
 namespace {
 
@@ -64,6 +67,33 @@ uint64_t t_check_table(int B, int max_ctx, int shift, int num_pages, const int32
     if (const uint64_t kind = ckv::paged_check_item(a, i)) got = std::min(got, kind << 56 | i);
   munmap(m, room + guard);
   return got;
+}
+// Threads that take and give debug mode's flags: times that one was found in use,
+// and (flags) how many there were.
+int t_flag_pool(int threads, int rounds, int* flags) {
+  ckv::FlagPool pool;
+  std::atomic<unsigned long long> words[256] = {};
+  std::atomic<int> made{0}, met{0};
+  std::vector<std::thread> all;
+  for (int t = 0; t < threads; ++t)
+    all.emplace_back([&] {
+      for (int i = 0; i < rounds; ++i) {
+        ckv::FlagPool::Flag* f = pool.take([&](unsigned long long** word) {
+          const int n = made.fetch_add(1);
+          *word = reinterpret_cast<unsigned long long*>(&words[n < 256 ? n : 255]);
+          return n < 256;
+        });
+        if (!f) continue;
+        auto* w = reinterpret_cast<std::atomic<unsigned long long>*>(f->word);
+        if (w->exchange(1)) met.fetch_add(1);
+        std::this_thread::yield();
+        w->store(0);
+        pool.give(f);
+      }
+    });
+  for (std::thread& t : all) t.join();
+  *flags = made.load();
+  return met.load();
 }
 int t_half_last(int first, int n) { return ckv::half_last(first, n); }
 }

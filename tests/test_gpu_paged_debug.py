@@ -1,6 +1,8 @@
 """Debug mode's checks of the paged cache (MI355X only)."""
 from __future__ import annotations
 
+import threading
+
 import pytest
 import torch
 
@@ -39,3 +41,36 @@ def test_debug_mode_over_columns_of_a_wider_table(debug_mode):
     with pytest.raises(ckv.CkvError) as e:
         ckv.paged_score_keys(s, cache, q, pool.ctx, SCALE, a)
     assert e.value.status == 1 and "page_table[2][4]" in str(e.value)
+
+
+def test_debug_findings_of_two_threads_stay_apart(debug_mode):
+    """Threads with a stream each, one of whose tables is bad: each call's finding
+    is its own."""
+    pools = [Pool([90, 40], 1, 16, "bf16", seed=i) for i in range(3)]
+    pools[0].table[1, 2] = 999
+    pools[0].ctx[1] = 48
+    pools[1].ctx[1] = 91            # of the dense entries' check
+    s = pools[0].shape(2)
+    q = torch.randn((2, 2, D), device=DEV).to(torch.bfloat16)
+    scores = [torch.empty((2, 1, 90), device=DEV) for _ in pools]
+    torch.cuda.synchronize()
+    found = [[] for _ in pools]
+
+    def run(i):
+        stream = torch.cuda.Stream()
+        for _ in range(150):
+            try:
+                ckv.paged_score_keys(s, pools[i].cache, q, pools[i].ctx, SCALE, scores[i],
+                                     stream=stream)
+                found[i].append("")
+            except ckv.CkvError as e:
+                found[i].append(str(e))
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(3)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all("page_table[1][2]" in f for f in found[0])
+    assert all("ctx_lens[1]" in f for f in found[1])
+    assert all(f == "" for f in found[2]) and all(len(f) == 150 for f in found)

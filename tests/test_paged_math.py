@@ -70,3 +70,9 @@ def test_checked_table_entries_belong_to_positions():
     r = subprocess.run([sys.executable, "-c", code], cwd=HERE, capture_output=True, text=True,
                        env=dict(os.environ, PYTHONPATH=os.path.dirname(HERE)), timeout=120)
     assert r.returncode == 0, (r.returncode, r.stderr[-2000:])
+
+
+def test_debug_flags_are_held_by_one_call():
+    flags = ctypes.c_int()
+    assert lib().t_flag_pool(8, 2000, ctypes.byref(flags)) == 0
+    assert 1 <= flags.value <= 8
