@@ -1450,16 +1450,30 @@ __device__ __forceinline__ void join_steps(const PagedAttnArgs& a, int b, int h,
 
 // The same with a workgroup for every piece of 2^piece steps of every unit
 // (workgroup unit * chunks + piece) and the join inside the launch, for few
-// steps: each hands its partial over through its flag, which takes the launch's
-// tag once the partial's device-coherent stores are done; the workgroup of the
-// unit's last piece waits for the flags, clears them and joins.  Only
-// higher-numbered workgroups wait, for lower-numbered ones that never do, and the
-// wait is bounded all the same: one that ends without its flags (lower-numbered
-// workgroups kept from the device for that long) leaves NaN.  8 units of 2001
-// positions: 7.6 us, against 10.4 with ranges and a second launch; a chain of
+// steps: each hands its partial over through its flag, once the partial's
+// device-coherent stores are done; the workgroup of the unit's last piece waits
+// for the flags, which are clear again after the launch, and joins.  Of one
+// launch only higher-numbered workgroups wait, for lower-numbered ones that
+// never do; should several launches keep each other's off the device, the bound
+// ends the wait, and that call's outputs of the unit are NaN.  8 units of 2001
+// positions: 7.7 us, against 10.4 with ranges and a second launch; a chain of
 // latencies (length, page, rows, hand-over, join), which 8 MB of rows hardly
 // lengthen.
 constexpr uint32_t kJoinSpinLimit = 1u << 24;  // about 20 s
+
+struct JoinFlag {
+  uint64_t* f;
+  __device__ __forceinline__ uint64_t load() const {
+    return __hip_atomic_load(f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ void store(uint64_t x) const {
+    __hip_atomic_store(f, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ uint64_t exchange(uint64_t x) const {
+    return __hip_atomic_exchange(f, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  __device__ __forceinline__ void pause() const { __builtin_amdgcn_s_sleep(2); }
+};
 
 template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(PagedAttnArgs a) {
@@ -1505,22 +1519,12 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
   if (!last) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0)
-      __hip_atomic_store(a.flags + blockIdx.x, a.tag, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) hand_over(JoinFlag{a.flags + blockIdx.x}, a.tag);
     return;
   }
   bool late = false;
-  if (tid < pieces - 1) {
-    uint64_t* f = a.flags + (int64_t)unit * a.chunks + tid;
-    uint32_t spin = 0;
-    while (__hip_atomic_load(f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != a.tag &&
-           spin < kJoinSpinLimit) {
-      __builtin_amdgcn_s_sleep(2);
-      ++spin;
-    }
-    late = spin == kJoinSpinLimit;
-    __hip_atomic_store(f, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
+  if (tid < pieces - 1)
+    late = !take_over(JoinFlag{a.flags + (int64_t)unit * a.chunks + tid}, a.tag, kJoinSpinLimit);
   if (__syncthreads_or(late) && tid < rows) lds.jl[tid] = NAN;  // every output of the unit
   __syncthreads();
   if (rows <= 4) join_steps<1>(a, b, h, pieces, part, lds);

@@ -148,6 +148,31 @@ struct PagedAttnArgs {
   int32_t piece;           // direct: a piece has 2^piece steps
 };
 
+// The hand-over of a partial in the one-launch attention: a flag (any word at
+// first) that the partial's workgroup sets to the launch's tag, and that the
+// joining one waits for, `limit` polls at most.  Whoever comes second clears it,
+// also where the wait was given up, so it is always zero after the launch: a
+// captured launch has the same tag in every replay, and a flag left over would
+// pass the replay before's partial off as this one's.  Flag has load, store,
+// exchange (relaxed: what is handed over is made visible before) and pause.
+template <class Flag>
+__host__ __device__ inline void hand_over(Flag f, uint64_t tag) {
+  if (f.exchange(tag) == ~tag) f.store(0);  // given up: nobody else looks at it
+}
+
+template <class Flag>
+__host__ __device__ inline bool take_over(Flag f, uint64_t tag, uint32_t limit) {
+  for (uint32_t spin = 0; f.load() != tag; ++spin) {
+    if (spin == limit) {
+      if (f.exchange(~tag) == tag) break;  // it came after all
+      return false;
+    }
+    f.pause();
+  }
+  f.store(0);
+  return true;
+}
+
 // Page of position pos of request b, or -1 where it is not there.
 __host__ __device__ inline int page_of(const PagedPages& pg, int b, int pos) {
   const int page = pg.table[(int64_t)b * pg.table_stride + (pos >> pg.shift)];

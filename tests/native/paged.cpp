@@ -4,7 +4,9 @@
 #include <sys/mman.h>
 
 #include <atomic>
+#include <condition_variable>
 #include <cstring>
+#include <mutex>
 #include <thread>
 #include <vector>
 
@@ -15,9 +17,77 @@ bool has_pages(const uint8_t* there, int shift, int p, int n) {
   return there[ckv::half_first(p, 0, n) >> shift] || there[ckv::half_first(p, 1, n) >> shift];
 }
 
+// A flag whose two users take turns as `turns` says, an access at a time (bit i:
+// the joining one has the i-th; who is alone goes on).
+struct Turns {
+  uint64_t word;
+  uint32_t turns;
+  int at = 0;
+  bool ended[2] = {false, false}, given = false;
+  std::mutex mu = {};
+  std::condition_variable cv = {};
+};
+
+struct TurnFlag {
+  Turns* t;
+  int me;
+  template <class Access>
+  uint64_t access(Access a) const {
+    std::unique_lock<std::mutex> lk(t->mu);
+    t->cv.wait(lk, [&] { return t->ended[1 - me] || (int)(t->turns >> t->at & 1u) == me; });
+    const uint64_t was = a();
+    t->at = std::min(t->at + 1, 31);
+    t->cv.notify_all();
+    return was;
+  }
+  uint64_t load() const {
+    return access([&] { return t->word; });
+  }
+  void store(uint64_t x) const {
+    access([&] { return t->word = x; });
+  }
+  uint64_t exchange(uint64_t x) const {
+    return access([&] {
+      const uint64_t was = t->word;
+      t->word = x;
+      if (me == 0) t->given = true;
+      return was;
+    });
+  }
+  void pause() const {}
+  void end() const {
+    std::lock_guard<std::mutex> lk(t->mu);
+    t->ended[me] = true;
+    t->cv.notify_all();
+  }
+};
+
 }  // namespace
 
 extern "C" {
+// One hand-over through *word in that order of accesses.  Bit 0: it was taken;
+// bit 1: it had been given by then.
+int t_hand_over(uint64_t* word, uint64_t tag, uint32_t limit, uint32_t turns) {
+  Turns t{*word, turns};
+  int result = 0;
+  std::thread give([&] {
+    const TurnFlag f{&t, 0};
+    ckv::hand_over(f, tag);
+    f.end();
+  });
+  std::thread take([&] {
+    const TurnFlag f{&t, 1};
+    result = ckv::take_over(f, tag, limit);
+    std::lock_guard<std::mutex> lk(t.mu);
+    if (t.given) result |= 2;
+    t.ended[1] = true;
+    t.cv.notify_all();
+  });
+  give.join();
+  take.join();
+  *word = t.word;
+  return result;
+}
 // A wave's steps through positions [step, step + take) * kPagedStep of a context
 // of n, in the attention's order: the first positions of all halves whose rows it
 // loads, steps without pages passed over.  Returns their number.

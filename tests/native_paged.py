@@ -33,4 +33,6 @@ def lib() -> ctypes.CDLL:
     os.replace(tmp, out)
     so = ctypes.CDLL(out)
     so.t_check_table.restype = ctypes.c_uint64
+    so.t_hand_over.argtypes = [ctypes.POINTER(ctypes.c_uint64), ctypes.c_uint64, ctypes.c_uint32,
+                               ctypes.c_uint32]
     return so

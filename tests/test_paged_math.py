@@ -76,3 +76,21 @@ def test_debug_flags_are_held_by_one_call():
     flags = ctypes.c_int()
     assert lib().t_flag_pool(8, 2000, ctypes.byref(flags)) == 0
     assert 1 <= flags.value <= 8
+
+
+@pytest.mark.parametrize("limit", [0, 1, 2, 4])
+def test_hand_over_leaves_no_flag(limit):
+    """Every order of the two sides' accesses, the wait given up before, between and
+    after the other's: what is taken has been given, and the flag is zero again, so
+    that the same tag's next launch does not take what is not there yet."""
+    so, tag = lib(), 0x9E3779B161C8864E
+    outcomes = set()
+    for start in (0, 0xFFFFFFFFFFFFFFFF, 12345):
+        for turns in range(1 << (limit + 4)):
+            word = ctypes.c_uint64(start)
+            for replay in range(2):
+                got = so.t_hand_over(ctypes.byref(word), tag, limit, turns)
+                outcomes.add(got)
+                assert word.value == 0, (start, turns, replay)
+                assert got != 1, (start, turns, replay)      # taken and not given
+    assert {0, 3} <= outcomes <= {0, 2, 3}
