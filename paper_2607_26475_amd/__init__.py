@@ -553,17 +553,20 @@ def paged_write(shape: Shape, cache: PagedCache, requests, positions: torch.Tens
     if requests is not None:
         _dense("requests", requests, torch.int32, n, dev)
     heads = shape.num_kv_heads
-    want, strides = (n, heads, 128), k.stride()
-    if k.shape != want or v.shape != want or strides != v.stride() or strides[2] != 1 or \
-            (strides[1] != 128 and heads > 1) or k.dtype != torch.bfloat16 or \
+    want, ks, vs = (n, heads, 128), k.stride(), v.stride()
+    # (of a dimension that holds a single entry any stride will do)
+    if k.shape != want or v.shape != want or ks[2] != 1 or vs[2] != 1 or \
+            (heads > 1 and (ks[1] != 128 or vs[1] != 128)) or \
+            (n > 1 and ks[0] != vs[0]) or k.dtype != torch.bfloat16 or \
             v.dtype != torch.bfloat16 or k.get_device() != dev or v.get_device() != dev:
-        raise ValueError(f"k, v: bf16 {want} with dense heads on device {dev}, not {k.dtype} "
-                         f"{tuple(k.shape)} on {k.device}")
+        raise ValueError(f"k, v: bf16 {want} with dense heads and one token stride on device "
+                         f"{dev}, not {k.dtype} {tuple(k.shape)} {ks} and {v.dtype} "
+                         f"{tuple(v.shape)} {vs} on {k.device}")
     if rope is not None:
         _rope_ok(rope, dev)
         if q is not None:
             _rows_ok("q", q, rope, n, dev)
-    stride = strides[0] if n > 1 else max(strides[0], 128 * heads)
+    stride = ks[0] if n > 1 else 128 * heads
     _call(_lib.ckv_paged_write, dev, stream, shape, cache, n, _ptr(requests),
           positions.data_ptr(), k.data_ptr(), v.data_ptr(), stride, rope, q)
 

@@ -1,0 +1,30 @@
+"""The paged cache's binding without a GPU: what it passes on."""
+from __future__ import annotations
+
+import pytest
+import torch
+
+import paper_2607_26475_amd as ckv
+
+
+def _write(n, heads, k, v):
+    """A call that all checks of the binding pass ends at the missing GPU."""
+    pages = torch.zeros((4, heads, 16, 128), dtype=torch.bfloat16)
+    table = torch.zeros((2, 4), dtype=torch.int32)
+    ckv.paged_write(ckv.shape_for(2, 4 * heads, heads, 64), ckv.paged_cache_for(pages, pages, table),
+                    None, torch.zeros(n, dtype=torch.int32), k, v)
+
+
+def test_write_takes_single_tokens_and_heads_of_any_stride():
+    """K and V of one token from tensors of unlike rows, and heads of one row: the
+    strides of a single entry do not matter; all others have to be alike."""
+    x, y = (torch.zeros((2, m, 128), dtype=torch.bfloat16) for m in (6, 9))
+    for n, heads, k, v in ((1, 2, x[:1, :2], y[:1, 3:5]), (2, 1, x[:, :1], x[:, 3:4]),
+                           (2, 1, x[:, :1], x.view(2, 3, 2, 128)[:, 1, ::2]),
+                           (2, 2, x[:, :2], x[:, 4:])):
+        with pytest.raises(ValueError, match="on a GPU"):
+            _write(n, heads, k, v)
+    for n, heads, k, v in ((2, 2, x[:, :2], y[:, :2]), (1, 2, x[:1, :2], x[:1, ::3]),
+                           (1, 2, x[:1, ::3], x[:1, :2]), (2, 1, x[:, :1], y[:, :1])):
+        with pytest.raises(ValueError, match="token stride"):
+            _write(n, heads, k, v)
