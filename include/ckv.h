@@ -525,7 +525,7 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
  *   lse[b][t][g] = log sum_p exp(l_p)        (natural logarithm; may be NULL)
  * q [B][T][Hq][d] bf16, out [B][T][Hq][d] fp32, lse [B][T][Hq] fp32.  A token
  * with nothing to attend to gets out = 0 and lse = -inf.  Logits, weights and
- * sums are fp32.  T >= 1 and T * G <= 16.  The positions of all units are cut
+ * sums are fp32.  T >= 1, T * G <= 16 and 0 < scale <= 2^126.  The positions of all units are cut
  * into equal ranges, one a workgroup, and a unit that ranges share is joined by a
  * second launch; where the stored positions (max_ctx) are few, every 128 of them
  * (up to 1024) have a workgroup and the join is inside the one launch.  Joins go in a fixed

@@ -364,6 +364,8 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   CKV_RC(check_cache(cache, d, &a.pg));
   CKV_RC(check_tokens(d, num_tokens));
   CKV_RC(check_scale(scale));
+  if (scale > 0x1p126f)  // 2 log2(e) times it, a factor of the logits, has to be finite
+    return fail(CKV_EINVAL, "scale %g above 2^126", scale);
   CKV_PTR(q);
   CKV_PTR(ctx_lens);
   CKV_PTR(out);

@@ -1,4 +1,4 @@
-"""The paged cache's binding without a GPU: what it passes on."""
+"""The paged cache's binding without a GPU: what it passes on, and scales."""
 from __future__ import annotations
 
 import pytest
@@ -28,3 +28,13 @@ def test_write_takes_single_tokens_and_heads_of_any_stride():
                            (1, 2, x[:1, ::3], x[:1, :2]), (2, 1, x[:, :1], y[:, :1])):
         with pytest.raises(ValueError, match="token stride"):
             _write(n, heads, k, v)
+
+
+def test_attention_refuses_scales_whose_factor_overflows():
+    """A logit of 0 times an infinite factor would be a NaN."""
+    fake, s = 0x100000, ckv.shape_for(0, 8, 2, 64)
+    c = ckv.PagedCache(fake, fake, None, None, fake, 4096, 2048, 128, 0, 16, 9, 4)
+    need = ckv.workspace_bytes(s, 1, ckv.ENTRY_PAGED_DECODE_ATTN)
+    for scale, status in ((2.0 ** 126, 0), (1e-30, 0), (2.0 ** 126 * 1.0000002, 1), (2.5e38, 1)):
+        assert ckv._lib.ckv_paged_decode_attn(s, c, 1, fake, fake, scale, fake, None, fake, need,
+                                              None) == status, scale
