@@ -70,6 +70,9 @@
 extern "C" {
 #endif
 
+/* Changes where an existing entry, structure or value does.  Version 9 has gained
+ * entries since (the rotary positions and the paged cache): a library without them
+ * lacks their symbols. */
 #define CKV_ABI_VERSION 9
 
 typedef enum ckv_status {

@@ -205,7 +205,9 @@ def _load() -> ctypes.CDLL:
                                            vp]),
     }
     for name, (res, args) in sig.items():
-        f = getattr(lib, name)
+        f = getattr(lib, name, None)
+        if f is None:  # entries are added under one version
+            raise ImportError(f"{LIB_PATH} has no {name}, the binding expects it; rebuild it")
         f.restype = res
         f.argtypes = args
     return lib

@@ -1,6 +1,9 @@
 """The paged cache's binding without a GPU: what it passes on, and scales."""
 from __future__ import annotations
 
+import shutil
+import subprocess
+
 import pytest
 import torch
 
@@ -38,3 +41,15 @@ def test_attention_refuses_scales_whose_factor_overflows():
     for scale, status in ((2.0 ** 126, 0), (1e-30, 0), (2.0 ** 126 * 1.0000002, 1), (2.5e38, 1)):
         assert ckv._lib.ckv_paged_decode_attn(s, c, 1, fake, fake, scale, fake, None, fake, need,
                                               None) == status, scale
+
+
+def test_a_library_without_an_entry_is_refused_by_name(tmp_path, monkeypatch):
+    """An older build of the same ABI version: the first entry it lacks is named."""
+    src, so = tmp_path / "old.c", tmp_path / "libold.so"
+    names = [n for n in ckv.EXPORTS if "rope" not in n and "paged" not in n]
+    src.write_text("int ckv_abi_version(void) { return 9; }\n" + "".join(
+        f"int {n}(void) {{ return 0; }}\n" for n in names if n != "ckv_abi_version"))
+    subprocess.run([shutil.which("gcc"), "-shared", "-fPIC", str(src), "-o", str(so)], check=True)
+    monkeypatch.setattr(ckv, "LIB_PATH", str(so))
+    with pytest.raises(ImportError, match="ckv_(rope|paged)_"):
+        ckv._load()
