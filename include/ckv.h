@@ -485,9 +485,9 @@ typedef struct ckv_paged_cache {
  * [num_tokens][Hkv][d] bf16 at token stride kv_token_stride elements (a
  * multiple of 8, at least Hkv * d); without tokens they may be NULL.
  * A token whose position is outside [0, max_ctx) (-1: padding), whose request is
- * outside [0, B) or whose page is not there is not written.  Positions written by one call are distinct (the
- * bytes of a row written twice are unspecified, inside the row).  All other
- * rows keep their bytes.
+ * outside [0, B) or whose page is not there is not written.  Positions written by
+ * one call are distinct (the bytes of a row written twice are unspecified, inside
+ * the row).  All other rows keep their bytes.
  *   With rope (bf16, head_dim 128), K rows are turned by their positions on the
  * way, in fp32, and rounded once to what is stored; with q as well, the query
  * rows of the same tokens (all of them, padding included) are rotated as
@@ -528,11 +528,14 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
  *   lse[b][t][g] = log sum_p exp(l_p)        (natural logarithm; may be NULL)
  * q [B][T][Hq][d] bf16, out [B][T][Hq][d] fp32, lse [B][T][Hq] fp32.  A token
  * with nothing to attend to gets out = 0 and lse = -inf.  Logits, weights and
- * sums are fp32.  T >= 1, T * G <= 16 and 0 < scale <= 2^126.  The positions of all units are cut
- * into equal ranges, one a workgroup, and a unit that ranges share is joined by a
- * second launch; where the stored positions (max_ctx) are few, every 128 of them
- * (up to 1024) have a workgroup and the join is inside the one launch.  Joins go in a fixed
- * order: the same call gives the same bits.
+ * sums are fp32.  T >= 1, T * G <= 16 and 0 < scale <= 2^126.  The positions of
+ * all units are cut into equal ranges, one a workgroup, and a unit that ranges
+ * share is joined by a second launch; where the stored positions (max_ctx) are
+ * few, every 128 of them (up to 1024) have a workgroup and the join is inside the
+ * one launch.  Joins go in a fixed order: the same call gives the same bits.  The
+ * one launch's join waits for its unit's other workgroups, at most about 20 s:
+ * should other launches keep them off the device for so long, the unit's outputs
+ * of that call are NaN (later calls and replays are not affected).
  * Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
 int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
                           int32_t num_tokens, const uint16_t* q, const int32_t* ctx_lens,

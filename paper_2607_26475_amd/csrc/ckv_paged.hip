@@ -47,9 +47,10 @@ __device__ __forceinline__ uint2 ld8_nt(const uint8_t* p) {
 
 // ---- rotary positions ------------------------------------------------------------
 // (cos, sin) of pos * inv_freq.  The angle is formed in quarter turns in fp64
-// (an fp32 angle of 2^20 radians is off by up to 1/16), its whole quarters are taken off there, and what is left, |x| <= pi/4, goes through
-// the Taylor series of sine (to x^9, remainder below 1.8e-9) and cosine (to
-// x^10, below 1.2e-10) in fp32.
+// (an fp32 angle of 2^20 radians is off by up to 1/16), its whole quarters are
+// taken off there, and what is left, |x| <= pi/4, goes through the Taylor series
+// of sine (to x^9, remainder below 1.8e-9) and cosine (to x^10, below 1.2e-10) in
+// fp32.
 __device__ __forceinline__ float2 cos_sin(double quarters) {
   const double whole = rint(quarters);
   const float x = (float)(quarters - whole) * 1.5707963267948966f;
@@ -197,7 +198,8 @@ __device__ __forceinline__ void rope_vectors(const RopeSpec& r, const RopeRows& 
   }
 }
 
-// The same pair by pair.
+// The same pair by pair: 16384 tokens of 40 bf16 rows with 20 of 128 elements
+// turned 113 us, where vectors (96 of 128) take 71.
 template <typename T, bool HALF>
 __device__ __forceinline__ void rope_pairs(const RopeSpec& r, const RopeRows& rows, int t0,
                                            int tokens, const float2* tab) {
@@ -384,8 +386,10 @@ __device__ __forceinline__ void store_row(uint8_t* row, uint8_t* exp, int c, con
 
 // A workgroup writes `per` tokens: their pages and cosines first, into LDS, then
 // K and V rows, 16 lanes each, the loads of kRopeBatch rows a thread at once,
-// then the queries.  Bound by the memory: 22 k tokens of 32 query rows and 8 keys and values each,
-// these to e4m3 (505 MB in and out) 95 us, 5.3 TB/s; 64 tokens 6 us.
+// then the queries.  Bound by the memory: 22 k tokens of 32 query rows and 8 keys
+// and values each, these to e4m3 (505 MB in and out) 98 us, 5.15 TB/s; to bf16
+// (550 MB) 107, 5.15.  With 20 of 128 elements turned, one by one, 169 and 174; 64
+// tokens 5.4 us.
 template <bool E4M3, Turn TURN>
 __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, int per) {
   __shared__ float2 tab[TURN == Turn::kNone ? 1 : kRopeTokens * (kD / 2)];
@@ -703,7 +707,8 @@ __device__ __forceinline__ void next_unit(const Lens& n, int64_t at, Range& r) {
 // row i keeps the results of the step's i-th 16 positions: lane l has position
 // p + l.  Scores wait in LDS while keys are loaded: a store between loads would
 // be waited for with them (106 -> 92 us for 0.54 GB of e4m3 keys and 17 MB of
-// scores, 6.1 TB/s).
+// scores, 6.1 TB/s).  128 units of 16384 positions, pages of 64, 16, 8, 4, 2 and 1:
+// e4m3 49, 49, 58, 61, 66 and 78 us, bf16 91, 90, 110, 110, 114 and 117.
 constexpr int kPagedScoreThreads = 256;
 constexpr int kScoreHold = 16;  // steps whose scores a wave holds
 
@@ -784,7 +789,8 @@ __device__ __forceinline__ float step_scores(ScoreStep<E4M3>& s, const bf16x8* q
 }
 
 template <bool E4M3, bool WIDE, int G>
-__global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_paged_score(PagedScoreArgs a) {
+__global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_paged_score(
+    PagedScoreArgs a) {
   __shared__ float hold[4][64 * kScoreHold];  // finished scores, stored some steps later
   __shared__ RangeLds range;
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -844,7 +850,8 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
     static_assert(kScoreStep == kPagedScoreThreads, "a position a thread");
     const int unit = blockIdx.x / a.chunks;
     const int p = (blockIdx.x - unit * a.chunks) * kScoreStep + threadIdx.x;
-    if (p >= lens(unit / a.pg.Hkv) && p < a.max_ctx) a.scores[(int64_t)unit * a.max_ctx + p] = -INFINITY;
+    if (p >= lens(unit / a.pg.Hkv) && p < a.max_ctx)
+      a.scores[(int64_t)unit * a.max_ctx + p] = -INFINITY;
     return;
   }
   // positions past the contexts' ends, in pieces shared out over the grid
@@ -1181,7 +1188,8 @@ __device__ __forceinline__ int with_pages(const PagedPages& pg, const Ctx& x, in
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         const uint64_t any = __ballot(page[j] >= 0);
-        mask |= (uint32_t)((uint32_t)any != 0) << 2 * j | (uint32_t)(any >> 32 != 0) << (2 * j + 1);
+        mask |= (uint32_t)((uint32_t)any != 0) << 2 * j |
+                (uint32_t)(any >> 32 != 0) << (2 * j + 1);
       }
       mask &= ~1u;
       skip = mask ? __builtin_ctz(mask) : 16;
@@ -1332,9 +1340,12 @@ __device__ __forceinline__ void store_empty(const PagedAttnArgs& a, int64_t firs
 }
 
 // A workgroup attends over a range of steps, unit by unit; sums of a unit that
-// other ranges share go to memory.  Bound by the reading of K and V: 4.4 GB of 64
-// bf16 sequences 658 us (6.7 TB/s), 0.76 GB of two e4m3 sequences with 16 query
-// rows a unit 119 (6.4), and the join 6 to 8 us more.
+// other ranges share go to memory.  Bound by the reading of K and V, whose lines
+// are fetched once (4.44 of 4.43 GB, 769 of 762 MB): 4.43 GB of 64 bf16 sequences
+// 664 us a call (6.7 TB/s), 0.76 GB of two e4m3 sequences with 16 query rows a unit
+// 128 (6.0), of which the join is 6 to 8.  128 units of 16384 positions, pages of
+// 64, 16, 8, 4, 2 and 1: e4m3 93, 97, 113, 114, 123 and 148 us, bf16 172, 174, 182,
+// 185, 190 and 204.
 template <bool E4M3, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
@@ -1547,7 +1558,8 @@ __global__ __launch_bounds__(kPagedMergeThreads) void k_paged_merge(PagedAttnArg
   if (t.unit < 0) return;
   // the last range that begins before the unit's end: total * i / nwg < end
   const int64_t nwg = ranges_of(t.total, a.nwg, kLeastSteps);
-  const int n = (int)((t.end * nwg - 1) / t.total) - w + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int n = (int)((t.end * nwg - 1) / t.total) - w + 1;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   auto partial = [&](int i) {
     return a.part + (((int64_t)(w + i) * 2 + (i == 0 ? t.slot : 0)) * rows + row) * kPartStride;
   };

@@ -43,7 +43,8 @@ struct RopeArgs {
 
 struct PagedWriteArgs {
   PagedPages pg;
-  RopeArgs rope;           // r.inv_freq NULL: rows are stored as they are; q: heads 0, or rotated too
+  RopeArgs rope;           // r.inv_freq NULL: rows are stored as they are; q: heads 0, or
+                           // rotated too
   const int32_t* req;      // NULL: token t is request t's
   const uint16_t* k;
   const uint16_t* v;

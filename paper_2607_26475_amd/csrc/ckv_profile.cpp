@@ -96,8 +96,9 @@ const char* ckv_kernel_name(int id) {
   static const char* names[CKV_K_TOTAL] = {"zero", "score", "hist", "filter", "finish",
                                            "attn", "combine", "dual", "gather", "miss",
                                            "landmarks", "expand", "reconstruct",
-                                           "select_attn", "probe", "critical", "rope", "paged_write",
-                                           "paged_read", "paged_score", "paged_attn", "paged_merge"};
+                                           "select_attn", "probe", "critical", "rope",
+                                           "paged_write", "paged_read", "paged_score",
+                                           "paged_attn", "paged_merge"};
   return (id >= 0 && id < CKV_K_TOTAL) ? names[id] : "";
 }
 
