@@ -459,18 +459,28 @@ int ckv_rope_frequencies(int32_t rot_dim, double base, const ckv_rope_scaling* s
  *                     with one exponent byte a row, k_exps / v_exps
  *                     [num_pages][Hkv][page_size]: an element is code *
  *                     2^(byte - 127), byte in [0, 254]
+ *   CKV_CACHE_E2M1    4-bit codes, two a byte (element 2i in the low half of byte i
+ *                     of its row): sign, two exponent bits, one bit of mantissa,
+ *                     the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6; every 32 elements
+ *                     have one exponent byte, k_exps / v_exps
+ *                     [num_pages][Hkv][page_size][4]: an element is code *
+ *                     2^(byte - 127), byte in [0, 252], or NaN where it is 255
  * Strides are multiples of 16 bytes and at least 128 elements; page_size is a
  * power of two up to 65536, and page_size * row_stride elements take less than
  * 2^31 bytes.  Entries of page_table past ceil(n_b / page_size) are not used.
  * Rows at or past n_b may hold anything; rows below it are finite.  ckv_shape
  * gives batch, heads and max_ctx (its row strides are checked and not used);
  * positions live in [0, max_ctx). */
-typedef enum ckv_cache_kind { CKV_CACHE_BF16 = 0, CKV_CACHE_E4M3 = 1 } ckv_cache_kind;
+typedef enum ckv_cache_kind {
+  CKV_CACHE_BF16 = 0,
+  CKV_CACHE_E4M3 = 1,
+  CKV_CACHE_E2M1 /* 2 */
+} ckv_cache_kind;
 
 typedef struct ckv_paged_cache {
   void* k_pages;
   void* v_pages;
-  uint8_t* k_exps;            /* CKV_CACHE_E4M3, else NULL */
+  uint8_t* k_exps;            /* NULL for CKV_CACHE_BF16   */
   uint8_t* v_exps;
   const int32_t* page_table;  /* [B][table_stride] device  */
   int64_t page_stride, head_stride, row_stride; /* elements */
@@ -496,14 +506,20 @@ typedef struct ckv_paged_cache {
  * with amax the largest finite |x| of the row and e the smallest integer in
  * [-127, 127] with amax <= 448 * 2^e, the byte e + 127 and the codes of x /
  * 2^e (exact) rounded to nearest, ties to even; an infinity or NaN is stored as
- * NaN.  A power of two loses nothing: e4m3's own exponent carries the rest. */
+ * NaN.  A power of two loses nothing: e4m3's own exponent carries the rest.
+ *   CKV_CACHE_E2M1: for every 32 elements, with amax their largest |x| and e the
+ * smallest integer in [-125, 125] with amax <= 6 * 2^e (or 125), the byte e + 127
+ * and the codes of x / 2^e rounded to nearest, ties to the even code, 6 at most;
+ * where one of the 32 is an infinity or NaN, the byte is 255 and the codes are
+ * unspecified.  Every stored value is exact in bf16. */
 int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t num_tokens,
                     const int32_t* requests, const int32_t* positions, const uint16_t* k,
                     const uint16_t* v, int64_t kv_token_stride, const ckv_rope* rope,
                     const ckv_rows* q, void* stream);
 
 /* Reads rows of a paged cache back as bf16 (values of CKV_CACHE_E4M3 rows are
- * exact, or rounded where they fall among bf16's subnormals):
+ * exact, or rounded where they fall among bf16's subnormals; those of
+ * CKV_CACHE_E2M1 rows are exact):
  *   idx NULL:  slot i < min(k, n_b) of k_dst/v_dst [B][Hkv][k][d] gets position i;
  *   idx given: slot i < n_sel[b][h] (clamped to [0, k]) gets position
  *              idx[b][h][i], as ckv_gather_kv does from a dense cache; entries

@@ -393,7 +393,7 @@ def chunked_kv_attn(shape: Shape, chunk: int, q_att, q_sel, landmarks, ctx_lens,
 ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 ROPE_BF16, ROPE_F32 = 0, 1
 ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_BANDS, ROPE_RAMP = 0, 1, 2, 3, 4
-CACHE_BF16, CACHE_E4M3 = 0, 1
+CACHE_BF16, CACHE_E4M3, CACHE_E2M1 = 0, 1, 2
 
 
 # The current stream's handle without a Stream object around it (2.6 us of an
@@ -497,28 +497,37 @@ def rope_rows(rope: Rope, positions: torch.Tensor, q: Rows, k: Optional[Rows] = 
     _call(_lib.ckv_rope_rows, dev, stream, rope, n, positions.data_ptr(), q, k)
 
 
+_E2M1 = getattr(torch, "float4_e2m1fn_x2", torch.uint8)  # bytes of two codes
+
+
 def paged_cache_for(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
                     k_exps: Optional[torch.Tensor] = None,
                     v_exps: Optional[torch.Tensor] = None) -> PagedCache:
     """The handle of a paged cache: pages as [pages][Hkv][page_size][d] views
-    of one pair of strides (bf16, or uint8 / float8_e4m3fn codes with uint8
-    exponents [pages][Hkv][page_size]), page_table [B][pages per request].
-    The handle keeps the tensors alive."""
+    of one pair of strides (bf16, uint8 / float8_e4m3fn codes with uint8
+    exponents [pages][Hkv][page_size], or uint8 / float4_e2m1fn_x2 bytes of two
+    e2m1 codes, 64 a row, with uint8 exponents [pages][Hkv][page_size][4]),
+    page_table [B][pages per request].  The handle keeps the tensors alive."""
     if k_pages.dim() != 4 or k_pages.shape != v_pages.shape or \
             k_pages.stride() != v_pages.stride() or k_pages.dtype != v_pages.dtype or \
-            k_pages.stride(3) != 1 or k_pages.shape[3] != 128:
-        raise ValueError("k_pages, v_pages: [pages][Hkv][page_size][128], alike, rows dense")
-    kind = CACHE_BF16 if k_pages.element_size() == 2 else CACHE_E4M3
-    if k_pages.dtype not in (torch.bfloat16, torch.uint8, torch.float8_e4m3fn):
-        raise ValueError(f"pages of {k_pages.dtype}")
+            k_pages.stride(3) != 1 or k_pages.shape[3] not in (64, 128):
+        raise ValueError("k_pages, v_pages: [pages][Hkv][page_size][128] (64 bytes of two codes), "
+                         "alike, rows dense")
+    four = k_pages.shape[3] == 64
+    kind = CACHE_E2M1 if four else CACHE_BF16 if k_pages.element_size() == 2 else CACHE_E4M3
+    if k_pages.dtype not in ((torch.uint8, _E2M1) if four else
+                             (torch.bfloat16, torch.uint8, torch.float8_e4m3fn)):
+        raise ValueError(f"pages of {k_pages.dtype} {tuple(k_pages.shape)}")
+    want = (*k_pages.shape[:3], 4) if four else k_pages.shape[:3]
     for e in (k_exps, v_exps):
-        if (e is not None) != (kind == CACHE_E4M3) or (e is not None and (
-                e.dtype != torch.uint8 or e.shape != k_pages.shape[:3] or not e.is_contiguous())):
-            raise ValueError("k_exps, v_exps: dense uint8 [pages][Hkv][page_size] of e4m3 pages")
+        if (e is not None) != (kind != CACHE_BF16) or (e is not None and (
+                e.dtype != torch.uint8 or e.shape != want or not e.is_contiguous())):
+            raise ValueError("k_exps, v_exps: dense uint8 [pages][Hkv][page_size] of e4m3 pages, "
+                             "[pages][Hkv][page_size][4] of e2m1 pages, none of bf16 pages")
     if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.stride(1) != 1:
         raise ValueError("page_table: int32 [B][pages]")
     c = PagedCache(k_pages.data_ptr(), v_pages.data_ptr(), _ptr(k_exps), _ptr(v_exps),
-                   page_table.data_ptr(), *(_stride(k_pages, i) for i in range(3)), kind,
+                   page_table.data_ptr(), *((2 if four else 1) * _stride(k_pages, i) for i in range(3)), kind,
                    k_pages.shape[2], k_pages.shape[0],
                    page_table.shape[1] if page_table.shape[0] == 1 else page_table.stride(0))
     c.keep = (k_pages, v_pages, page_table, k_exps, v_exps)

@@ -75,16 +75,15 @@ int check_num_tokens(int32_t n) {
 
 int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p) {
   if (!c) return fail(CKV_EINVAL, "cache is NULL");
-  if (c->kind != CKV_CACHE_BF16 && c->kind != CKV_CACHE_E4M3)
+  if (c->kind != CKV_CACHE_BF16 && c->kind != CKV_CACHE_E4M3 && c->kind != CKV_CACHE_E2M1)
     return fail(CKV_EINVAL, "bad cache.kind %d", c->kind);
-  const bool e4m3 = c->kind == CKV_CACHE_E4M3;
   void *k_pages = c->k_pages, *v_pages = c->v_pages;
   const int32_t* page_table = c->page_table;
   uint8_t *k_exps = c->k_exps, *v_exps = c->v_exps;
   CKV_PTR(k_pages);
   CKV_PTR(v_pages);
   CKV_PTR(page_table);
-  if (e4m3) {
+  if (c->kind != CKV_CACHE_BF16) {
     CKV_PTR(k_exps);
     CKV_PTR(v_exps);
   } else if (k_exps || v_exps) {
@@ -98,17 +97,18 @@ int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p) {
   if (c->table_stride < slots)
     return fail(CKV_ESHAPE, "table_stride %d below the %lld pages of max_ctx", c->table_stride,
                 (long long)slots);
-  const int size = e4m3 ? 1 : 2;
+  // bytes of x elements: x * size / 2
+  const int size = c->kind == CKV_CACHE_BF16 ? 4 : c->kind == CKV_CACHE_E4M3 ? 2 : 1;
   const int64_t strides[3] = {c->page_stride, c->head_stride, c->row_stride};
   for (int64_t x : strides)
-    if (x < kD || x > ((int64_t)1 << 36) || x * size % 16)
+    if (x < kD || x > ((int64_t)1 << 36) || x * size % 32)
       return fail(CKV_ESHAPE, "cache stride %lld (128 .. 2^36 elements, a multiple of 16 bytes)",
                   (long long)x);
-  if (c->row_stride * size * ps >= ((int64_t)1 << 31))
+  if (c->row_stride * size / 2 * ps >= ((int64_t)1 << 31))
     return fail(CKV_EUNSUPPORTED, "page_size %d rows at stride %lld reach 2^31 bytes", ps,
                 (long long)c->row_stride);
   int64_t last = 0;
-  if (__builtin_mul_overflow((int64_t)c->num_pages, c->page_stride * size, &last) ||
+  if (__builtin_mul_overflow((int64_t)c->num_pages, c->page_stride * size / 2, &last) ||
       last > ((int64_t)1 << 61))
     return fail(CKV_ESHAPE, "page_stride %lld times %d pages", (long long)c->page_stride,
                 c->num_pages);
@@ -117,9 +117,9 @@ int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p) {
   p->k_exps = k_exps;
   p->v_exps = v_exps;
   p->table = page_table;
-  p->page_bytes = c->page_stride * size;
-  p->head_bytes = c->head_stride * size;
-  p->row_bytes = (int32_t)(c->row_stride * size);
+  p->page_bytes = c->page_stride * size / 2;
+  p->head_bytes = c->head_stride * size / 2;
+  p->row_bytes = (int32_t)(c->row_stride * size / 2);
   p->shift = __builtin_ctz((unsigned)ps);
   p->num_pages = c->num_pages;
   p->table_stride = c->table_stride;
@@ -280,7 +280,7 @@ int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_
   a.tok = kv_token_stride;
   a.B = d.B;
   a.max_ctx = d.max_ctx;
-  CKV_TRY_HIP(launch_paged_write(a, cache->kind == CKV_CACHE_E4M3, s), "paged write launch");
+  CKV_TRY_HIP(launch_paged_write(a, (Kind)cache->kind, s), "paged write launch");
   return CKV_OK;
 }
 
@@ -317,7 +317,7 @@ int ckv_paged_read(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.max_ctx = d.max_ctx;
   a.k = k;
   a.units = d.U;
-  CKV_TRY_HIP(launch_paged_read(a, cache->kind == CKV_CACHE_E4M3, s), "paged read launch");
+  CKV_TRY_HIP(launch_paged_read(a, (Kind)cache->kind, s), "paged read launch");
   return CKV_OK;
 }
 
@@ -350,7 +350,7 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.nwg = a.direct ? (int)steps : slots;
   a.piece = a.direct ? kScoreStep : kScorePiece;
   a.chunks = (d.max_ctx + a.piece - 1) / a.piece;
-  CKV_TRY_HIP(launch_paged_score(a, cache->kind == CKV_CACHE_E4M3, d.G, s), "paged score launch");
+  CKV_TRY_HIP(launch_paged_score(a, (Kind)cache->kind, d.G, s), "paged score launch");
   return CKV_OK;
 }
 
@@ -412,7 +412,7 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
   a.chunks = direct ? (int)n : 0;
   a.piece = lg;
   a.tag = next_fused_tag();
-  CKV_TRY_HIP(launch_paged_attn(a, cache->kind == CKV_CACHE_E4M3, s), "paged attention launch");
+  CKV_TRY_HIP(launch_paged_attn(a, (Kind)cache->kind, s), "paged attention launch");
   return CKV_OK;
 }
 

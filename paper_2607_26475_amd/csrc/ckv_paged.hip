@@ -38,11 +38,43 @@ __device__ __forceinline__ uint4 e4m3_octet(uint2 w) {
                     e4m3_pair<true>(w.y));
 }
 
+// Codes 2 i and 2 i + 1 of w as two bf16 times 2^(byte - 127), the byte in bits
+// 30 .. 23 of `scale` (its other bits do not matter): exact while |value| < 2^128;
+// byte 255 gives NaN.  All 256 bytes and all codes were compared with ldexp.
+template <int I>
+__device__ __forceinline__ uint32_t e2m1_pair(uint32_t w, uint32_t scale) {
+  return __builtin_bit_cast(
+      uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, __uint_as_float(scale), I));
+}
+
+// (i is a constant of an unrolled loop.)
+__device__ __forceinline__ uint32_t e2m1_pair_at(uint32_t w, uint32_t scale, int i) {
+  return i == 0   ? e2m1_pair<0>(w, scale)
+         : i == 1 ? e2m1_pair<1>(w, scale)
+         : i == 2 ? e2m1_pair<2>(w, scale)
+                  : e2m1_pair<3>(w, scale);
+}
+
+// Eight codes as eight bf16.
+__device__ __forceinline__ uint4 e2m1_octet(uint32_t w, uint32_t scale) {
+  return make_uint4(e2m1_pair<0>(w, scale), e2m1_pair<1>(w, scale), e2m1_pair<2>(w, scale),
+                    e2m1_pair<3>(w, scale));
+}
+
+// Byte i of w in bits 30 .. 23.
+__device__ __forceinline__ uint32_t scale_of(uint32_t w, int i) {
+  return __builtin_amdgcn_alignbit(w, w, 9 + 8 * i);
+}
+
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 __device__ __forceinline__ uint2 ld8_nt(const uint8_t* p) {
   const u32x2 v = __builtin_nontemporal_load(reinterpret_cast<const u32x2*>(p));
   return make_uint2(v[0], v[1]);
+}
+
+__device__ __forceinline__ uint32_t ld4_nt(const uint8_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
 }
 
 // ---- rotary positions ------------------------------------------------------------
@@ -305,6 +337,15 @@ __device__ __forceinline__ int64_t exp_offset(const PagedPages& pg, int page, in
   return (((int64_t)page * pg.Hkv + h) << pg.shift) + (pos & ((1 << pg.shift) - 1));
 }
 
+// Codes of 16 bytes of bf16 elements, and exponent bytes a row.
+__host__ __device__ constexpr int row_part(Kind k) {
+  return k == Kind::kBf16 ? 16 : k == Kind::kE4M3 ? 8 : 4;
+}
+
+__host__ __device__ constexpr int exps_of(Kind k) {
+  return k == Kind::kBf16 ? 0 : k == Kind::kE4M3 ? 1 : kD / kExpGroup;
+}
+
 // How a written row is turned: not at all; halves or neighbouring pairs in
 // whole vectors; one by one.
 enum class Turn { kNone, kHalf, kPairs, kEach };
@@ -354,10 +395,32 @@ __device__ __forceinline__ void turn8(const RopeSpec& r, const uint16_t* row, in
 }
 
 // Sixteen lanes write a row: lane c its elements [8c, 8c + 8).
-template <bool E4M3>
+template <Kind KIND>
 __device__ __forceinline__ void store_row(uint8_t* row, uint8_t* exp, int c, const float* y) {
-  if (!E4M3) {
+  if (KIND == Kind::kBf16) {
     *reinterpret_cast<uint4*>(row + 16 * c) = pack8_bf16(y);
+    return;
+  }
+  if (KIND == Kind::kE2M1) {
+    // four lanes hold a group; as bits, magnitudes rank as their values do, and an
+    // infinity or NaN above all of them
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = max(most, __float_as_uint(y[j]) & 0x7fffffffu);
+    most = max(most, dpp_u32<0xB1, 0xF, false>(most));  // quad_perm [1,0,3,2]
+    most = max(most, dpp_u32<0x4E, 0xF, false>(most));  // [2,3,0,1]
+    // 6 = 1.5 * 2^2: the byte is the leading power's field less 2, one more where
+    // the largest is above 1.5 times it
+    const int field = (int)(most >> 23) - 2 + ((most & 0x7fffffu) > 0x400000u ? 1 : 0);
+    const uint32_t byte = min(max(field, 2), 252);  // stored values are normal bf16 numbers
+    const float scale = __uint_as_float(byte << 23);
+    // x / scale, nearest, ties to even, 6 at most
+    uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], scale, 3);
+    *reinterpret_cast<uint32_t*>(row + 4 * c) = w;
+    if ((c & 3) == 0) exp[c >> 2] = most >= 0x7f800000u ? 255 : (uint8_t)byte;
     return;
   }
   float most = 0.f;
@@ -390,7 +453,7 @@ __device__ __forceinline__ void store_row(uint8_t* row, uint8_t* exp, int c, con
 // and values each, these to e4m3 (505 MB in and out) 98 us, 5.15 TB/s; to bf16
 // (550 MB) 107, 5.15.  With 20 of 128 elements turned, one by one, 169 and 174; 64
 // tokens 5.4 us.
-template <bool E4M3, Turn TURN>
+template <Kind KIND, Turn TURN>
 __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, int per) {
   __shared__ float2 tab[TURN == Turn::kNone ? 1 : kRopeTokens * (kD / 2)];
   __shared__ int64_t row_at[kRopeTokens], exp_at[kRopeTokens];  // of head 0; -1: not written
@@ -403,7 +466,7 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
     if ((unsigned)pos < (unsigned)a.max_ctx && (unsigned)b < (unsigned)a.B)
       page = page_of(a.pg, b, pos);
     row_at[tid] = page < 0 ? -1 : row_offset(a.pg, page, 0, pos);
-    exp_at[tid] = page < 0 ? -1 : exp_offset(a.pg, page, 0, pos);
+    exp_at[tid] = page < 0 ? -1 : exps_of(KIND) * exp_offset(a.pg, page, 0, pos);
   }
   if (TURN != Turn::kNone) rope_table(r, a.rope.pos, t0, tokens, tab);
   __syncthreads();
@@ -432,7 +495,7 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
       const int64_t at = row_at[tok[i]];
       if (at < 0) continue;
       uint8_t* row = (is_v ? a.pg.v : a.pg.k) + at + head[i] * a.pg.head_bytes;
-      if (!E4M3 && (TURN == Turn::kNone || is_v)) {  // the bits as they are
+      if (KIND == Kind::kBf16 && (TURN == Turn::kNone || is_v)) {  // the bits as they are
         *reinterpret_cast<u32x4*>(row + 16 * c) = x[i];
         continue;
       }
@@ -440,10 +503,10 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
       if (TURN == Turn::kNone || is_v) unpack8(make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]), y);
       else turn8<TURN>(r, src[i], c, tab + tok[i] * (r.rot >> 1), x[i], o[i], y);
       uint8_t* exp = nullptr;
-      if (E4M3)
+      if (KIND != Kind::kBf16)
         exp = (is_v ? a.pg.v_exps : a.pg.k_exps) + exp_at[tok[i]] +
-              ((int64_t)head[i] << a.pg.shift);
-      store_row<E4M3>(row, exp, c, y);
+              exps_of(KIND) * ((int64_t)head[i] << a.pg.shift);
+      store_row<KIND>(row, exp, c, y);
     }
   }
   if (TURN == Turn::kNone || a.rope.q.heads == 0) return;
@@ -468,7 +531,7 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
 constexpr int kPagedReadThreads = 256;
 constexpr int kReadUnroll = kReadSlots * 32 / kPagedReadThreads;
 
-template <bool E4M3>
+template <Kind KIND>
 __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs a) {
   const int c = threadIdx.x & 15;
   const bool is_v = threadIdx.x & 16;
@@ -478,7 +541,7 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
   const int count = a.idx ? clamp_len(((TablePtr)(uintptr_t)a.n_sel)[unit], a.k) : min(a.k, n);
   const int64_t slot0 = (int64_t)unit * a.k;
   const int32_t* table = a.pg.table + (int64_t)b * a.pg.table_stride;
-  const uint8_t* pages = (is_v ? a.pg.v : a.pg.k) + h * a.pg.head_bytes + (E4M3 ? 8 : 16) * c;
+  const uint8_t* pages = (is_v ? a.pg.v : a.pg.k) + h * a.pg.head_bytes + row_part(KIND) * c;
   const uint8_t* exps = is_v ? a.pg.v_exps : a.pg.k_exps;
   uint16_t* dst = (is_v ? a.v_dst : a.k_dst) + slot0 * kD + 8 * c;
   int pos[kReadUnroll], page[kReadUnroll];
@@ -502,10 +565,13 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
     const int row = page[i] >= 0 ? pos[i] & mask : 0;
     const int64_t pg = max(page[i], 0);
     const uint8_t* p = pages + pg * a.pg.page_bytes + row * a.pg.row_bytes;
-    if (E4M3) {
+    if (KIND == Kind::kE4M3) {
       const uint2 x = ld8_nt(p);
       w[i] = u32x4{x.x, x.y, 0u, 0u};
       e[i] = exps[((pg * a.pg.Hkv + h) << a.pg.shift) + row];
+    } else if (KIND == Kind::kE2M1) {
+      w[i] = u32x4{ld4_nt(p), 0u, 0u, 0u};
+      e[i] = exps[4 * (((pg * a.pg.Hkv + h) << a.pg.shift) + row) + (c >> 2)];
     } else {
       w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
     }
@@ -514,7 +580,9 @@ __global__ __launch_bounds__(kPagedReadThreads) void k_paged_read(PagedReadArgs 
   for (int i = 0; i < kReadUnroll; ++i) {
     if (page[i] < 0) continue;
     const int s = first + i * (kPagedReadThreads / 32) + (threadIdx.x >> 5);
-    if (E4M3) {
+    if (KIND == Kind::kE2M1) {
+      *reinterpret_cast<uint4*>(dst + (int64_t)s * kD) = e2m1_octet(w[i][0], e[i] << 23);
+    } else if (KIND == Kind::kE4M3) {
       float x[8];
       unpack8(e4m3_octet(make_uint2(w[i][0], w[i][1])), x);
 #pragma unroll
@@ -545,17 +613,21 @@ struct Ctx {
 // (g, r) = (lane / 16, lane % 16) holds row r, in the fragments f = 0 .. 3 the
 // elements frag_base(f) + 0 .. 7, 16 bytes a load.  Any order of the 128
 // products will do as long as the queries' fragments have the same.
-template <bool E4M3>
+template <Kind KIND>
 __device__ __forceinline__ int frag_base(int f, int g) {
-  return E4M3 ? 64 * (f >> 1) + 16 * g + 8 * (f & 1) : 32 * f + 8 * g;
+  return KIND == Kind::kE4M3   ? 64 * (f >> 1) + 16 * g + 8 * (f & 1)
+         : KIND == Kind::kE2M1 ? kExpGroup * g + 8 * f
+                               : 32 * f + 8 * g;
 }
 
-template <bool E4M3>
+template <Kind KIND>
 struct KRaw {
-  uint4 w[E4M3 ? 2 : 4];
+  static constexpr int kN = row_part(KIND) / 4;  // 16-byte loads
+  uint4 w[kN];
+  uint32_t e;  // e2m1: the exponent byte of the lane's 32 elements
   __device__ __forceinline__ void load(const uint8_t* row, int g) {
 #pragma unroll
-    for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+    for (int i = 0; i < kN; ++i)
       w[i] = *reinterpret_cast<const uint4*>(row + 64 * i + 16 * g);
   }
   // The same from whole 128-byte lines, streamed past the caches (rows of one
@@ -565,17 +637,22 @@ struct KRaw {
   // belongs to the other's row.
   __device__ __forceinline__ void load_lines(const uint8_t* base, int32_t row_bytes, int32_t cap,
                                              int g, int r) {
+    if constexpr (KIND == Kind::kE2M1) {  // rows of 64 bytes: 16 of them a load
+      w[0] = ld16_nt(reinterpret_cast<const uint16_t*>(base + (uint32_t)min(r * row_bytes, cap) +
+                                                       16 * g));
+      return;
+    }
     const uint8_t* p = base + 8 * (r & 8) + 16 * g;
     const uint32_t at[2] = {(uint32_t)min((r & 7) * row_bytes, cap),
                             (uint32_t)min(((r & 7) + 8) * row_bytes, cap)};
 #pragma unroll
-    for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+    for (int i = 0; i < kN; ++i)
       w[i] = ld16_nt(reinterpret_cast<const uint16_t*>(p + at[i & 1] + 128 * (i >> 1)));
   }
   __device__ __forceinline__ void swap_halves(int r) {
     const bool lo = r < 8;
 #pragma unroll
-    for (int l = 0; l < (E4M3 ? 2 : 4); l += 2) {
+    for (int l = 0; l + 1 < kN; l += 2) {
       uint32_t a[4] = {w[l].x, w[l].y, w[l].z, w[l].w};
       uint32_t b[4] = {w[l + 1].x, w[l + 1].y, w[l + 1].z, w[l + 1].w};
 #pragma unroll
@@ -589,7 +666,11 @@ struct KRaw {
     }
   }
   __device__ __forceinline__ bf16x8 frag(int f) const {
-    if (!E4M3) return as_bf16x8(w[f]);
+    if constexpr (KIND == Kind::kBf16) return as_bf16x8(w[f]);
+    if constexpr (KIND == Kind::kE2M1) {
+      const uint32_t c = f & 2 ? (f & 1 ? w[0].w : w[0].z) : (f & 1 ? w[0].y : w[0].x);
+      return as_bf16x8(e2m1_octet(c, e << 23));
+    }
     const uint4 q = w[f >> 1];
     return as_bf16x8(e4m3_octet(f & 1 ? make_uint2(q.z, q.w) : make_uint2(q.x, q.y)));
   }
@@ -712,10 +793,10 @@ __device__ __forceinline__ void next_unit(const Lens& n, int64_t at, Range& r) {
 constexpr int kPagedScoreThreads = 256;
 constexpr int kScoreHold = 16;  // steps whose scores a wave holds
 
-template <bool E4M3>
+template <Kind KIND>
 struct ScoreStep {
-  KRaw<E4M3> k[4];
-  uint32_t e;   // of the lane's own position
+  KRaw<KIND> k[4];
+  uint32_t e;   // of the lane's own position (e4m3)
   bool there;   // likewise
 };
 
@@ -745,12 +826,13 @@ __device__ __forceinline__ ScorePages<WIDE> score_pages(const PagedPages& pg, co
   return t;
 }
 
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __device__ __forceinline__ void load_score_step(const PagedPages& pg, const Ctx& x, int p,
-                                                const ScorePages<WIDE>& t, ScoreStep<E4M3>& s) {
+                                                const ScorePages<WIDE>& t, ScoreStep<KIND>& s) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   s.there = (unsigned)t.own < (unsigned)pg.num_pages && p + lane < x.n;
-  if (E4M3) s.e = pg.k_exps[exp_offset(pg, s.there ? t.own : 0, x.h, min(p + lane, x.n - 1))];
+  if (KIND == Kind::kE4M3)
+    s.e = pg.k_exps[exp_offset(pg, s.there ? t.own : 0, x.h, min(p + lane, x.n - 1))];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const bool has = (unsigned)t.row[i] < (unsigned)pg.num_pages;
@@ -759,7 +841,13 @@ __device__ __forceinline__ void load_score_step(const PagedPages& pg, const Ctx&
       const uint8_t* base = pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, first);
       const int32_t cap = half_last(first, x.n) * pg.row_bytes;
       s.k[i].load_lines(base, pg.row_bytes, cap, g, r);
+      if (KIND == Kind::kE2M1)
+        s.k[i].e = pg.k_exps[4 * (exp_offset(pg, has ? t.row[i] : 0, x.h, first) +
+                                  min(r, half_last(first, x.n))) + g];
     } else {
+      if (KIND == Kind::kE2M1)
+        s.k[i].e = pg.k_exps[4 * exp_offset(pg, has ? t.row[i] : 0, x.h,
+                                            min(p + 16 * i + r, x.n - 1)) + g];
       s.k[i].load(pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, min(p + 16 * i + r, x.n - 1)),
                   g);
     }
@@ -767,8 +855,8 @@ __device__ __forceinline__ void load_score_step(const PagedPages& pg, const Ctx&
 }
 
 // Scores of a step: the largest over the group's heads, of position p + lane.
-template <bool E4M3, bool WIDE, int G>
-__device__ __forceinline__ float step_scores(ScoreStep<E4M3>& s, const bf16x8* q, float scale) {
+template <Kind KIND, bool WIDE, int G>
+__device__ __forceinline__ float step_scores(ScoreStep<KIND>& s, const bf16x8* q, float scale) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   float best[4];
 #pragma unroll
@@ -784,11 +872,11 @@ __device__ __forceinline__ float step_scores(ScoreStep<E4M3>& s, const bf16x8* q
     if (G == 16) best[i] = fmaxf(best[i], __shfl_xor(best[i], 32));
   }
   float mine = (g & 2 ? (g & 1 ? best[3] : best[2]) : (g & 1 ? best[1] : best[0])) * scale;
-  if (E4M3) mine = times_exp(mine, s.e);
+  if (KIND == Kind::kE4M3) mine = times_exp(mine, s.e);
   return s.there ? mine : -INFINITY;
 }
 
-template <bool E4M3, bool WIDE, int G>
+template <Kind KIND, bool WIDE, int G>
 __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_paged_score(
     PagedScoreArgs a) {
   __shared__ float hold[4][64 * kScoreHold];  // finished scores, stored some steps later
@@ -819,18 +907,18 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
     const int stop = min((rg.step + take) * kScoreStep, x.n);
     int p = rg.step * kScoreStep + 64 * wave;
     if (p < stop) {
-      ScoreStep<E4M3> s;
+      ScoreStep<KIND> s;
       ScorePages<WIDE> pages = score_pages<WIDE>(a.pg, x, p);
-      load_score_step<E4M3, WIDE>(a.pg, x, p, pages, s);
+      load_score_step<KIND, WIDE>(a.pg, x, p, pages, s);
       pages = score_pages<WIDE>(a.pg, x, lookup_at(p + kScoreStep, stop));
       bf16x8 q[4];
 #pragma unroll
       for (int f = 0; f < 4; ++f)
         q[f] = as_bf16x8(ld16(a.q + ((int64_t)x.b * a.Hq + x.h * G + (r & (G - 1))) * kD +
-                              frag_base<E4M3>(f, g)));
+                              frag_base<KIND>(f, g)));
       float* mine = hold[wave] + lane;
       for (int i = 0;;) {
-        mine[64 * i++] = step_scores<E4M3, WIDE, G>(s, q, a.scale);
+        mine[64 * i++] = step_scores<KIND, WIDE, G>(s, q, a.scale);
         p += kScoreStep;
         const bool more = p < stop;
         if (!more || i == kScoreHold) {
@@ -839,7 +927,7 @@ __global__ __launch_bounds__(kPagedScoreThreads, score_wgs_per_cu(WIDE)) void k_
           i = 0;
         }
         if (!more) break;
-        load_score_step<E4M3, WIDE>(a.pg, x, p, pages, s);
+        load_score_step<KIND, WIDE>(a.pg, x, p, pages, s);
         pages = score_pages<WIDE>(a.pg, x, lookup_at(p + kScoreStep, stop));
       }
     }
@@ -905,11 +993,14 @@ struct WaveState {
 // V once the products have taken its rows: a wave always has one of them in
 // flight, and none needs a second set of registers.  Both are streamed past the
 // caches by loads of whole lines (4.4 GB of a bf16 batch 745 -> 667 us).
-template <bool E4M3>
+template <Kind KIND>
 struct Tile {
-  KRaw<E4M3> k[2];
-  uint32_t v[8][E4M3 ? 2 : 4];      // row j: bf16, or codes
-  uint32_t ke[E4M3 ? 2 : 1], ve[E4M3 ? 2 : 1];  // exponent bytes of each half's four positions
+  KRaw<KIND> k[2];
+  static constexpr int kV = row_part(KIND) / 4;
+  uint32_t v[8][kV];                // row j: bf16, or codes
+  // exponent bytes: e4m3 of each half's four positions; e2m1 of row j's four groups
+  uint32_t ke[KIND == Kind::kE4M3 ? 2 : 1];
+  uint32_t ve[KIND == Kind::kE4M3 ? 2 : KIND == Kind::kE2M1 ? 8 : 1];
   uint32_t there;                   // bit j: position j of the lane's rows has a page
 };
 
@@ -958,30 +1049,36 @@ __device__ __forceinline__ int64_t half_base(const PagedPages& pg, const Ctx& x,
   return row_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
 }
 
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TileAt<WIDE>& at,
-                                       Tile<E4M3>& t) {
+                                       Tile<KIND>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
+    const int page = max(at.page[i], 0), row = min(at.first[i] + r, x.n - 1);
     if constexpr (WIDE)
       t.k[i].load_lines(pg.k + half_base(pg, x, at, i), pg.row_bytes, at.cap[i], g, r);
     else
-      t.k[i].load(
-          pg.k + row_offset(pg, max(at.page[i], 0), x.h, min(at.first[i] + r, x.n - 1)), g);
+      t.k[i].load(pg.k + row_offset(pg, page, x.h, row), g);
+    if (KIND == Kind::kE2M1) t.k[i].e = pg.k_exps[4 * exp_offset(pg, page, x.h, row) + g];
   }
 }
 
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TileAt<WIDE>& at,
-                                       Tile<E4M3>& t) {
+                                       Tile<KIND>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
   t.there = 0;
   if constexpr (WIDE) {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       if (at.page[i] >= 0) t.there |= 15u << (4 * i);
-      if (E4M3) {  // four positions' bytes at once: rows of one page, a multiple of 4
+      if (KIND == Kind::kE2M1) {  // four positions' words at once
+        const uint4 e = *reinterpret_cast<const uint4*>(
+            pg.v_exps + 4 * (exp_offset(pg, max(at.page[i], 0), x.h, at.first[i]) + 4 * g));
+        t.ve[4 * i] = e.x, t.ve[4 * i + 1] = e.y, t.ve[4 * i + 2] = e.z, t.ve[4 * i + 3] = e.w;
+      }
+      if (KIND == Kind::kE4M3) {  // four positions' bytes at once: rows of one page, a multiple of 4
         const int64_t e = exp_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
         t.ke[i] = *reinterpret_cast<const uint32_t*>(pg.k_exps + e + 4 * g);
         t.ve[i] = *reinterpret_cast<const uint32_t*>(pg.v_exps + e + 4 * g);
@@ -992,16 +1089,20 @@ __device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       if (at.v_page[j] >= 0) t.there |= 1u << j;
-      if (E4M3) {
+      if (KIND != Kind::kBf16) {
         const int pos = min(at.first[j >> 2] + 4 * g + (j & 3), x.n - 1);
         const int64_t e = exp_offset(pg, max(at.v_page[j], 0), x.h, pos);
-        ke[j] = pg.k_exps[e];
-        ve[j] = pg.v_exps[e];
+        if (KIND == Kind::kE2M1) {
+          t.ve[j] = reinterpret_cast<const uint32_t*>(pg.v_exps)[e];
+        } else {
+          ke[j] = pg.k_exps[e];
+          ve[j] = pg.v_exps[e];
+        }
       }
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      if (E4M3) {
+      if (KIND == Kind::kE4M3) {
         t.ke[i] = ke[4 * i] | ke[4 * i + 1] << 8 | ke[4 * i + 2] << 16 | ke[4 * i + 3] << 24;
         t.ve[i] = ve[4 * i] | ve[4 * i + 1] << 8 | ve[4 * i + 2] << 16 | ve[4 * i + 3] << 24;
       }
@@ -1015,7 +1116,9 @@ __device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const
     else
       p = pg.v + row_offset(pg, max(at.v_page[j], 0), x.h, min(at.first[i] + row, x.n - 1));
     uint32_t* v = t.v[j];
-    if (E4M3) {
+    if constexpr (KIND == Kind::kE2M1) {
+      v[0] = ld4_nt(p + 4 * r);
+    } else if constexpr (KIND == Kind::kE4M3) {
       const uint2 w = ld8_nt(p + 8 * r);
       v[0] = w.x, v[1] = w.y;
     } else {
@@ -1032,8 +1135,8 @@ __device__ __forceinline__ float scaled(float x, uint32_t w, int j) {
 
 // Logits of a step for query row r: lg[j] at position p0 + 16 (j / 4) + 4g +
 // j % 4, before the scale.
-template <bool E4M3, bool WIDE>
-__device__ __forceinline__ void tile_logits(Tile<E4M3>& t, const bf16x8* q, float* lg) {
+template <Kind KIND, bool WIDE>
+__device__ __forceinline__ void tile_logits(Tile<KIND>& t, const bf16x8* q, float* lg) {
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     if (WIDE) t.k[i].swap_halves(threadIdx.x & 15);
@@ -1048,21 +1151,25 @@ __device__ __forceinline__ void tile_logits(Tile<E4M3>& t, const bf16x8* q, floa
 
 // Positions that the query row does not see, or that are not there: logits of
 // -inf, V rows of zeros (what was read in their place may be anything).
-template <bool E4M3>
-__device__ __forceinline__ void tile_mask(Tile<E4M3>& t, int p0, int limit, float* lg) {
+template <Kind KIND>
+__device__ __forceinline__ void tile_mask(Tile<KIND>& t, int p0, int limit, int n, float* lg) {
   const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     const bool has = t.there >> j & 1u;
-    if (!has || p0 + 16 * (j >> 2) + 4 * g + (j & 3) >= limit) lg[j] = -INFINITY;
+    const int pos = p0 + 16 * (j >> 2) + 4 * g + (j & 3);
+    if (!has || pos >= limit) lg[j] = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < (E4M3 ? 2 : 4); ++i)
+    for (int i = 0; i < Tile<KIND>::kV; ++i)
       if (!has) t.v[j][i] = 0u;
+    // NaN's byte would make zeros NaN, and the words of four positions may be past
+    // the context's end
+    if (KIND == Kind::kE2M1 && (!has || pos >= n)) t.ve[j] = 0u;
   }
 }
 
-template <bool E4M3>
-__device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, float c, const float* lg,
+template <Kind KIND>
+__device__ __forceinline__ void tile_weights(const Tile<KIND>& t, float c, const float* lg,
                                              uint32_t part[3][8], WaveState& st) {
   float top = lg[0];
 #pragma unroll
@@ -1084,7 +1191,7 @@ __device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, float c, const
   for (int j = 0; j < 8; ++j) {
     float p = __builtin_amdgcn_exp2f(fmaf(lg[j], c, less));
     st.l += p;
-    if (E4M3) p = scaled(p, t.ve[j >> 2] ^ 0x80808080u, j & 3);
+    if (KIND == Kind::kE4M3) p = scaled(p, t.ve[j >> 2] ^ 0x80808080u, j & 3);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       part[i][j] = __float_as_uint(p);
@@ -1093,10 +1200,14 @@ __device__ __forceinline__ void tile_weights(const Tile<E4M3>& t, float c, const
   }
 }
 
-template <bool E4M3>
-__device__ __forceinline__ void tile_output(const Tile<E4M3>& t, const uint32_t part[3][8],
+template <Kind KIND>
+__device__ __forceinline__ void tile_output(const Tile<KIND>& t, const uint32_t part[3][8],
                                             WaveState& st) {
   bf16x8 w[3];
+  uint32_t scale[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    scale[j] = KIND == Kind::kE2M1 ? scale_of(t.ve[j], (threadIdx.x & 15) >> 2) : 0u;
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     uint32_t y[4];
@@ -1111,7 +1222,10 @@ __device__ __forceinline__ void tile_output(const Tile<E4M3>& t, const uint32_t 
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       uint32_t lo, hi;  // channels e, e + 1 of two rows
-      if (E4M3) {
+      if constexpr (KIND == Kind::kE2M1) {
+        lo = e2m1_pair_at(t.v[2 * j][0], scale[2 * j], e >> 1);
+        hi = e2m1_pair_at(t.v[2 * j + 1][0], scale[2 * j + 1], e >> 1);
+      } else if constexpr (KIND == Kind::kE4M3) {
         lo = e & 2 ? e4m3_pair<true>(t.v[2 * j][e >> 2]) : e4m3_pair<false>(t.v[2 * j][e >> 2]);
         hi = e & 2 ? e4m3_pair<true>(t.v[2 * j + 1][e >> 2])
                    : e4m3_pair<false>(t.v[2 * j + 1][e >> 2]);
@@ -1132,17 +1246,17 @@ __device__ __forceinline__ void tile_output(const Tile<E4M3>& t, const uint32_t 
   }
 }
 
-template <bool E4M3>
-__device__ __forceinline__ void tile_rest(Tile<E4M3>& t, bool masked, int p, int limit, float c,
-                                          float* lg, WaveState& st) {
-  if (E4M3) {
+template <Kind KIND>
+__device__ __forceinline__ void tile_rest(Tile<KIND>& t, bool masked, int p, int limit, int n,
+                                          float c, float* lg, WaveState& st) {
+  if (KIND == Kind::kE4M3) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) lg[j] = scaled(lg[j], t.ke[j >> 2] ^ 0x80808080u, j & 3);
   }
-  if (masked) tile_mask<E4M3>(t, p, limit, lg);
+  if (masked) tile_mask<KIND>(t, p, limit, n, lg);
   uint32_t part[3][8];
-  tile_weights<E4M3>(t, c, lg, part, st);
-  tile_output<E4M3>(t, part, st);
+  tile_weights<KIND>(t, c, lg, part, st);
+  tile_output<KIND>(t, part, st);
 }
 
 // Whether a step has no page at all (for the whole wave).
@@ -1204,36 +1318,36 @@ __device__ __forceinline__ int with_pages(const PagedPages& pg, const Ctx& x, in
 // the last one can meet the end of a query row's positions (T <= 16 of them are
 // not seen by all); the loop's loads are unconditional, so that each wait is
 // for the rows it needs and not for all that is in flight.
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x, int p, int end,
                                            int limit, float c, const bf16x8* q, WaveState& st) {
   if (p >= end) return;
   const PagedPages& pg = a.pg;
-  Tile<E4M3> t;
+  Tile<KIND> t;
   float lg[8];
   TileAt<WIDE> at = tile_at<WIDE>(pg, x, p);
   p = with_pages<WIDE>(pg, x, p, end, &at);
   if (p >= end) return;
-  load_k<E4M3, WIDE>(pg, x, at, t);
-  load_v<E4M3, WIDE>(pg, x, at, t);
+  load_k<KIND, WIDE>(pg, x, at, t);
+  load_v<KIND, WIDE>(pg, x, at, t);
   int next = p + kPagedStep;
   at = tile_at<WIDE>(pg, x, lookup_at(next, end));
   while (next < end) {
-    tile_logits<E4M3, WIDE>(t, q, lg);
+    tile_logits<KIND, WIDE>(t, q, lg);
     next = with_pages<WIDE>(pg, x, next, end, &at);  // from end on: rows that nobody uses
-    load_k<E4M3, WIDE>(pg, x, at, t);
+    load_k<KIND, WIDE>(pg, x, at, t);
     __builtin_amdgcn_sched_barrier(0);
     const bool masked = WIDE ? t.there != 255u : __any(t.there != 255u);
-    tile_rest<E4M3>(t, masked, p, limit, c, lg, st);
+    tile_rest<KIND>(t, masked, p, limit, x.n, c, lg, st);
     __builtin_amdgcn_sched_barrier(0);
-    load_v<E4M3, WIDE>(pg, x, at, t);
+    load_v<KIND, WIDE>(pg, x, at, t);
     p = next;
     next += kPagedStep;
     at = tile_at<WIDE>(pg, x, lookup_at(next, end));
   }
   if (p >= end) return;
-  tile_logits<E4M3, WIDE>(t, q, lg);
-  tile_rest<E4M3>(t, true, p, limit, c, lg, st);
+  tile_logits<KIND, WIDE>(t, q, lg);
+  tile_rest<KIND>(t, true, p, limit, x.n, c, lg, st);
 }
 
 __device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h, int row) {
@@ -1252,7 +1366,7 @@ __device__ __forceinline__ float log_sum(float M, float L) {
 
 // One piece: positions [step, step + take) * kPagedStep of unit (b, h), the four
 // waves' states left in lds.
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __device__ __forceinline__ void attn_piece(const PagedAttnArgs& a, int b, int h, int n, int step,
                                            int take, PagedAttnLds& lds) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -1260,21 +1374,21 @@ __device__ __forceinline__ void attn_piece(const PagedAttnArgs& a, int b, int h,
   const int rows = a.T << a.lg;
   // e4m3 exponents are taken less 128: one power of two more in the logits'
   // factor and, at the end, in the sums of V
-  const float c = a.scale * (E4M3 ? 2.f : 1.f) * 1.4426950408889634f;
+  const float c = a.scale * (KIND == Kind::kE4M3 ? 2.f : 1.f) * 1.4426950408889634f;
   const Ctx x = {b, h, n, table_of(a.pg, b)};
   const int64_t qrow = out_row(a, b, h, r);
   const int limit = r < rows ? n - (a.T - 1 - (r >> a.lg)) : 0;
   bf16x8 q[4];
 #pragma unroll
   for (int f = 0; f < 4; ++f)
-    q[f] = as_bf16x8(r < rows ? ld16(a.q + qrow * kD + frag_base<E4M3>(f, g))
+    q[f] = as_bf16x8(r < rows ? ld16(a.q + qrow * kD + frag_base<KIND>(f, g))
                               : make_uint4(0u, 0u, 0u, 0u));
   WaveState st;
   st.m = -INFINITY;
   st.l = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  attn_steps<E4M3, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
+  attn_steps<KIND, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
                          min((step + take) * kPagedStep, n), limit, c, q, st);
   st.l += __shfl_xor(st.l, 16);
   st.l += __shfl_xor(st.l, 32);
@@ -1287,7 +1401,7 @@ __device__ __forceinline__ void attn_piece(const PagedAttnArgs& a, int b, int h,
     for (int j = 0; j < 4; ++j) {
       float* o = &lds.o[wave][r][8 * (4 * g + j)];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[e] = E4M3 ? 2.f * st.o[e][j] : st.o[e][j];
+      for (int e = 0; e < 8; ++e) o[e] = KIND == Kind::kE4M3 ? 2.f * st.o[e][j] : st.o[e][j];
     }
   }
   __syncthreads();
@@ -1346,7 +1460,7 @@ __device__ __forceinline__ void store_empty(const PagedAttnArgs& a, int64_t firs
 // 128 (6.0), of which the join is 6 to 8.  128 units of 16384 positions, pages of
 // 64, 16, 8, 4, 2 and 1: e4m3 93, 97, 113, 114, 123 and 148 us, bf16 172, 174, 182,
 // 185, 190 and 204.
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, w = blockIdx.x, rows = a.T << a.lg;
@@ -1359,7 +1473,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
   while (at < rg.s1) {
     const int b = rg.b, h = rg.h, step = rg.step, steps = rg.steps;
     const int take = (int)min((int64_t)(steps - step), rg.s1 - at);
-    attn_piece<E4M3, WIDE>(a, b, h, lens(b), step, take, lds);
+    attn_piece<KIND, WIDE>(a, b, h, lens(b), step, take, lds);
     const int slot = at == rg.s0 ? 0 : 1;
     for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
       const int row = i >> 5, d = 4 * (i & 31);
@@ -1486,7 +1600,7 @@ struct JoinFlag {
   __device__ __forceinline__ void pause() const { __builtin_amdgcn_s_sleep(2); }
 };
 
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, rows = a.T << a.lg;
@@ -1500,7 +1614,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
         store_empty(a, out_row(a, b, h, t << a.lg), (int64_t)1 << a.lg);
     return;
   }
-  attn_piece<E4M3, WIDE>(a, b, h, n, piece << a.piece, 1 << a.piece, lds);
+  attn_piece<KIND, WIDE>(a, b, h, n, piece << a.piece, 1 << a.piece, lds);
   const bool last = piece == pieces - 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * rows * kPartStride;
   for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
@@ -1629,6 +1743,14 @@ __global__ __launch_bounds__(256) void k_paged_check(PagedCheckArgs a) {
 }
 
 // ---- launchers ---------------------------------------------------------------------------
+// fn with the kind as a constant.
+template <class Fn>
+static void of_kind(Kind kind, Fn fn) {
+  if (kind == Kind::kBf16) fn(std::integral_constant<Kind, Kind::kBf16>{});
+  else if (kind == Kind::kE4M3) fn(std::integral_constant<Kind, Kind::kE4M3>{});
+  else fn(std::integral_constant<Kind, Kind::kE2M1>{});
+}
+
 static inline int grid_for(int64_t n, int per, int cap) {
   const int64_t b = (n + per - 1) / per;
   return (int)std::max<int64_t>(1, std::min<int64_t>(b, cap));
@@ -1657,75 +1779,73 @@ hipError_t launch_rope(const RopeArgs& a, hipStream_t s) {
   return launch_status();
 }
 
-template <bool E4M3, Turn TURN>
+template <Kind KIND, Turn TURN>
 static void launch_write_t(const PagedWriteArgs& a, hipStream_t s) {
   const int per = rope_per(a.rope.tokens);
-  launch_kernel(CKV_K_PAGED_WRITE, k_paged_write<E4M3, TURN>,
+  launch_kernel(CKV_K_PAGED_WRITE, k_paged_write<KIND, TURN>,
                 dim3((a.rope.tokens + per - 1) / per), dim3(kRopeThreads), s, a, per);
 }
 
-template <bool E4M3>
+template <Kind KIND>
 static void launch_write_e(const PagedWriteArgs& a, hipStream_t s) {
   const RopeSpec& r = a.rope.r;
-  if (!r.inv_freq) launch_write_t<E4M3, Turn::kNone>(a, s);
-  else if (!rope_whole<uint16_t>(r.rot, r.layout)) launch_write_t<E4M3, Turn::kEach>(a, s);
-  else if (r.layout == CKV_ROPE_HALF) launch_write_t<E4M3, Turn::kHalf>(a, s);
-  else launch_write_t<E4M3, Turn::kPairs>(a, s);
+  if (!r.inv_freq) launch_write_t<KIND, Turn::kNone>(a, s);
+  else if (!rope_whole<uint16_t>(r.rot, r.layout)) launch_write_t<KIND, Turn::kEach>(a, s);
+  else if (r.layout == CKV_ROPE_HALF) launch_write_t<KIND, Turn::kHalf>(a, s);
+  else launch_write_t<KIND, Turn::kPairs>(a, s);
 }
 
-hipError_t launch_paged_write(const PagedWriteArgs& a, bool e4m3, hipStream_t s) {
-  e4m3 ? launch_write_e<true>(a, s) : launch_write_e<false>(a, s);
+hipError_t launch_paged_write(const PagedWriteArgs& a, Kind kind, hipStream_t s) {
+  of_kind(kind, [&](auto k) { launch_write_e<k.value>(a, s); });
   return launch_status();
 }
 
-hipError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, hipStream_t s) {
+hipError_t launch_paged_read(const PagedReadArgs& a, Kind kind, hipStream_t s) {
   PagedReadArgs r = a;
   r.chunks = (a.k + kReadSlots - 1) / kReadSlots;
   const dim3 grid((unsigned)(a.units * r.chunks)), block(kPagedReadThreads);
-  if (e4m3) launch_kernel(CKV_K_PAGED_READ, k_paged_read<true>, grid, block, s, r);
-  else launch_kernel(CKV_K_PAGED_READ, k_paged_read<false>, grid, block, s, r);
+  of_kind(kind, [&](auto k) {
+    launch_kernel(CKV_K_PAGED_READ, k_paged_read<k.value>, grid, block, s, r);
+  });
   return launch_status();
 }
 
-template <bool E4M3, bool WIDE>
+template <Kind KIND, bool WIDE>
 static void launch_score_g(const PagedScoreArgs& a, int G, hipStream_t s) {
   const dim3 grid(a.nwg), block(kPagedScoreThreads);
   switch (G) {
-    case 1: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 1>, grid, block, s, a); break;
-    case 2: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 2>, grid, block, s, a); break;
-    case 4: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 4>, grid, block, s, a); break;
-    case 8: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 8>, grid, block, s, a); break;
-    default: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<E4M3, WIDE, 16>, grid, block, s, a);
+    case 1: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<KIND, WIDE, 1>, grid, block, s, a); break;
+    case 2: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<KIND, WIDE, 2>, grid, block, s, a); break;
+    case 4: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<KIND, WIDE, 4>, grid, block, s, a); break;
+    case 8: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<KIND, WIDE, 8>, grid, block, s, a); break;
+    default: launch_kernel(CKV_K_PAGED_SCORE, k_paged_score<KIND, WIDE, 16>, grid, block, s, a);
   }
 }
 
-hipError_t launch_paged_score(const PagedScoreArgs& a, bool e4m3, int G, hipStream_t s) {
-  const bool wide = a.pg.shift >= 4;
-  if (e4m3) wide ? launch_score_g<true, true>(a, G, s) : launch_score_g<true, false>(a, G, s);
-  else wide ? launch_score_g<false, true>(a, G, s) : launch_score_g<false, false>(a, G, s);
+hipError_t launch_paged_score(const PagedScoreArgs& a, Kind kind, int G, hipStream_t s) {
+  of_kind(kind, [&](auto k) {
+    if (a.pg.shift >= 4) launch_score_g<k.value, true>(a, G, s);
+    else launch_score_g<k.value, false>(a, G, s);
+  });
   return launch_status();
 }
 
-hipError_t launch_paged_attn(const PagedAttnArgs& a, bool e4m3, hipStream_t s) {
-  const bool wide = a.pg.shift >= 4;
+template <Kind KIND, bool WIDE>
+static void launch_attn_t(const PagedAttnArgs& a, hipStream_t s) {
   const dim3 grid(a.nwg), block(kPagedAttnThreads);
-  if (a.chunks) {
-    if (e4m3 && wide)
-      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<true, true>, grid, block, s, a);
-    else if (e4m3)
-      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<true, false>, grid, block, s, a);
-    else if (wide)
-      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<false, true>, grid, block, s, a);
-    else
-      launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<false, false>, grid, block, s, a);
-    return launch_status();
-  }
-  if (e4m3 && wide) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<true, true>, grid, block, s, a);
-  else if (e4m3) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<true, false>, grid, block, s, a);
-  else if (wide) launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<false, true>, grid, block, s, a);
-  else launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<false, false>, grid, block, s, a);
+  if (a.chunks)
+    launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn_direct<KIND, WIDE>, grid, block, s, a);
+  else
+    launch_kernel(CKV_K_PAGED_ATTN, k_paged_attn<KIND, WIDE>, grid, block, s, a);
+}
+
+hipError_t launch_paged_attn(const PagedAttnArgs& a, Kind kind, hipStream_t s) {
+  of_kind(kind, [&](auto k) {
+    if (a.pg.shift >= 4) launch_attn_t<k.value, true>(a, s);
+    else launch_attn_t<k.value, false>(a, s);
+  });
   const hipError_t e = launch_status();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.chunks) return e;
   launch_kernel(CKV_K_PAGED_MERGE, k_paged_merge, dim3(a.nwg, a.T << a.lg),
                 dim3(kPagedMergeThreads), s, a);
   return launch_status();

@@ -3,16 +3,21 @@
 #pragma once
 
 #include <algorithm>
+#include <type_traits>
 
 #include "ckv_check.hpp"
 
 namespace ckv {
 
+// ckv_cache_kind.
+enum class Kind { kBf16 = CKV_CACHE_BF16, kE4M3 = CKV_CACHE_E4M3, kE2M1 = CKV_CACHE_E2M1 };
+constexpr int kExpGroup = 32;  // elements of an e2m1 row that share an exponent
+
 // Pages as the kernels see them: byte strides, sizes as shifts.
 struct PagedPages {
   uint8_t* k;
   uint8_t* v;
-  uint8_t* k_exps;        // [num_pages][Hkv][page_size], e4m3 only
+  uint8_t* k_exps;        // [num_pages][Hkv][page_size] (e4m3), ... [4] (e2m1)
   uint8_t* v_exps;
   const int32_t* table;   // [B][table_stride]
   int64_t page_bytes, head_bytes;
@@ -216,10 +221,10 @@ __host__ __device__ inline unsigned paged_check_item(const PagedCheckArgs& a, in
 }
 
 hipError_t launch_rope(const RopeArgs& a, hipStream_t s);
-hipError_t launch_paged_write(const PagedWriteArgs& a, bool e4m3, hipStream_t s);
-hipError_t launch_paged_read(const PagedReadArgs& a, bool e4m3, hipStream_t s);
-hipError_t launch_paged_score(const PagedScoreArgs& a, bool e4m3, int G, hipStream_t s);
-hipError_t launch_paged_attn(const PagedAttnArgs& a, bool e4m3, hipStream_t s);
+hipError_t launch_paged_write(const PagedWriteArgs& a, Kind kind, hipStream_t s);
+hipError_t launch_paged_read(const PagedReadArgs& a, Kind kind, hipStream_t s);
+hipError_t launch_paged_score(const PagedScoreArgs& a, Kind kind, int G, hipStream_t s);
+hipError_t launch_paged_attn(const PagedAttnArgs& a, Kind kind, hipStream_t s);
 hipError_t launch_paged_check(const PagedCheckArgs& a, hipStream_t s);
 
 inline int check_tokens(const Dims& d, int32_t tokens) {
