@@ -71,8 +71,8 @@ extern "C" {
 #endif
 
 /* Changes where an existing entry, structure or value does.  Version 9 has gained
- * entries since (the rotary positions and the paged cache): a library without them
- * lacks their symbols. */
+ * entries since (the rotary positions, the paged cache and the attention over
+ * selected blocks) and a cache kind: a library without them lacks their symbols. */
 #define CKV_ABI_VERSION 9
 
 typedef enum ckv_status {
@@ -558,6 +558,63 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
                           float scale, float* out, float* lse, void* ws, size_t ws_bytes,
                           void* stream);
 
+/* ---- attention over selected blocks ------------------------------------------
+ * Sparse attention of many query tokens (a prefill's chunk, or a decode step's)
+ * over a paged cache of any kind.  Positions are taken in blocks of `block` (32, 64,
+ * 128 or 256): block j holds positions [j * block, (j + 1) * block), nb =
+ * ceil(max_ctx / block) of them.  Every query token keeps, for each KV head, its own
+ * block and the k - 1 earlier blocks whose landmarks score best (Sec. 2.2 chunk
+ * landmarks, one set per GQA group, selected per query token).  1 <= k <= 64;
+ * pages of at least 16 positions (CKV_EUNSUPPORTED otherwise).
+ *   Query token t (0 <= t < num_tokens <= 2^24) is position positions[t] of request
+ * requests[t] (NULL: request t), its query row q[t] of [num_tokens][Hq][d] bf16; a
+ * token whose position is outside [0, max_ctx) (-1: padding) or whose request is
+ * outside [0, B) keeps nothing and gets out = 0 and lse = -inf.  Tokens may come in
+ * any order; neighbours of one request next to each other share the reading of the
+ * blocks that both keep.
+ *
+ * ckv_paged_landmarks: landmarks [B][Hkv][nb][d] bf16, of block j the mean of the
+ * keys at its positions below n_b that are there, summed in fp64 and rounded once
+ * (NaN or infinite sums: NaN).  Only the blocks from first[b] / block on (first NULL:
+ * from 0 on) that have such a position are written, so that a step renews what its
+ * new tokens touched. */
+int ckv_paged_landmarks(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t block,
+                        const int32_t* ctx_lens, const int32_t* first, uint16_t* landmarks,
+                        void* stream);
+
+/* Selects the blocks of every query token: idx [num_tokens][Hkv][k] int32, ascending,
+ * then -1.  With o = positions[t] / block, the last one is o; the others are the
+ * blocks j < o that have a page and the largest
+ *   max over the G heads g of h's group of sum_c q[t][h*G+g][c] * landmarks[r][h][j][c],
+ * equal ones the lower block first.  The set is that of the exact sums (fp32 sums
+ * decide, those within their error of the last place are summed again in fp64);
+ * landmarks whose score is NaN or -inf are not selected.  Landmarks of blocks from o
+ * on are not read.  ws: ckv_blocks_workspace_bytes. */
+int ckv_select_blocks(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t block,
+                      int32_t k, int32_t num_tokens, const int32_t* requests,
+                      const int32_t* positions, const uint16_t* q, const uint16_t* landmarks,
+                      int32_t* idx, void* ws, size_t ws_bytes, void* stream);
+
+/* Attention of every query token over the positions p <= positions[t] of the blocks
+ * idx [num_tokens][Hkv][k] (ascending, -1 and blocks past its own are passed over)
+ * that are there:
+ *   l_p = scale * q[t][g] . K_p,  out[t][g] = sum_p softmax(l)_p V_p,
+ *   lse[t][g] = log sum_p exp(l_p)       (natural logarithm; may be NULL)
+ * out [num_tokens][Hq][d] fp32, lse [num_tokens][Hq] fp32; nothing to attend to:
+ * out = 0, lse = -inf.  Logits, weights and sums are fp32; 0 < scale <= 2^126.  The
+ * same call gives the same bits.  Rows at positions up to the tokens' own are written
+ * before.  ws: ckv_blocks_workspace_bytes. */
+int ckv_paged_block_attn(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t block,
+                         int32_t k, int32_t num_tokens, const int32_t* requests,
+                         const int32_t* positions, const uint16_t* q, const int32_t* idx,
+                         float scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                         void* stream);
+
+/* Bytes of the workspace that serves both calls with these sizes (4 a token, KV head
+ * and block of max_ctx, and little more, or at most 4.2 MiB of partial sums). */
+int ckv_blocks_workspace_bytes(const ckv_shape* shape, int32_t block, int32_t k,
+                               int32_t num_tokens, size_t* bytes);
+
 /* ---- layer pipeline --------------------------------------------------------
  * The decode loop of Sec. 5.3 (layer-aware transfer overlap) and Sec. 5.4
  * (two-layer ping-pong buffer): the set selected for a layer at step t-1 is
@@ -726,7 +783,12 @@ typedef enum ckv_kernel_id {
   CKV_K_PAGED_SCORE = 19, /* scores of paged keys                           */
   CKV_K_PAGED_ATTN = 20,  /* attention over a paged cache, by ranges        */
   CKV_K_PAGED_MERGE = 21, /* join of the ranges that share a unit           */
-  CKV_K_TOTAL = 22        /* all classes (ckv_profile_end_n)                */
+  CKV_K_BLOCK_MARKS = 22, /* landmarks of a paged cache's blocks            */
+  CKV_K_BLOCK_SCORE = 23, /* scores of landmarks for many query tokens      */
+  CKV_K_BLOCK_SELECT = 24, /* each token's blocks                           */
+  CKV_K_BLOCK_ATTN = 25,  /* attention over selected blocks                 */
+  CKV_K_BLOCK_MERGE = 26, /* join of a tile's pieces                        */
+  CKV_K_TOTAL = 27        /* all classes (ckv_profile_end_n)                */
 } ckv_kernel_id;
 
 #define CKV_K_ALL ((1u << CKV_K_COUNT) - 1u)     /* those of ckv_profile_end */

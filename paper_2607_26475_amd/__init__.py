@@ -14,7 +14,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import Optional, Tuple
 
 import torch
 
@@ -34,7 +34,8 @@ __all__ = [
     "ROPE_HALF", "ROPE_INTERLEAVED", "ROPE_BF16", "ROPE_F32", "ROPE_PLAIN", "ROPE_LINEAR",
     "ROPE_BASE", "ROPE_BANDS", "ROPE_RAMP", "PagedCache", "paged_cache_for", "paged_write",
     "paged_read", "paged_score_keys", "paged_decode_attn", "CACHE_BF16", "CACHE_E4M3",
-    "ENTRY_PAGED_DECODE_ATTN",
+    "CACHE_E2M1", "ENTRY_PAGED_DECODE_ATTN", "paged_landmarks", "select_blocks",
+    "paged_block_attn", "blocks_workspace", "blocks_workspace_bytes",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libckv.so")
@@ -59,8 +60,9 @@ EXPORTS = ("ckv_abi_version", "ckv_status_str", "ckv_last_error_detail",
            "ckv_decode_step", "ckv_probe_read_rows", "ckv_probe_sink_words", "ckv_set_debug",
            "ckv_set_one_launch_same_step", "ckv_rope_rows", "ckv_rope_frequencies",
            "ckv_paged_write", "ckv_paged_read", "ckv_paged_score_keys",
-           "ckv_paged_decode_attn")
-KERNEL_COUNT = 22
+           "ckv_paged_decode_attn", "ckv_paged_landmarks", "ckv_select_blocks",
+           "ckv_paged_block_attn", "ckv_blocks_workspace_bytes")
+KERNEL_COUNT = 27
 MAX_RANK = 4096
 ABI_VERSION = 9  # CKV_ABI_VERSION of include/ckv.h that this binding marshals for
 
@@ -188,6 +190,14 @@ def _load() -> ctypes.CDLL:
                                                 ctypes.c_float, vp, vp]),
         "ckv_paged_decode_attn": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), i32, vp, vp,
                                                  ctypes.c_float, vp, vp, vp, sz, vp]),
+        "ckv_paged_landmarks": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), i32, vp, vp, vp,
+                                               vp]),
+        "ckv_select_blocks": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), i32, i32, i32, vp,
+                                             vp, vp, vp, vp, vp, sz, vp]),
+        "ckv_paged_block_attn": (ctypes.c_int, [sp, ctypes.POINTER(PagedCache), i32, i32, i32,
+                                                vp, vp, vp, vp, ctypes.c_float, vp, vp, vp, sz,
+                                                vp]),
+        "ckv_blocks_workspace_bytes": (ctypes.c_int, [sp, i32, i32, i32, ctypes.POINTER(sz)]),
         "ckv_probe_read_rows": (ctypes.c_int, [sp, vp, vp, vp, i32, ctypes.c_int, vp, sz, vp]),
         "ckv_probe_sink_words": (sz, [sp, i32, ctypes.c_int]),
         "ckv_set_debug": (ctypes.c_int, [ctypes.c_int]),
@@ -629,11 +639,89 @@ def paged_decode_attn(shape: Shape, cache: PagedCache, num_tokens: int, q: torch
           ws.numel() if ws is not None else 0)
 
 
+# ---- attention over selected blocks -----------------------------------------------------
+def blocks_workspace_bytes(shape: Shape, block: int, k: int, num_tokens: int) -> int:
+    out = ctypes.c_size_t(0)
+    _check("ckv_blocks_workspace_bytes", _lib.ckv_blocks_workspace_bytes(
+        ctypes.byref(shape), block, k, num_tokens, ctypes.byref(out)))
+    return int(out.value)
+
+
+def blocks_workspace(shape: Shape, block: int, k: int, num_tokens: int,
+                     device="cuda") -> torch.Tensor:
+    """A workspace for ``select_blocks`` and ``paged_block_attn`` of these sizes."""
+    return torch.empty(max(256, blocks_workspace_bytes(shape, block, k, num_tokens)),
+                       dtype=torch.uint8, device=device)
+
+
+def paged_landmarks(shape: Shape, cache: PagedCache, block: int, ctx_lens: torch.Tensor,
+                    landmarks: torch.Tensor, first: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+    """Mean keys of the cache's blocks into landmarks [B][Hkv][ceil(max_ctx /
+    block)][128] bf16, from position first[b]'s block on (None: all)."""
+    dev = ctx_lens.get_device()
+    _cache_ok(shape, cache, dev)
+    _dense("ctx_lens", ctx_lens, torch.int32, shape.batch, dev)
+    if first is not None:
+        _dense("first", first, torch.int32, shape.batch, dev)
+    _dense("landmarks", landmarks, torch.bfloat16, _marks(shape, block), dev)
+    _call(_lib.ckv_paged_landmarks, dev, stream, shape, cache, block, ctx_lens.data_ptr(),
+          _ptr(first), landmarks.data_ptr())
+
+
+def _marks(shape: Shape, block: int) -> int:
+    return shape.batch * shape.num_kv_heads * -(-shape.max_ctx // max(block, 1)) * 128
+
+
+def _tokens_ok(shape: Shape, cache: PagedCache, requests, positions: torch.Tensor,
+               q: torch.Tensor) -> Tuple[int, int]:
+    n, dev = positions.numel(), positions.get_device()
+    _cache_ok(shape, cache, dev)
+    _dense("positions", positions, torch.int32, n, dev)
+    if requests is not None:
+        _dense("requests", requests, torch.int32, n, dev)
+    _dense("q", q, torch.bfloat16, n * shape.num_q_heads * 128, dev)
+    return n, dev
+
+
+def select_blocks(shape: Shape, cache: PagedCache, block: int, k: int, requests,
+                  positions: torch.Tensor, q: torch.Tensor, landmarks: torch.Tensor,
+                  idx: torch.Tensor, ws: torch.Tensor, stream=None) -> None:
+    """Each query token's blocks for each KV head into idx [tokens][Hkv][k]: its
+    own and the k - 1 best earlier ones by their landmarks (requests None: token t
+    is request t's; q [tokens][Hq][128])."""
+    n, dev = _tokens_ok(shape, cache, requests, positions, q)
+    _dense("landmarks", landmarks, torch.bfloat16, _marks(shape, block), dev)
+    _dense("idx", idx, torch.int32, n * shape.num_kv_heads * k, dev)
+    _dense("ws", ws, torch.uint8, 0, dev)
+    _call(_lib.ckv_select_blocks, dev, stream, shape, cache, block, k, n, _ptr(requests),
+          positions.data_ptr(), q.data_ptr(), landmarks.data_ptr(), idx.data_ptr(),
+          ws.data_ptr(), ws.numel())
+
+
+def paged_block_attn(shape: Shape, cache: PagedCache, block: int, k: int, requests,
+                     positions: torch.Tensor, q: torch.Tensor, idx: torch.Tensor, scale: float,
+                     out: torch.Tensor, lse: Optional[torch.Tensor], ws: torch.Tensor,
+                     stream=None) -> None:
+    """Attention of each query token over the blocks idx [tokens][Hkv][k] up to
+    its own position, into out [tokens][Hq][128] fp32 and, unless None, lse."""
+    n, dev = _tokens_ok(shape, cache, requests, positions, q)
+    _dense("idx", idx, torch.int32, n * shape.num_kv_heads * k, dev)
+    _dense("out", out, torch.float32, n * shape.num_q_heads * 128, dev)
+    if lse is not None:
+        _dense("lse", lse, torch.float32, n * shape.num_q_heads, dev)
+    _dense("ws", ws, torch.uint8, 0, dev)
+    _call(_lib.ckv_paged_block_attn, dev, stream, shape, cache, block, k, n, _ptr(requests),
+          positions.data_ptr(), q.data_ptr(), idx.data_ptr(), scale, out.data_ptr(), _ptr(lse),
+          ws.data_ptr(), ws.numel())
+
+
 KERNEL_IDS = {"zero": 0, "score": 1, "hist": 2, "filter": 3, "finish": 4, "attn": 5,
               "combine": 6, "dual": 7, "gather": 8, "miss": 9, "landmarks": 10,
               "expand": 11, "reconstruct": 12, "select_attn": 13, "probe": 14,
               "critical": 15, "rope": 16, "paged_write": 17, "paged_read": 18,
-              "paged_score": 19, "paged_attn": 20, "paged_merge": 21}
+              "paged_score": 19, "paged_attn": 20, "paged_merge": 21, "block_marks": 22,
+              "block_score": 23, "block_select": 24, "block_attn": 25, "block_merge": 26}
 
 
 def profile_begin(kernels=None, every: int = 1) -> None:

@@ -1541,23 +1541,6 @@ __global__ __launch_bounds__(kAttnThreads) void k_combine(AttnArgs a) {
 }
 
 // ---- chunk landmarks -----------------------------------------------------------
-// Nearest bf16 to x, ties to the even significand, from the binary64 fields:
-// normal results keep 7 of the 52 stored significand bits; below the
-// smallest normal bf16 (2^-126) the quantum is 2^-133.
-__device__ __forceinline__ uint16_t f64_to_bf16_rne(double x) {
-  uint64_t b = (uint64_t)__double_as_longlong(x);
-  const uint16_t sign = (uint16_t)((b >> 48) & 0x8000u);
-  b &= 0x7fffffffffffffffull;
-  if (b == 0) return sign;
-  if ((int)(b >> 52) < 1023 - 126) {
-    const double r = rint(__longlong_as_double((long long)b) * 0x1p133);
-    return (uint16_t)(sign | (uint16_t)r);  // r = 128 is the smallest normal
-  }
-  b += 0x00000fffffffffffull + ((b >> 45) & 1u);  // 2^44 - 1 + kept lsb
-  const uint32_t e = (uint32_t)(b >> 52) - 1023u + 127u;
-  return (uint16_t)(sign | (e << 7) | (uint32_t)((b >> 45) & 0x7fu));
-}
-
 // One item = 8 channels of one landmark: the fp64 sum of the chunk's rows
 // below n_b in row order, divided by their count, rounded once to bf16.  A pass
 // over the keys, bound by how much of it is in flight: a thread requests BATCH

@@ -6,6 +6,106 @@
 
 #include "ckv_profile.hpp"
 
+namespace ckv {
+
+int check_num_tokens(int32_t n) {
+  if (n < 0 || n > (1 << 24)) return fail(CKV_ESHAPE, "num_tokens %d outside [0, 2^24]", n);
+  return CKV_OK;
+}
+
+int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p) {
+  if (!c) return fail(CKV_EINVAL, "cache is NULL");
+  if (c->kind != CKV_CACHE_BF16 && c->kind != CKV_CACHE_E4M3 && c->kind != CKV_CACHE_E2M1)
+    return fail(CKV_EINVAL, "bad cache.kind %d", c->kind);
+  void *k_pages = c->k_pages, *v_pages = c->v_pages;
+  const int32_t* page_table = c->page_table;
+  uint8_t *k_exps = c->k_exps, *v_exps = c->v_exps;
+  CKV_PTR(k_pages);
+  CKV_PTR(v_pages);
+  CKV_PTR(page_table);
+  if (c->kind != CKV_CACHE_BF16) {
+    CKV_PTR(k_exps);
+    CKV_PTR(v_exps);
+  } else if (k_exps || v_exps) {
+    return fail(CKV_EINVAL, "a bf16 cache has no exponents");
+  }
+  const int ps = c->page_size;
+  if (ps < 1 || ps > 65536 || (ps & (ps - 1)))
+    return fail(CKV_EUNSUPPORTED, "page_size %d (a power of two up to 65536)", ps);
+  if (c->num_pages < 1) return fail(CKV_ESHAPE, "num_pages %d", c->num_pages);
+  const int64_t slots = ((int64_t)d.max_ctx + ps - 1) / ps;
+  if (c->table_stride < slots)
+    return fail(CKV_ESHAPE, "table_stride %d below the %lld pages of max_ctx", c->table_stride,
+                (long long)slots);
+  // bytes of x elements: x * size / 2
+  const int size = c->kind == CKV_CACHE_BF16 ? 4 : c->kind == CKV_CACHE_E4M3 ? 2 : 1;
+  const int64_t strides[3] = {c->page_stride, c->head_stride, c->row_stride};
+  for (int64_t x : strides)
+    if (x < kD || x > ((int64_t)1 << 36) || x * size % 32)
+      return fail(CKV_ESHAPE, "cache stride %lld (128 .. 2^36 elements, a multiple of 16 bytes)",
+                  (long long)x);
+  if (c->row_stride * size / 2 * ps >= ((int64_t)1 << 31))
+    return fail(CKV_EUNSUPPORTED, "page_size %d rows at stride %lld reach 2^31 bytes", ps,
+                (long long)c->row_stride);
+  int64_t last = 0;
+  if (__builtin_mul_overflow((int64_t)c->num_pages, c->page_stride * size / 2, &last) ||
+      last > ((int64_t)1 << 61))
+    return fail(CKV_ESHAPE, "page_stride %lld times %d pages", (long long)c->page_stride,
+                c->num_pages);
+  p->k = static_cast<uint8_t*>(k_pages);
+  p->v = static_cast<uint8_t*>(v_pages);
+  p->k_exps = k_exps;
+  p->v_exps = v_exps;
+  p->table = page_table;
+  p->page_bytes = c->page_stride * size / 2;
+  p->head_bytes = c->head_stride * size / 2;
+  p->row_bytes = (int32_t)(c->row_stride * size / 2);
+  p->shift = __builtin_ctz((unsigned)ps);
+  p->num_pages = c->num_pages;
+  p->table_stride = c->table_stride;
+  p->Hkv = d.Hkv;
+  return CKV_OK;
+}
+
+int debug_check_paged(hipStream_t s, const PagedPages& pg, const int32_t* ctx_lens,
+                      const int32_t* req, const int32_t* pos, int B, int max_ctx, int tokens,
+                      bool attending) {
+  if (!debug_on()) return CKV_OK;
+  PagedCheckArgs a;
+  a.pg = pg;
+  a.ctx_lens = ctx_lens;
+  a.req = req;
+  a.pos = pos;
+  a.B = B;
+  a.max_ctx = max_ctx;
+  a.tokens = tokens;
+  a.slots = (int32_t)(((int64_t)max_ctx + (1 << pg.shift) - 1) >> pg.shift);
+  unsigned long long got = 0;
+  const int rc = debug_run(
+      s,
+      [&](unsigned long long* flag) {
+        a.flag = flag;
+        return launch_paged_check(a, s);
+      },
+      &got);
+  if (rc) return rc;
+  if (got == ~0ull) return CKV_OK;
+  const unsigned kind = (unsigned)(got >> 56);
+  if (kind == 7 && attending) return CKV_OK;  // the last of the findings
+  const long long item = (long long)(got & ((1ull << 56) - 1));
+  if (kind == 4)
+    return fail(CKV_EINVAL, "debug check: page_table[%lld][%lld] is neither -1 nor below %d",
+                item / a.slots, item % a.slots, pg.num_pages);
+  if (kind == 5)
+    return fail(CKV_EINVAL, "debug check: positions[%lld] is neither -1 nor in [0, %d)", item,
+                max_ctx);
+  if (kind == 6)
+    return fail(CKV_EINVAL, "debug check: requests[%lld] outside [0, %d)", item, B);
+  return fail(CKV_EINVAL, "debug check: token %lld has no page to be written to", item);
+}
+
+}  // namespace ckv
+
 namespace {
 
 using namespace ckv;
@@ -67,108 +167,6 @@ int check_rows(const char* what, const ckv_rows* rows, int32_t tokens, const Rop
   out->heads = rows->heads;
   return CKV_OK;
 }
-
-int check_num_tokens(int32_t n) {
-  if (n < 0 || n > (1 << 24)) return fail(CKV_ESHAPE, "num_tokens %d outside [0, 2^24]", n);
-  return CKV_OK;
-}
-
-int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p) {
-  if (!c) return fail(CKV_EINVAL, "cache is NULL");
-  if (c->kind != CKV_CACHE_BF16 && c->kind != CKV_CACHE_E4M3 && c->kind != CKV_CACHE_E2M1)
-    return fail(CKV_EINVAL, "bad cache.kind %d", c->kind);
-  void *k_pages = c->k_pages, *v_pages = c->v_pages;
-  const int32_t* page_table = c->page_table;
-  uint8_t *k_exps = c->k_exps, *v_exps = c->v_exps;
-  CKV_PTR(k_pages);
-  CKV_PTR(v_pages);
-  CKV_PTR(page_table);
-  if (c->kind != CKV_CACHE_BF16) {
-    CKV_PTR(k_exps);
-    CKV_PTR(v_exps);
-  } else if (k_exps || v_exps) {
-    return fail(CKV_EINVAL, "a bf16 cache has no exponents");
-  }
-  const int ps = c->page_size;
-  if (ps < 1 || ps > 65536 || (ps & (ps - 1)))
-    return fail(CKV_EUNSUPPORTED, "page_size %d (a power of two up to 65536)", ps);
-  if (c->num_pages < 1) return fail(CKV_ESHAPE, "num_pages %d", c->num_pages);
-  const int64_t slots = ((int64_t)d.max_ctx + ps - 1) / ps;
-  if (c->table_stride < slots)
-    return fail(CKV_ESHAPE, "table_stride %d below the %lld pages of max_ctx", c->table_stride,
-                (long long)slots);
-  // bytes of x elements: x * size / 2
-  const int size = c->kind == CKV_CACHE_BF16 ? 4 : c->kind == CKV_CACHE_E4M3 ? 2 : 1;
-  const int64_t strides[3] = {c->page_stride, c->head_stride, c->row_stride};
-  for (int64_t x : strides)
-    if (x < kD || x > ((int64_t)1 << 36) || x * size % 32)
-      return fail(CKV_ESHAPE, "cache stride %lld (128 .. 2^36 elements, a multiple of 16 bytes)",
-                  (long long)x);
-  if (c->row_stride * size / 2 * ps >= ((int64_t)1 << 31))
-    return fail(CKV_EUNSUPPORTED, "page_size %d rows at stride %lld reach 2^31 bytes", ps,
-                (long long)c->row_stride);
-  int64_t last = 0;
-  if (__builtin_mul_overflow((int64_t)c->num_pages, c->page_stride * size / 2, &last) ||
-      last > ((int64_t)1 << 61))
-    return fail(CKV_ESHAPE, "page_stride %lld times %d pages", (long long)c->page_stride,
-                c->num_pages);
-  p->k = static_cast<uint8_t*>(k_pages);
-  p->v = static_cast<uint8_t*>(v_pages);
-  p->k_exps = k_exps;
-  p->v_exps = v_exps;
-  p->table = page_table;
-  p->page_bytes = c->page_stride * size / 2;
-  p->head_bytes = c->head_stride * size / 2;
-  p->row_bytes = (int32_t)(c->row_stride * size / 2);
-  p->shift = __builtin_ctz((unsigned)ps);
-  p->num_pages = c->num_pages;
-  p->table_stride = c->table_stride;
-  p->Hkv = d.Hkv;
-  return CKV_OK;
-}
-
-// Debug mode: the pages that a reading entry (ctx_lens) or a writing entry
-// (req, pos) reaches, checked on the device before its launch.
-int debug_check_paged(hipStream_t s, const PagedPages& pg, const int32_t* ctx_lens,
-                      const int32_t* req, const int32_t* pos, int B, int max_ctx, int tokens) {
-  if (!debug_on()) return CKV_OK;
-  PagedCheckArgs a;
-  a.pg = pg;
-  a.ctx_lens = ctx_lens;
-  a.req = req;
-  a.pos = pos;
-  a.B = B;
-  a.max_ctx = max_ctx;
-  a.tokens = tokens;
-  a.slots = (int32_t)(((int64_t)max_ctx + (1 << pg.shift) - 1) >> pg.shift);
-  unsigned long long got = 0;
-  const int rc = debug_run(
-      s,
-      [&](unsigned long long* flag) {
-        a.flag = flag;
-        return launch_paged_check(a, s);
-      },
-      &got);
-  if (rc) return rc;
-  if (got == ~0ull) return CKV_OK;
-  const unsigned kind = (unsigned)(got >> 56);
-  const long long item = (long long)(got & ((1ull << 56) - 1));
-  if (kind == 4)
-    return fail(CKV_EINVAL, "debug check: page_table[%lld][%lld] is neither -1 nor below %d",
-                item / a.slots, item % a.slots, pg.num_pages);
-  if (kind == 5)
-    return fail(CKV_EINVAL, "debug check: positions[%lld] is neither -1 nor in [0, %d)", item,
-                max_ctx);
-  if (kind == 6)
-    return fail(CKV_EINVAL, "debug check: requests[%lld] outside [0, %d)", item, B);
-  return fail(CKV_EINVAL, "debug check: token %lld has no page to be written to", item);
-}
-
-#define CKV_RC(expr)             \
-  do {                           \
-    const int rc_ = (expr);      \
-    if (rc_) return rc_;         \
-  } while (0)
 
 }  // namespace
 

@@ -227,6 +227,21 @@ hipError_t launch_paged_score(const PagedScoreArgs& a, Kind kind, int G, hipStre
 hipError_t launch_paged_attn(const PagedAttnArgs& a, Kind kind, hipStream_t s);
 hipError_t launch_paged_check(const PagedCheckArgs& a, hipStream_t s);
 
+int check_cache(const ckv_paged_cache* c, const Dims& d, PagedPages* p);
+int check_num_tokens(int32_t n);
+// Debug mode: the pages that a reading entry (ctx_lens) or a writing entry
+// (req, pos) reaches, checked on the device before its launch; attending: tokens
+// need no page.
+int debug_check_paged(hipStream_t s, const PagedPages& pg, const int32_t* ctx_lens,
+                      const int32_t* req, const int32_t* pos, int B, int max_ctx, int tokens,
+                      bool attending = false);
+
+#define CKV_RC(expr)             \
+  do {                           \
+    const int rc_ = (expr);      \
+    if (rc_) return rc_;         \
+  } while (0)
+
 inline int check_tokens(const Dims& d, int32_t tokens) {
   if (tokens < 1 || (int64_t)tokens * d.G > 16)
     return fail(CKV_EUNSUPPORTED, "%d tokens of %d heads a group (1 <= tokens * heads <= 16)",

@@ -98,7 +98,9 @@ const char* ckv_kernel_name(int id) {
                                            "landmarks", "expand", "reconstruct",
                                            "select_attn", "probe", "critical", "rope",
                                            "paged_write", "paged_read", "paged_score",
-                                           "paged_attn", "paged_merge"};
+                                           "paged_attn", "paged_merge", "block_marks",
+                                           "block_score", "block_select", "block_attn",
+                                           "block_merge"};
   return (id >= 0 && id < CKV_K_TOTAL) ? names[id] : "";
 }
 
