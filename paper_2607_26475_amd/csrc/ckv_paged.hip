@@ -884,6 +884,64 @@ __device__ __forceinline__ void attn_steps(const PagedAttnArgs& a, const Ctx& x,
   tile_rest<KIND>(t, true, p, limit, x.n, c, lg, st);
 }
 
+// The same two steps at a time, for the 4-bit kind: a step's rows are few bytes, and
+// loads of one step in flight a wave do not cover the memory's latency (64 sequences
+// of 1 k to 32 k positions 262 -> 237 us, two of 150 k to 200 k 100 -> 91; three
+// workgroups a CU instead of two: 239 and 98).
+template <Kind KIND, bool WIDE>
+__device__ __forceinline__ void attn_pairs(const PagedAttnArgs& a, const Ctx& x, int p, int end,
+                                           int limit, float c, const bf16x8* q, WaveState& st) {
+  if (p >= end) return;
+  const PagedPages& pg = a.pg;
+  Tile<KIND> t[2];
+  TileAt<WIDE> at[2];
+  at[0] = tile_at<WIDE>(pg, x, p);
+  p = with_pages<WIDE>(pg, x, p, end, &at[0]);
+  if (p >= end) return;
+  limit = min(limit, end);  // the second step of a pair may lie past the piece
+  at[1] = tile_at<WIDE>(pg, x, lookup_at(p + kPagedStep, end));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    load_k<KIND, WIDE>(pg, x, at[i], t[i]);
+    load_v<KIND, WIDE>(pg, x, at[i], t[i]);
+  }
+  int next = p + 2 * kPagedStep;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) at[i] = tile_at<WIDE>(pg, x, lookup_at(next + i * kPagedStep, end));
+  while (p < end) {
+    float lg[2][8];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) tile_logits<KIND, WIDE>(t[i], q, lg[i]);
+    const int to = with_pages<WIDE>(pg, x, next, end, &at[0]);
+    if (to != next) at[1] = tile_at<WIDE>(pg, x, lookup_at(to + kPagedStep, end));
+    next = to;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_k<KIND, WIDE>(pg, x, at[i], t[i]);
+    __builtin_amdgcn_sched_barrier(0);
+    const uint32_t all = t[0].there & t[1].there;
+    if (next >= end || (WIDE ? all != 255u : __any(all != 255u))) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        tile_mask<KIND>(t[i], p + i * kPagedStep, limit, x.n, lg[i]);
+    }
+    raise_max(fmaxf(top_of(lg[0]), top_of(lg[1])), c, st);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t part[3][8];
+      tile_weights<KIND>(t[i].ve, c, lg[i], part, st);
+      tile_output<KIND>(t[i], part, st);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load_v<KIND, WIDE>(pg, x, at[i], t[i]);
+    p = next;
+    next += 2 * kPagedStep;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      at[i] = tile_at<WIDE>(pg, x, lookup_at(next + i * kPagedStep, end));
+  }
+}
+
 __device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h, int row) {
   const int t = row >> a.lg, g = row & ((1 << a.lg) - 1);
   return ((int64_t)b * a.T + t) * a.Hq + (h << a.lg) + g;
@@ -891,7 +949,7 @@ __device__ __forceinline__ int64_t out_row(const PagedAttnArgs& a, int b, int h,
 
 // One piece: positions [step, step + take) * kPagedStep of unit (b, h), the four
 // waves' states left in lds.
-template <Kind KIND, bool WIDE>
+template <Kind KIND, bool WIDE, bool LONG>
 __device__ __forceinline__ void attn_piece(const PagedAttnArgs& a, int b, int h, int n, int step,
                                            int take, PagedAttnLds& lds) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -913,8 +971,11 @@ __device__ __forceinline__ void attn_piece(const PagedAttnArgs& a, int b, int h,
   st.l = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  attn_steps<KIND, WIDE>(a, x, step * kPagedStep + wave * kPagedTile,
-                         min((step + take) * kPagedStep, n), limit, c, q, st);
+  const int p = step * kPagedStep + wave * kPagedTile, end = min((step + take) * kPagedStep, n);
+  if constexpr (LONG && KIND == Kind::kE2M1)
+    attn_pairs<KIND, WIDE>(a, x, p, end, limit, c, q, st);
+  else
+    attn_steps<KIND, WIDE>(a, x, p, end, limit, c, q, st);
   st.l += __shfl_xor(st.l, 16);
   st.l += __shfl_xor(st.l, 32);
   if (g == 0) {
@@ -959,7 +1020,8 @@ __device__ __forceinline__ void store_empty(const PagedAttnArgs& a, int64_t firs
 // 64, 16, 8, 4, 2 and 1: e4m3 93, 97, 113, 114, 123 and 148 us, bf16 172, 174, 182,
 // 185, 190 and 204.
 template <Kind KIND, bool WIDE>
-__global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnArgs a) {
+__global__ __launch_bounds__(kPagedAttnThreads, paged_wgs_per_cu(KIND)) void k_paged_attn(
+    PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, w = blockIdx.x, rows = a.T << a.lg;
   const Lens lens = {(TablePtr)(uintptr_t)a.ctx_lens, a.B, a.pg.Hkv, a.max_ctx};
@@ -971,7 +1033,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(PagedAttnAr
   while (at < rg.s1) {
     const int b = rg.b, h = rg.h, step = rg.step, steps = rg.steps;
     const int take = (int)min((int64_t)(steps - step), rg.s1 - at);
-    attn_piece<KIND, WIDE>(a, b, h, lens(b), step, take, lds);
+    attn_piece<KIND, WIDE, true>(a, b, h, lens(b), step, take, lds);
     const int slot = at == rg.s0 ? 0 : 1;
     for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {
       const int row = i >> 5, d = 4 * (i & 31);
@@ -1112,7 +1174,7 @@ __global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn_direct(Page
         store_empty(a, out_row(a, b, h, t << a.lg), (int64_t)1 << a.lg);
     return;
   }
-  attn_piece<KIND, WIDE>(a, b, h, n, piece << a.piece, 1 << a.piece, lds);
+  attn_piece<KIND, WIDE, false>(a, b, h, n, piece << a.piece, 1 << a.piece, lds);
   const bool last = piece == pieces - 1;
   float* part = a.part + (int64_t)blockIdx.x * 2 * rows * kPartStride;
   for (int i = tid; i < rows * (kD / 4); i += kPagedAttnThreads) {

@@ -382,14 +382,21 @@ __device__ __forceinline__ void tile_mask(Tile<KIND>& t, int p0, int limit, int 
   }
 }
 
-template <Kind KIND>
-__device__ __forceinline__ void tile_weights(const Tile<KIND>& t, float c, const float* lg,
-                                             uint32_t part[3][8], WaveState& st) {
-  float top = lg[0];
-#pragma unroll
-  for (int j = 1; j < 8; ++j) top = fmaxf(top, lg[j]);
-  top = fmaxf(top, __shfl_xor(top, 16));
-  top = fmaxf(top, __shfl_xor(top, 32));
+// Max over the lanes of a query row, r, r + 16, r + 32, r + 48: rows of lanes
+// change places, and then halves (no LDS round trip in the steps' chain).
+__device__ __forceinline__ float query_row_max(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const uint32_t v = __float_as_uint(x);
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Logits up to `top` (of this lane) are about to be taken: the running maximum
+// follows, and what was summed under the old one is scaled.
+__device__ __forceinline__ void raise_max(float top, float c, WaveState& st) {
+  top = query_row_max(top);
   const float m = fmaxf(st.m, top * c);
   if (__any(m > st.m)) {
     const float f = st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
@@ -400,17 +407,42 @@ __device__ __forceinline__ void tile_weights(const Tile<KIND>& t, float c, const
       for (int j = 0; j < 4; ++j) st.o[e][j] *= f;
     st.m = m;
   }
-  const float less = m == -INFINITY ? 0.f : -m;  // nothing seen yet: all weights are 0
+}
+
+__device__ __forceinline__ float top_of(const float* lg) {
+  float top = lg[0];
+#pragma unroll
+  for (int j = 1; j < 8; ++j) top = fmaxf(top, lg[j]);
+  return top;
+}
+
+// ve: e4m3's exponent bytes of the lane's positions of each half.
+template <Kind KIND>
+__device__ __forceinline__ void tile_weights(const uint32_t* ve, float c, const float* lg,
+                                             uint32_t part[3][8], WaveState& st) {
+  const float less = st.m == -INFINITY ? 0.f : -st.m;  // nothing seen yet: all weights are 0
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float p = __builtin_amdgcn_exp2f(fmaf(lg[j], c, less));
     st.l += p;
-    if (KIND == Kind::kE4M3) p = scaled(p, t.ve[j >> 2] ^ 0x80808080u, j & 3);
+    if (KIND == Kind::kE4M3) p = scaled(p, ve[j >> 2] ^ 0x80808080u, j & 3);
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       part[i][j] = __float_as_uint(p);
       p -= __uint_as_float(part[i][j] & 0xffff0000u);
     }
+  }
+}
+
+// The weights' parts as operands.
+__device__ __forceinline__ void pack_weights(const uint32_t part[3][8], bf16x8* w) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    uint32_t y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      y[j] = __builtin_amdgcn_perm(part[i][2 * j + 1], part[i][2 * j], 0x07060302u);
+    w[i] = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
   }
 }
 
@@ -422,14 +454,7 @@ __device__ __forceinline__ void tile_output(const Tile<KIND>& t, const uint32_t 
 #pragma unroll
   for (int j = 0; j < 8; ++j)
     scale[j] = KIND == Kind::kE2M1 ? scale_of(t.ve[j], (threadIdx.x & 15) >> 2) : 0u;
-#pragma unroll
-  for (int i = 0; i < 3; ++i) {
-    uint32_t y[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      y[j] = __builtin_amdgcn_perm(part[i][2 * j + 1], part[i][2 * j], 0x07060302u);
-    w[i] = as_bf16x8(make_uint4(y[0], y[1], y[2], y[3]));
-  }
+  pack_weights(part, w);
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     uint32_t even[4], odd[4];
@@ -468,8 +493,9 @@ __device__ __forceinline__ void tile_rest(Tile<KIND>& t, bool masked, int p, int
     for (int j = 0; j < 8; ++j) lg[j] = scaled(lg[j], t.ke[j >> 2] ^ 0x80808080u, j & 3);
   }
   if (masked) tile_mask<KIND>(t, p, limit, n, lg);
+  raise_max(top_of(lg), c, st);
   uint32_t part[3][8];
-  tile_weights<KIND>(t, c, lg, part, st);
+  tile_weights<KIND>(t.ve, c, lg, part, st);
   tile_output<KIND>(t, part, st);
 }
 
