@@ -1020,7 +1020,7 @@ __device__ __forceinline__ void store_empty(const PagedAttnArgs& a, int64_t firs
 // 64, 16, 8, 4, 2 and 1: e4m3 93, 97, 113, 114, 123 and 148 us, bf16 172, 174, 182,
 // 185, 190 and 204.
 template <Kind KIND, bool WIDE>
-__global__ __launch_bounds__(kPagedAttnThreads, paged_wgs_per_cu(KIND)) void k_paged_attn(
+__global__ __launch_bounds__(kPagedAttnThreads, 2) void k_paged_attn(
     PagedAttnArgs a) {
   __shared__ PagedAttnLds lds;
   const int tid = threadIdx.x, w = blockIdx.x, rows = a.T << a.lg;
