@@ -92,6 +92,20 @@ int cut_pieces(const BlockTokens& t) {
       1, std::min<int64_t>({kBlockWgs / units, steps / 8, (int64_t)kMaxPieces}));
 }
 
+// Many tokens of a bf16 cache: four tiles share the staging of a block that one of them
+// keeps.  A tile a workgroup against it, us, 16 blocks of 64, 8 KV heads of 4 query
+// heads: 512 tokens (256 workgroups of four tiles) 202 / 218, 1024 386 / 253, 2048 756 /
+// 304, 1024 tokens and 4 heads of 8 259 / 182; 1500 tokens, 8 heads of 1 (192) 248 / 317.
+// Rows of codes are less to read and have to be made bf16: 2048 tokens e4m3 362 / 359,
+// e2m1 269 / 337.  With fewer tokens a request than four tiles have a block would be of
+// use to one wave.
+constexpr int kManyWgs = 384;
+
+bool many_tokens(const BlockTokens& t, Kind kind) {
+  return kind == Kind::kBf16 && (int64_t)t.n >= (int64_t)t.B * (kManyTiles * 16 >> t.lg) &&
+         tiles_of(t, kManyTiles) * t.Hkv >= kManyWgs;
+}
+
 size_t part_bytes(const BlockTokens& t) {
   const int pieces = cut_pieces(t);
   if (pieces == 1) return 0;
@@ -218,6 +232,7 @@ int ckv_paged_block_attn(const ckv_shape* shape, const ckv_paged_cache* cache, i
   a.part = static_cast<float*>(ws);
   a.scale = scale;
   a.pieces = cut_pieces(a.t);
+  a.many = requests && many_tokens(a.t, (Kind)cache->kind);
   hipStream_t s = (hipStream_t)stream;
   CKV_RC(debug_check_paged(s, a.pg, nullptr, requests, positions, d.B, d.max_ctx, num_tokens,
                            true));

@@ -403,12 +403,16 @@ static_assert(1 << kStepLg == kPagedTile, "a step");
 
 struct BlockLds {
   float m[4][16], l[4][16];
-  float o[4][16][kPartStride];
   int32_t pos[16], req[16], end[16];
-  uint32_t list[16 * kMaxKept];   // the tokens' blocks (all ones: none)
-  int32_t block[16 * kMaxKept];   // of the tile, each once
-  uint32_t who[16 * kMaxKept];    // its tokens' bits, and the first of them << 16
   int32_t count[4];
+  union {
+    float o[4][16][kPartStride];
+    struct {                         // until the last step
+      uint32_t list[16 * kMaxKept];  // the tokens' blocks (all ones: none)
+      int32_t block[16 * kMaxKept];  // of the tile, each once
+      uint32_t who[16 * kMaxKept];   // its tokens' bits, and the first of them << 16
+    };
+  };
 };
 
 // Whether token i's ascending list holds block v.
@@ -516,16 +520,76 @@ __device__ __forceinline__ void store_block_row(const BlockAttnArgs& a, int64_t 
   if (a.lse && d == 0) a.lse[at] = log_sum(p.M, p.L);
 }
 
-template <Kind KIND>
-__global__ __launch_bounds__(kBlockThreads, 2) void k_block_attn(BlockAttnArgs a) {
-  __shared__ BlockLds lds;
+// raise_max for a maximum that may lie up to 2^8 below what it stands for: weights
+// are then at most 2^8 and sums as exact as before, and scaling is needed at the
+// first steps only.
+__device__ __forceinline__ void raise_max_lazily(float top, float c, WaveState& st) {
+  const float m = query_row_max(top) * c;
+  const bool more = m > st.m + 8.f;
+  if (__any(more)) {
+    const float f = !more ? 1.f : st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
+    st.l *= f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) st.o[e][j] *= f;
+    if (more) st.m = m;
+  }
+}
+
+// The weights of a step and its products with V.  APART: these a token at a time,
+// without the rows that it does not see, for V rows whose product with a weight of
+// zero is no zero.
+template <Kind KIND, bool APART>
+__device__ __forceinline__ void block_rest(const BlockAttnArgs& a, Tile<KIND>& t, int p0,
+                                           int limit, int n, float c, float* lg, WaveState& st) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  if (KIND == Kind::kE4M3) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lg[j] = scaled(lg[j], t.ke[j >> 2] ^ 0x80808080u, j & 3);
+  }
+  // Rows whose token does not keep the block get weights of exp2(-inf); single
+  // positions are left out only where a step has such.
+  const bool kept = limit > p0;
+  if (APART || t.there != 255u || __any(kept && limit < p0 + kPagedTile))
+    tile_mask<KIND>(t, p0, limit, n, lg);
+  raise_max_lazily(kept ? top_of(lg) : -INFINITY, c, st);
+  uint32_t part[3][8];
+  tile_weights<KIND>(t.ve, c, kept ? less_max(st) : -INFINITY, lg, part, st);
+  if (!APART) {
+    tile_output<KIND>(t, part, st);
+    return;
+  }
+  for (int k = 0; k < 16 >> a.t.lg; ++k) {
+    const int end = __builtin_amdgcn_readlane(limit, k << a.t.lg);
+    if (end <= p0) continue;
+    Tile<KIND> seen = t;
+    WaveState one = st;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (p0 + 16 * (j >> 2) + 4 * g + (j & 3) < end) continue;
+#pragma unroll
+      for (int i = 0; i < Tile<KIND>::kV; ++i) seen.v[j][i] = 0u;
+      if (KIND == Kind::kE2M1) seen.ve[j] = 0u;
+    }
+    tile_output<KIND>(seen, part, one);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (r >> a.t.lg == k) st.o[e][j] = one.o[e][j];
+  }
+}
+
+// The waves' sums of a piece of a tile's list, into lds; false: they hold a NaN, and
+// nothing is written.
+template <Kind KIND, bool APART>
+__device__ __forceinline__ bool block_sums(const BlockAttnArgs& a, BlockLds& lds, int h, int tile,
+                                           int piece, int blocks) {
   const BlockTokens& bt = a.t;
   const int tid = threadIdx.x, lane = tid & 63, g = lane >> 4, r = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = blockIdx.x % bt.Hkv, rest = blockIdx.x / bt.Hkv;
-  const int tile = rest / a.pieces, piece = rest - tile * a.pieces;
   const int64_t t0 = (int64_t)tile * (16 >> bt.lg);
-  const int blocks = gather_blocks(a, t0, h, lds);
   const int64_t steps = (int64_t)blocks << (bt.lb - kStepLg);
   const int s1 = (int)(steps * (piece + 1) / a.pieces);
   int s = (int)(steps * piece / a.pieces) + wave;
@@ -544,6 +608,9 @@ __global__ __launch_bounds__(kBlockThreads, 2) void k_block_attn(BlockAttnArgs a
   st.l = 0.f;
 #pragma unroll
   for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // (as constants the sums would be held twice, and copied at each step)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) asm("" : "+v"(st.o[e]));
   if (s < s1) {
     Tile<KIND> t;
     float lg[8];
@@ -553,20 +620,27 @@ __global__ __launch_bounds__(kBlockThreads, 2) void k_block_attn(BlockAttnArgs a
     s += 4;
     BlockStep next = block_step(a, lds, h, min(s, s1 - 1));
     auto limit = [&] { return now.who >> row_tok & 1u ? my_end : 0; };
-    while (s < s1) {
+    for (;;) {  // (the last step asks for K rows that nobody takes)
       tile_logits<KIND, true>(t, q, lg);
       load_k<KIND, true>(a.pg, next.x, next.at, t);
       __builtin_amdgcn_sched_barrier(0);
-      tile_rest<KIND>(t, true, now.p0, limit(), now.x.n, c, lg, st);
+      block_rest<KIND, APART>(a, t, now.p0, limit(), now.x.n, c, lg, st);
       __builtin_amdgcn_sched_barrier(0);
+      if (s >= s1) break;
       load_v<KIND, true>(a.pg, next.x, next.at, t);
       now = next;
       s += 4;
       next = block_step(a, lds, h, min(s, s1 - 1));
     }
-    tile_logits<KIND, true>(t, q, lg);
-    tile_rest<KIND>(t, true, now.p0, limit(), now.x.n, c, lg, st);
   }
+  bool bad = false;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) bad = bad || st.o[e][j] != st.o[e][j];
+  // (barriers: the lists have been read)
+  if (APART) __syncthreads();
+  else if (__builtin_amdgcn_readfirstlane(__syncthreads_or(bad))) return false;
   st.l += __shfl_xor(st.l, 16);
   st.l += __shfl_xor(st.l, 32);
   if (g == 0) {
@@ -579,6 +653,46 @@ __global__ __launch_bounds__(kBlockThreads, 2) void k_block_attn(BlockAttnArgs a
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] = KIND == Kind::kE4M3 ? 2.f * st.o[e][j] : st.o[e][j];
   }
+  return true;
+}
+
+// The rare case out of line, so that it costs the ordinary one no registers: its
+// arguments are read again from where the kernel has them.
+typedef const __attribute__((address_space(4))) BlockAttnArgs* BlockAttnArgsPtr;
+typedef __attribute__((address_space(3))) uint8_t* LdsPtr;
+
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+  return (uint32_t)(uintptr_t)(LdsPtr)p;
+}
+
+__device__ __forceinline__ BlockAttnArgs args_at(uint64_t args) {
+  const uint64_t at = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(args >> 32)) << 32 |
+                      (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)args);
+  return *(const BlockAttnArgs*)(BlockAttnArgsPtr)at;
+}
+
+template <Kind KIND>
+__device__ __attribute__((noinline)) void block_sums_apart(uint64_t args, uint32_t lds, int h,
+                                                           int tile, int piece, int blocks) {
+  const BlockAttnArgs a = args_at(args);
+  block_sums<KIND, true>(
+      a, *(BlockLds*)(LdsPtr)(uintptr_t)__builtin_amdgcn_readfirstlane(lds),
+      __builtin_amdgcn_readfirstlane(h), __builtin_amdgcn_readfirstlane(tile),
+      __builtin_amdgcn_readfirstlane(piece), __builtin_amdgcn_readfirstlane(blocks));
+}
+
+template <Kind KIND>
+__global__ __launch_bounds__(kBlockThreads, 3) void k_block_attn(BlockAttnArgs a) {
+  __shared__ BlockLds lds;
+  const BlockTokens& bt = a.t;
+  const int tid = threadIdx.x;
+  const int h = blockIdx.x % bt.Hkv, rest = blockIdx.x / bt.Hkv;
+  const int tile = rest / a.pieces, piece = rest - tile * a.pieces;
+  const int64_t t0 = (int64_t)tile * (16 >> bt.lg);
+  const int blocks = gather_blocks(a, t0, h, lds);
+  if (!block_sums<KIND, false>(a, lds, h, tile, piece, blocks))
+    block_sums_apart<KIND>((uint64_t)__builtin_amdgcn_kernarg_segment_ptr(), lds_address(&lds), h,
+                           tile, piece, blocks);
   __syncthreads();
   for (int i = tid; i < 16 * (kD / 4); i += kBlockThreads) {
     const int row = i >> 5, d = 4 * (i & 31);
@@ -624,6 +738,364 @@ __global__ __launch_bounds__(kBlockThreads) void k_block_merge(BlockAttnArgs a) 
   }
 }
 
+// ---- attention of many tokens --------------------------------------------------------
+// For a bf16 cache, whose rows many tokens would otherwise fetch from the L2 again and
+// again: a workgroup has four tiles, a wave each.  The blocks that any of its tokens
+// keeps are taken in ascending order, 32 positions at a time, into LDS, the next ones
+// while these are multiplied; a wave passes over what none of its tokens keeps.  V's
+// operands are made by transposing LDS reads, without byte permutes, and no waves are
+// joined.  All workgroups go through the positions alike, so that a head's L2 has what
+// they need (2048 tokens, 16 of 256 blocks of 64 each: 0.4 GB of 2.4 from behind it;
+// a workgroup a tile reads 5.1, 3.3 of it from behind).
+//   The blocks' order is a merge of the tokens' lists, each lane the cursor of a
+// token: the least head of all is next, the lanes that have it are its tokens.
+//   Rows are 256 bytes, the 16-byte part p of row i = 8 a + b (a < 2) at p ^ (2 b + a):
+// 16 rows of a part, K's operand, and 8 rows of two parts, V's, are in all banks.
+constexpr int kManyThreads = 64 * kManyTiles;
+constexpr uint32_t kRowBytes = 2 * kD;
+constexpr uint32_t kHalfBytes = 16 * kRowBytes, kRowsBytes = 2 * kHalfBytes;
+constexpr int kBlockBits = 25;  // max_ctx <= 2^30 in blocks of 32
+
+struct ManyLds {
+  alignas(256) uint8_t rows[4 * kPagedTile * kRowBytes];  // [buffer][K, V][row]
+  int32_t counts[64];
+};
+
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t x) {
+  x = min(x, dpp_u32<0x128, 0xF, false>(x));  // row_ror
+  x = min(x, dpp_u32<0x124, 0xF, false>(x));
+  x = min(x, dpp_u32<0x122, 0xF, false>(x));
+  x = min(x, dpp_u32<0x121, 0xF, false>(x));
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = min(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __builtin_amdgcn_readfirstlane(min(b[0], b[1]));
+}
+
+// 32 positions of a block, the same for the workgroup.
+struct ManyStep {
+  uint64_t who;     // its tokens
+  int p0, stop, n;  // stop: where its block ends for the tokens, n: for the request's
+  int req;
+  int first[2], page[2];
+  int pages;        // lane i: page[i & 1]
+  __device__ __forceinline__ void take_pages() {
+    page[0] = __builtin_amdgcn_readlane(pages, 0);
+    page[1] = __builtin_amdgcn_readlane(pages, 1);
+  }
+  __device__ __forceinline__ bool there(const PagedPages& pg, int i) const {
+    return (unsigned)page[i] < (unsigned)pg.num_pages;
+  }
+};
+
+// A lane's token and its place in its list.
+struct ManyCursor {
+  int req, end;     // the request's positions that the workgroup's tokens see
+  uint32_t rank;
+  uint32_t head;    // of the list (unless at == count)
+  int at, count;
+  const uint32_t* list;
+  __device__ __forceinline__ uint32_t key() const {
+    return at < count ? rank << kBlockBits | head : ~0u;
+  }
+};
+
+// The step after s; false: none.
+__device__ __forceinline__ bool next_step(const BlockAttnArgs& a, ManyCursor& c, ManyStep& s) {
+  s.p0 += kPagedTile;
+  if (s.p0 >= s.stop) {
+    const uint32_t key = c.key(), least = wave_min_u32(key);
+    if (least == ~0u) return false;
+    s.who = __ballot(key == least);
+    c.at += key == least;
+    c.head = c.list[c.at];
+    const int l = __builtin_ctzll(s.who);
+    s.req = __builtin_amdgcn_readlane(c.req, l);
+    s.n = __builtin_amdgcn_readlane(c.end, l);
+    s.p0 = (int)(least & ((1u << kBlockBits) - 1)) << a.t.lb;
+    s.stop = min(s.p0 + (1 << a.t.lb), s.n);
+  }
+  // The halves' pages by a vector load, to be looked at a step later: a scalar one
+  // would have to be back before the next read of LDS.
+#pragma unroll
+  for (int i = 0; i < 2; ++i) s.first[i] = half_first(s.p0, i, s.n);
+  s.pages = table_of(a.pg, s.req)[(threadIdx.x & 1 ? s.first[1] : s.first[0]) >> a.pg.shift];
+  return true;
+}
+
+__device__ __forceinline__ uint32_t part_at(int row, int part) {
+  return row * kRowBytes + ((part ^ (row << 1 & 14) ^ (row >> 3 & 1)) << 4);
+}
+
+// 64 times 16 bytes from base + offset (a lane's) to LDS bytes [to, to + 1024), without
+// registers between; there once this wave's vmcnt is 0.  (The builtin makes the
+// compiler wait for it at the next read of any LDS, of the other buffer too.)
+__device__ __forceinline__ void load_to_lds(const uint8_t* base, uint32_t offset, uint32_t to) {
+  asm volatile(
+      "s_mov_b32 m0, %0\n\t"
+      "s_nop 0\n\t"
+      "global_load_lds_dwordx4 %1, %2"
+      :
+      : "s"(to), "v"(offset), "s"(base)
+      : "memory", "m0");
+}
+
+// (A builtin, which tells the compiler that nothing of its own is in flight either.)
+__device__ __forceinline__ void wait_for_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt 0
+  asm volatile("" ::: "memory");
+}
+
+__device__ __forceinline__ void stage_load(const BlockAttnArgs& a, ManyLds& lds, int buf, int h,
+                                           const ManyStep& s) {
+  const PagedPages& pg = a.pg;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int v = wave >> 1, half = wave & 1;  // a wave has a half of K or V
+  const bool there = half ? s.there(pg, 1) : s.there(pg, 0);
+  const int page = there ? half ? s.page[1] : s.page[0] : 0;
+  const int first = half ? s.first[1] : s.first[0], last = half_last(first, s.n);
+  const uint8_t* rows = (v ? pg.v : pg.k) + row_offset(pg, page, h, first);
+  uint8_t* dst = lds.rows + (2 * buf + v) * kRowsBytes + half * kHalfBytes;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int row = 4 * i + (lane >> 4);
+    uint8_t* to = dst + 4 * i * kRowBytes;
+    if (there)
+      load_to_lds(rows, min(row, last) * pg.row_bytes + (part_at(row, lane & 15) & 255u),
+                  lds_address(to));
+    else
+      *reinterpret_cast<uint4*>(to + 16 * lane) = make_uint4(0, 0, 0, 0);
+  }
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// Channels of four rows transposed: lane i of 16 gives the 8 bytes that hold channels
+// [4 (i % 4), ...) of row i / 4 and gets channel i of the four rows.
+__device__ __forceinline__ uint2 read_transposed(const uint8_t* p) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                 (__attribute__((address_space(3))) s16x4*)(p)));
+}
+
+// Rows of four positions from the n-th on as zeros.
+__device__ __forceinline__ uint2 first_of(uint2 x, int n) {
+  const uint64_t keep = n <= 0 ? 0ull : n >= 4 ? ~0ull : (1ull << 16 * n) - 1;
+  return make_uint2(x.x & (uint32_t)keep, x.y & (uint32_t)(keep >> 32));
+}
+
+// A wave's 16 query rows over one step.  APART: the products with V a token at a time,
+// without the rows that it does not see, for V rows whose product with a weight of
+// zero is no zero.
+template <bool APART>
+__device__ __forceinline__ void many_step(const BlockAttnArgs& a, const ManyLds& lds, int buf,
+                                          const ManyStep& s, const bf16x8* q, float c, int tok,
+                                          int my_end, WaveState& st) {
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int limit = s.who >> tok & 1 ? my_end : 0;
+  if (!__any(limit > s.p0)) return;
+  float lg[8];
+  // (offsets from the buffer's on, so that they are not held in registers)
+  const uint32_t k = 2 * buf * kRowsBytes + part_at(r, g);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      x = mfma_16x16x32(as_bf16x8(*static_cast<const uint4*>(__builtin_assume_aligned(
+                            lds.rows + (k ^ 64u * f) + i * kHalfBytes, 16))),
+                        q[f], x);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lg[4 * i + j] = x[j];
+  }
+  // Rows whose token does not keep the block get weights of exp2(-inf); single
+  // positions are left out only where a step has such.
+  const bool kept = limit > s.p0;
+  if (APART || !s.there(a.pg, 0) || !s.there(a.pg, 1) ||
+      __any(kept && limit < s.p0 + kPagedTile)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int end = s.there(a.pg, j >> 2) ? limit : 0;
+      if (s.p0 + 16 * (j >> 2) + 4 * g + (j & 3) >= end) lg[j] = -INFINITY;
+    }
+  }
+  const int row = 4 * g + (r >> 2);
+  const uint32_t v = (2 * buf + 1) * kRowsBytes + part_at(row, (r >> 1) & 1) + 8 * (r & 1);
+  uint4 rows[4];  // of V, for four times 16 channels
+  auto read_rows = [&](int part) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint8_t* p = lds.rows + (v ^ 32u * (4 * part + e));
+      const uint2 lo = read_transposed(p), hi = read_transposed(p + kHalfBytes);
+      rows[e] = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    }
+  };
+  read_rows(0);  // on their way while the weights are made
+  raise_max_lazily(kept ? top_of(lg) : -INFINITY, c, st);
+  uint32_t part[3][8];
+  tile_weights<Kind::kBf16>(nullptr, c, kept ? less_max(st) : -INFINITY, lg, part, st);
+  bf16x8 w[3];
+  pack_weights(part, w);
+  if (!APART) {
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      if (part) read_rows(1);
+#pragma unroll
+      for (int i = 0; i < 3; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          st.o[4 * part + e] = mfma_16x16x32(as_bf16x8(rows[e]), w[i], st.o[4 * part + e]);
+    }
+    return;
+  }
+  for (int t = 0; t < 16 >> a.t.lg; ++t) {
+    const int end = __builtin_amdgcn_readlane(limit, t << a.t.lg) - s.p0 - 4 * g;
+    if (__builtin_amdgcn_readlane(limit, t << a.t.lg) <= s.p0) continue;
+#pragma unroll
+    for (int part = 0; part < 2; ++part) {
+      read_rows(part);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint2 lo = first_of(make_uint2(rows[e].x, rows[e].y), end);
+        const uint2 hi = first_of(make_uint2(rows[e].z, rows[e].w), end - 16);
+        f32x4 o = st.o[4 * part + e];
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          o = mfma_16x16x32(as_bf16x8(make_uint4(lo.x, lo.y, hi.x, hi.y)), w[i], o);
+        if (r >> a.t.lg == t) st.o[4 * part + e] = o;
+      }
+    }
+  }
+}
+
+template <bool APART>
+__device__ __forceinline__ void many_steps(const BlockAttnArgs& a, ManyLds& lds, ManyCursor& cur,
+                                           int h, const bf16x8* q, float c, int tok, int my_end,
+                                           WaveState& st) {
+  st.m = -INFINITY;
+  st.l = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) st.o[e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  cur.at = 0;
+  cur.head = cur.list[0];
+  // (as constants the sums would be held twice, and copied at each step)
+#pragma unroll
+  for (int e = 0; e < 8; ++e) asm("" : "+v"(st.o[e]));
+  ManyStep now, next;
+  next.p0 = next.stop = 0;
+  if (!next_step(a, cur, next)) return;  // the same for the workgroup
+  next.take_pages();
+  stage_load(a, lds, 0, h, next);
+  now = next;
+  bool more = next_step(a, cur, next);
+  for (int buf = 0;; buf ^= 1) {
+    // the rows are in LDS, the other buffer's have been used
+    wait_for_loads();
+    lds_barrier();
+    if (more) {
+      next.take_pages();
+      stage_load(a, lds, buf ^ 1, h, next);
+    }
+    ManyStep then = next;
+    const bool last = !more;
+    if (more) more = next_step(a, cur, then);
+    many_step<APART>(a, lds, buf, now, q, c, tok, my_end, st);
+    if (last) break;
+    now = next;
+    next = then;
+  }
+}
+
+// A workgroup's output; false: its sums hold a NaN, and nothing is written but the lists
+// and counts, which the call with APART takes as they are.
+template <bool APART>
+__device__ __forceinline__ bool many_tiles(const BlockAttnArgs& a, ManyLds& lds, uint32_t* lists,
+                                           int block) {
+  const BlockTokens& bt = a.t;
+  const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = block % bt.Hkv, tile = block / bt.Hkv;
+  const int tokens = 64 >> bt.lg;
+  const int64_t t0 = (int64_t)tile * tokens;
+  const Token x = lane < tokens ? token_of(bt, t0 + lane) : Token{-1, -1};
+  ManyCursor cur = {x.req, 0, 0, 0, 0, 0, lists + min(lane, tokens - 1) * bt.k};
+  uint64_t left = __ballot(x.req >= 0);
+  while (left) {  // each request once
+    const int l = __builtin_ctzll(left);
+    const bool member = x.req == __builtin_amdgcn_readlane(x.req, l);
+    const int end = (int)~wave_min_u32(member ? ~(uint32_t)(x.pos + 1) : ~0u);
+    if (member) cur.rank = l, cur.end = end;
+    left &= ~__ballot(member);
+  }
+  // what counts of a list, close together
+  for (int i = wave; !APART && i < tokens; i += kManyTiles) {
+    const int req = __builtin_amdgcn_readlane(x.req, i);
+    const int pos = __builtin_amdgcn_readlane(x.pos, i);
+    uint32_t v = ~0u;
+    if (req >= 0 && lane < bt.k) {
+      const int j = a.idx[((t0 + i) * bt.Hkv + h) * bt.k + lane];
+      if ((unsigned)j <= (unsigned)(pos >> bt.lb)) v = (uint32_t)j;
+    }
+    const uint32_t before = __shfl_up(v, 1);
+    const bool keep = v != ~0u && (lane == 0 || before != v);
+    const uint64_t all = __ballot(keep);
+    if (keep) lists[i * bt.k + __popcll(all & ((1ull << lane) - 1))] = v;
+    if (lane == 0) lds.counts[i] = __popcll(all);
+  }
+  __syncthreads();
+  if (lane < tokens) cur.count = lds.counts[lane];
+  const int tok = (wave << 4 | r) >> bt.lg;
+  const int my_end = __shfl(x.pos, tok) + 1;
+  const int64_t token = t0 + tok;
+  const int64_t row = min(token, (int64_t)bt.n - 1) * bt.Hq + (h << bt.lg) +
+                      (r & ((1 << bt.lg) - 1));
+  bf16x8 q[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) q[f] = as_bf16x8(ld16(bt.q + row * kD + 32 * f + 8 * g));
+  const float c = a.scale * 1.4426950408889634f;
+  WaveState st;
+  many_steps<APART>(a, lds, cur, h, q, c, tok, my_end, st);
+  if (!APART) {
+    bool bad = false;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) bad = bad || st.o[e][j] != st.o[e][j];
+    if (__builtin_amdgcn_readfirstlane(__syncthreads_or(bad))) return false;
+  }
+  st.l += __shfl_xor(st.l, 16);
+  st.l += __shfl_xor(st.l, 32);
+  const float inv = inverse_sum(st.l);
+  float* out = a.out + row * kD + 4 * g;
+  if (token < bt.n) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      *reinterpret_cast<float4*>(out + 16 * e) = make_float4(
+          st.o[e][0] * inv, st.o[e][1] * inv, st.o[e][2] * inv, st.o[e][3] * inv);
+    if (a.lse && g == 0) a.lse[row] = log_sum(st.m, st.l);
+  }
+  return true;
+}
+
+__device__ __attribute__((noinline)) void many_tiles_apart(uint64_t args, uint32_t lds,
+                                                           uint32_t lists, int block) {
+  const BlockAttnArgs a = args_at(args);
+  many_tiles<true>(
+      a, *(ManyLds*)(LdsPtr)(uintptr_t)__builtin_amdgcn_readfirstlane(lds),
+      (uint32_t*)(LdsPtr)(uintptr_t)__builtin_amdgcn_readfirstlane(lists),
+      __builtin_amdgcn_readfirstlane(block));
+}
+
+__global__ __launch_bounds__(kManyThreads, 4) void k_block_attn_many(BlockAttnArgs a) {
+  __shared__ ManyLds lds;
+  extern __shared__ uint32_t lists[];  // [tokens][k], and a word that an ended list reads
+  if (!many_tiles<false>(a, lds, lists, blockIdx.x))
+    many_tiles_apart((uint64_t)__builtin_amdgcn_kernarg_segment_ptr(), lds_address(&lds),
+                     lds_address(lists), blockIdx.x);
+}
+
 // ---- launchers ---------------------------------------------------------------------------
 hipError_t launch_marks(const MarkArgs& a, Kind kind, hipStream_t s) {
   of_kind(kind, [&](auto k) {
@@ -665,6 +1137,13 @@ hipError_t launch_select_blocks(const BlockSelectArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_block_attn(const BlockAttnArgs& a, Kind kind, hipStream_t s) {
+  if (a.many) {
+    const size_t lists = sizeof(uint32_t) * (a.t.k * (kManyTiles * 16 >> a.t.lg) + 1);
+    launch_kernel_lds(CKV_K_BLOCK_ATTN, k_block_attn_many,
+                      dim3((unsigned)(tiles_of(a.t, kManyTiles) * a.t.Hkv)), dim3(kManyThreads),
+                      lists, s, a);
+    return launch_status();
+  }
   const int64_t units = tiles_of(a.t) * a.t.Hkv;
   of_kind(kind, [&](auto k) {
     launch_kernel(CKV_K_BLOCK_ATTN, k_block_attn<k.value>, dim3((unsigned)(units * a.pieces)),

@@ -49,12 +49,15 @@ struct BlockAttnArgs {
   float* part;             // [tiles][Hkv][pieces][16][kPartStride]
   float scale;
   int32_t pieces;
+  int32_t many;            // 64 query rows a workgroup, blocks staged for its waves
 };
 
 inline int64_t tiles_of(const BlockTokens& t, int row_tiles = 1) {
   const int per = (16 >> t.lg) * row_tiles;
   return (t.n + per - 1) / per;
 }
+
+constexpr int kManyTiles = 4;  // tiles of a workgroup that stages blocks
 
 hipError_t launch_marks(const MarkArgs& a, Kind kind, hipStream_t s);
 hipError_t launch_select_blocks(const BlockSelectArgs& a, hipStream_t s);

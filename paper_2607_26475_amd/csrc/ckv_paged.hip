@@ -928,7 +928,7 @@ __device__ __forceinline__ void attn_pairs(const PagedAttnArgs& a, const Ctx& x,
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       uint32_t part[3][8];
-      tile_weights<KIND>(t[i].ve, c, lg[i], part, st);
+      tile_weights<KIND>(t[i].ve, c, less_max(st), lg[i], part, st);
       tile_output<KIND>(t[i], part, st);
     }
     __builtin_amdgcn_sched_barrier(0);

@@ -416,11 +416,17 @@ __device__ __forceinline__ float top_of(const float* lg) {
   return top;
 }
 
+// What logits times c are made less by: the running maximum; nothing seen yet: all
+// weights are 0.
+__device__ __forceinline__ float less_max(const WaveState& st) {
+  return st.m == -INFINITY ? 0.f : -st.m;
+}
+
 // ve: e4m3's exponent bytes of the lane's positions of each half.
 template <Kind KIND>
-__device__ __forceinline__ void tile_weights(const uint32_t* ve, float c, const float* lg,
-                                             uint32_t part[3][8], WaveState& st) {
-  const float less = st.m == -INFINITY ? 0.f : -st.m;  // nothing seen yet: all weights are 0
+__device__ __forceinline__ void tile_weights(const uint32_t* ve, float c, float less,
+                                             const float* lg, uint32_t part[3][8],
+                                             WaveState& st) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
     float p = __builtin_amdgcn_exp2f(fmaf(lg[j], c, less));
@@ -495,7 +501,7 @@ __device__ __forceinline__ void tile_rest(Tile<KIND>& t, bool masked, int p, int
   if (masked) tile_mask<KIND>(t, p, limit, n, lg);
   raise_max(top_of(lg), c, st);
   uint32_t part[3][8];
-  tile_weights<KIND>(t.ve, c, lg, part, st);
+  tile_weights<KIND>(t.ve, c, less_max(st), lg, part, st);
   tile_output<KIND>(t, part, st);
 }
 

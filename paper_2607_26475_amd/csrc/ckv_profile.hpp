@@ -20,15 +20,21 @@ void debug_after_launch(hipStream_t s);
 // synchronisation saw, else hipGetLastError().
 hipError_t launch_status();
 
-template <typename F, typename... Args>
-inline void launch_kernel(int id, F kernel, dim3 grid, dim3 block, hipStream_t s,
-                          Args... args) {
+template <class F, class... Args>
+inline void launch_kernel_lds(int id, F kernel, dim3 grid, dim3 block, size_t lds, hipStream_t s,
+                              Args... args) {
   hipEvent_t a, b;
   if (profile_events(id, &a, &b))
-    hipExtLaunchKernelGGL(kernel, grid, block, 0, s, a, b, 0, args...);
+    hipExtLaunchKernelGGL(kernel, grid, block, lds, s, a, b, 0, args...);
   else
-    hipLaunchKernelGGL(kernel, grid, block, 0, s, args...);
+    hipLaunchKernelGGL(kernel, grid, block, lds, s, args...);
   if (debug_on()) debug_after_launch(s);
+}
+
+template <class F, class... Args>
+inline void launch_kernel(int id, F kernel, dim3 grid, dim3 block, hipStream_t s,
+                          Args... args) {
+  launch_kernel_lds(id, kernel, grid, block, 0, s, args...);
 }
 
 }  // namespace ckv

@@ -76,3 +76,18 @@ def attend64(pool, block, req, pos, q, idx):
             d = 130 * U24 * (x.abs() @ K.abs().T).amax(-1) * SCALE
             tol[t, rows] = (2 * d + (len(at) + 64) * U24) * V.abs().max()
     return out, lse, tol
+
+
+def poison(pool, b, h, p, what, value=float("nan")):
+    """Makes a row of K or V (``what``) no numbers, on the device and in the plain form."""
+    page = int(pool.table[b, p // pool.page])
+    at = (page, h, p % pool.page)
+    if pool.kind == "bf16":
+        getattr(pool, what)[at] = value
+    elif pool.kind == "e4m3":
+        value = float("nan")                     # its codes have no infinities
+        getattr(pool, what)[at] = 0x7F
+    else:
+        value = float("nan")
+        getattr(pool, what + "_exps")[at] = 255
+    getattr(pool, what.upper())[b, h, p] = value

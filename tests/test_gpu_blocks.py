@@ -8,7 +8,7 @@ import pytest
 import torch
 
 import paper_2607_26475_amd as ckv
-from blocks_helpers import attend64, block_there, landmarks64, select64
+from blocks_helpers import attend64, block_there, landmarks64, poison, select64
 from e2m1_helpers import Pool4
 from paged_helpers import D, SCALE, Pool
 
@@ -267,6 +267,78 @@ def test_captured_and_replayed_and_on_another_stream(new, G):
         torch.cuda.synchronize()
         for a, b in ((c.marks, e.marks), (c.idx, e.idx), (c.out, e.out), (c.lse, e.lse)):
             assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("Hkv,G,block,k,page,order,new", [
+    (2, 16, 64, 6, 16, "pairs", 300), (8, 4, 32, 17, 64, "heads", 280),
+    (16, 1, 128, 3, 16, "rows", 560), (4, 8, 256, 2, 32, "heads", 290)])
+def test_many_tokens_of_a_bf16_cache(Hkv, G, block, k, page, order, new):
+    """Four tiles a workgroup: chunks of three requests, holes, padding and a
+    request's tokens apart from each other; every seventh token is compared."""
+    _log("many", Hkv, G, block, k, page, order, new)
+    lens = [900, 640, 1001]
+    pool = make("bf16", lens, Hkv, page, seed=G, order=order, holes=[(0, 1), (2, 3), (1, 0)],
+                max_ctx=1010)
+    tokens = ragged_tokens(lens, new)
+    tokens = tokens[:100] + [(0, -1), (3, 5), (0, 0), (2, 31)] + tokens[100:-5] + [(1, 500)]
+    req, pos = [t[0] for t in tokens], [t[1] for t in tokens]
+    g = torch.Generator().manual_seed(new)
+    q = torch.randn((len(tokens), G * Hkv, D), generator=g).to(torch.bfloat16)
+    c = Call(pool, G, block, k, len(tokens))
+    r, p, qd = _i32(req), _i32(pos), q.to(DEV)
+    c.landmarks()
+    c.select(r, p, qd)
+    idx = c.idx.cpu()
+    c.attend(r, p, qd)
+    some = sorted({*range(0, len(tokens), 7), 100, 101, 102, 103, len(tokens) - 1})
+    rq, ps = [req[i] for i in some], [pos[i] for i in some]
+    assert torch.equal(idx[some], select64(pool, block, k, rq, ps, q[some], c.marks.cpu()))
+    out, lse, tol = attend64(pool, block, rq, ps, q[some], idx[some])
+    got, gl = c.out.cpu().double()[some], c.lse.cpu().double()[some]
+    none = lse == -math.inf
+    assert none.any() and torch.all(got[none] == 0) and torch.all(gl[none] == -math.inf)
+    err = (got - out).abs().amax(-1)
+    assert torch.all(err <= tol), float((err / tol.clamp(min=1e-30)).max())
+    assert torch.all(((gl - lse).abs() <= tol + 2.0 ** -22 * lse.abs() + 1e-6)[~none])
+
+
+@pytest.mark.parametrize("kind,new,Hkv,G", [
+    ("bf16", 40, 2, 4), ("e4m3", 40, 2, 2), ("e2m1", 40, 2, 8), ("bf16", 3, 2, 1),
+    ("e2m1", 3, 2, 4), ("bf16", 780, 2, 16), ("bf16", 820, 8, 4)])
+def test_rows_that_are_no_numbers_reach_only_who_sees_them(kind, new, Hkv, G):
+    """NaN and infinite rows of K and V, seen by some tokens of a tile and not by
+    others (another block, a later position): the others' outputs are as without."""
+    _log("no numbers", kind, new, Hkv, G)
+    n, block, k = 1000, 32, 4
+    pool = make(kind, [n], Hkv, 16, seed=new)
+    g = torch.Generator().manual_seed(5)
+    pos = list(range(n - new, n))
+    own = torch.tensor(pos) // block
+    idx = torch.full((new, Hkv, k), -1, dtype=torch.int32)
+    for t in range(new):
+        for h in range(Hkv):
+            few = sorted(torch.randperm(6, generator=g)[:k - 1].tolist())
+            idx[t, h] = torch.tensor(few + [int(own[t])])
+    poison(pool, 0, 0, 2 * block + 7, "v")
+    poison(pool, 0, Hkv - 1, 4 * block, "v", math.inf)
+    poison(pool, 0, Hkv - 1, 5 * block + 31, "k")
+    poison(pool, 0, 0, n - 1, "v")          # of the last token's own block
+    poison(pool, 0, Hkv - 1, n - 2, "k", -math.inf if kind == "bf16" else 0)
+    q = torch.randn((new, G * Hkv, D), generator=g).to(torch.bfloat16)
+    c = Call(pool, G, block, k, new)
+    c.idx.copy_(idx)
+    c.attend(_i32([0] * new), _i32(pos), q.to(DEV))
+    some = sorted({*range(0, new, max(1, new // 60)), *range(max(0, new - 20), new)})
+    out, lse, tol = attend64(pool, block, [0] * len(some), [pos[i] for i in some], q[some],
+                             idx[some])
+    got = c.out.cpu().double()[some]
+    good = torch.isfinite(out)
+    assert good.any() and not good.all()
+    assert torch.equal(torch.isfinite(got), good)
+    rows = good.all(-1)
+    assert rows.any()
+    err = (got - out)[rows].abs().amax(-1)
+    assert torch.all(err <= tol[rows])
 
 
 def test_debug_mode_names_bad_tokens():
