@@ -19,12 +19,51 @@ __device__ __forceinline__ Token token_of(const BlockTokens& a, int64_t t) {
   return x;
 }
 
+// ---- reductions over a wave --------------------------------------------------------
+// By lane moves alone (an LDS round trip at each of six steps would be the latency of
+// what one wave does here): rows of 16 by rotations, then rows and halves exchanged.
+// The result is the same in every lane.
+template <class Op>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t x, Op op) {
+  x = op(x, dpp_u32<0x128, 0xF, false>(x));  // row_ror
+  x = op(x, dpp_u32<0x124, 0xF, false>(x));
+  x = op(x, dpp_u32<0x122, 0xF, false>(x));
+  x = op(x, dpp_u32<0x121, 0xF, false>(x));
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op(a[0], a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return __builtin_amdgcn_readfirstlane(op(b[0], b[1]));
+}
+
+__device__ __forceinline__ uint32_t wave_min_u32(uint32_t x) {
+  return wave_reduce(x, [](uint32_t a, uint32_t b) { return min(a, b); });
+}
+
+template <class Op>
+__device__ __forceinline__ float wave_reduce_f32(float x, Op op) {
+  return __uint_as_float(wave_reduce(__float_as_uint(x), [op](uint32_t a, uint32_t b) {
+    return __float_as_uint(op(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+
+__device__ __forceinline__ float wave_min_f32(float x) {
+  return wave_reduce_f32(x, [](float a, float b) { return fminf(a, b); });
+}
+
+__device__ __forceinline__ float wave_max_f32(float x) {
+  return wave_reduce_f32(x, [](float a, float b) { return fmaxf(a, b); });
+}
+
+__device__ __forceinline__ float wave_sum_f32(float x) {
+  return wave_reduce_f32(x, [](float a, float b) { return a + b; });
+}
+
 // ---- landmarks -------------------------------------------------------------------
 // A wave a block: lane (s, c) adds elements [8c, 8c + 8) of rows s, s + 4, ... in
 // fp64, the four sums are added in one order, and the mean is rounded once.  Blocks
 // are those from first[b]'s on, `slices` workgroups of four waves a unit over them,
 // so that the grid does not grow with max_ctx where only the last block is new.
-constexpr int kMarkThreads = 256;
+constexpr int kMarkThreads = 256, kMarkRows = 64;  // rows in flight
 
 template <Kind KIND>
 __global__ __launch_bounds__(kMarkThreads) void k_block_marks(MarkArgs a) {
@@ -40,30 +79,34 @@ __global__ __launch_bounds__(kMarkThreads) void k_block_marks(MarkArgs a) {
     const int p0 = (int)(j << a.lb), end = min(p0 + block, n);
     double sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     int rows = 0;  // of this lane
-    for (int p = p0; p < end; p += 16) {  // 16 positions of one page
-      const int page = table[p >> a.pg.shift];
-      if ((unsigned)page >= (unsigned)a.pg.num_pages) continue;
-      u32x4 w[4];
-      uint32_t e[4];
+    for (int p = p0; p < end; p += kMarkRows) {  // 16 positions are of one page
+      int page[kMarkRows / 16];
+      u32x4 w[kMarkRows / 4];
+      uint32_t e[kMarkRows / 4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < kMarkRows / 16; ++i)
+        page[i] = table[min(p + 16 * i, end - 1) >> a.pg.shift];
+#pragma unroll
+      for (int i = 0; i < kMarkRows / 4; ++i) {
         const int row = min(p + 4 * i + s, end - 1);
-        const uint8_t* src = a.pg.k + row_offset(a.pg, page, h, row) + row_part(KIND) * c;
+        // (rows past the end are of the last one's page)
+        const int there = (unsigned)page[i >> 2] < (unsigned)a.pg.num_pages ? page[i >> 2] : 0;
+        const uint8_t* src = a.pg.k + row_offset(a.pg, there, h, row) + row_part(KIND) * c;
         e[i] = 0;
         if (KIND == Kind::kBf16) {
           w[i] = *reinterpret_cast<const u32x4*>(src);
         } else if (KIND == Kind::kE4M3) {
           const uint2 x = *reinterpret_cast<const uint2*>(src);
           w[i] = u32x4{x.x, x.y, 0u, 0u};
-          e[i] = a.pg.k_exps[exp_offset(a.pg, page, h, row)];
+          e[i] = a.pg.k_exps[exp_offset(a.pg, there, h, row)];
         } else {
           w[i] = u32x4{*reinterpret_cast<const uint32_t*>(src), 0u, 0u, 0u};
-          e[i] = a.pg.k_exps[4 * exp_offset(a.pg, page, h, row) + (c >> 2)];
+          e[i] = a.pg.k_exps[4 * exp_offset(a.pg, there, h, row) + (c >> 2)];
         }
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (p + 4 * i + s >= end) break;
+      for (int i = 0; i < kMarkRows / 4; ++i) {
+        if (p + 4 * i + s >= end || (unsigned)page[i >> 2] >= (unsigned)a.pg.num_pages) continue;
         ++rows;
         uint4 y = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
         if (KIND == Kind::kE4M3) y = e4m3_octet(make_uint2(y.x, y.y));
@@ -78,25 +121,27 @@ __global__ __launch_bounds__(kMarkThreads) void k_block_marks(MarkArgs a) {
     rows += __shfl_xor(rows, 16);
     rows += __shfl_xor(rows, 32);
     if (rows == 0) continue;  // for the whole wave
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      sum[k] += __shfl_xor(sum[k], 16);
-      sum[k] += __shfl_xor(sum[k], 32);
-    }
-    if (s != 0) continue;
-    uint32_t w[4];
+    // the four lanes of eight channels add them up, half of them each, then a quarter
+    double four[4], two[2];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      uint32_t bits[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const double mean = sum[2 * k + i] / rows;
-        bits[i] = mean - mean == 0.0 ? f64_to_bf16_rne(mean) : 0x7fc0u;
-      }
-      w[k] = bits[0] | bits[1] << 16;
+      const double other = __shfl_xor(s & 1 ? sum[k] : sum[4 + k], 16);
+      four[k] = (s & 1 ? sum[4 + k] : sum[k]) + other;
     }
-    uint16_t* dst = a.marks + ((int64_t)unit * a.nb + j) * kD + 8 * c;
-    *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const double other = __shfl_xor(s & 2 ? four[k] : four[2 + k], 32);
+      two[k] = (s & 2 ? four[2 + k] : four[k]) + other;
+    }
+    uint32_t bits[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const double mean = two[i] / rows;
+      bits[i] = mean - mean == 0.0 ? f64_to_bf16_rne(mean) : 0x7fc0u;
+    }
+    uint16_t* dst =
+        a.marks + ((int64_t)unit * a.nb + j) * kD + 8 * c + 4 * (s & 1) + 2 * (s >> 1);
+    *reinterpret_cast<uint32_t*>(dst) = bits[0] | bits[1] << 16;
   }
 }
 
@@ -200,7 +245,7 @@ __global__ __launch_bounds__(kSelThreads) void k_block_scores(BlockSelectArgs a)
       }
     }
   }
-  norm = wave_max(norm);
+  norm = wave_max_f32(norm);
   if (lane == 0) most[wave] = norm;
   __syncthreads();
   if (threadIdx.x == 0)
@@ -217,12 +262,6 @@ __global__ __launch_bounds__(kSelThreads) void k_block_scores(BlockSelectArgs a)
 //   The r-th best is found by halving an interval of scores until exactly r lie
 // above (8 halvings or so; ties end it at neighbouring floats).  The scores of up
 // to 64 V blocks are held in registers, of more read again at each halving.
-__device__ __forceinline__ float wave_min(float x) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) x = fminf(x, __shfl_xor(x, o));
-  return x;
-}
-
 // The group's best score of a block in fp64, the same in every lane: 64 / G lanes
 // a head, each 2 G channels in order.
 template <int G>
@@ -298,8 +337,8 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
   float sure = -INFINITY, maybe = INFINITY;
   int few = 0, mine = -1;
   if (avail > want) {
-    lo_s = wave_min(lo_s);
-    hi_s = wave_max(hi_s);
+    lo_s = wave_min_f32(lo_s);
+    hi_s = wave_max_f32(hi_s);
     sure = INFINITY;
     if (want > 0) {
       uint32_t lo = order_key(lo_s), hi = order_key(hi_s) + 1;  // above(lo) > want > above(hi)
@@ -327,8 +366,8 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
         if (s >= cut) in = fminf(in, s);
         else out_s = fmaxf(out_s, s);
       });
-      in = wave_min(in);
-      out_s = wave_max(out_s);
+      in = wave_min_f32(in);
+      out_s = wave_max_f32(out_s);
       const uint16_t* q = t.q + ((int64_t)tok * t.Hq + h * G) * kD;
       float qq = 0.f, mm = 0.f;
 #pragma unroll
@@ -337,11 +376,11 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
         const float y = __uint_as_float(w << 16), z = __uint_as_float(w & 0xffff0000u);
         qq = fmaf(y, y, fmaf(z, z, qq));
       }
-      qq = wave_sum(qq);
+      qq = wave_sum_f32(qq);
       const int per = (16 / G) * a.row_tiles;
       const float* norms = a.norms + ((int64_t)(tok / per) * t.Hkv + h) * a.chunks;
       for (int i = lane; i < (n + a.cols - 1) / a.cols; i += 64) mm = fmaxf(mm, norms[i]);
-      mm = wave_max(mm);
+      mm = wave_max_f32(mm);
       // (squares that vanish are below 2^-126: the bounds of 2^-100 cover them)
       const float e2 = 0x1p-14f * sqrtf(fmaxf(qq, 0x1p-100f)) * sqrtf(fmaxf(mm, 0x1p-100f));
       sure = in + e2;
@@ -711,31 +750,44 @@ __global__ __launch_bounds__(kBlockThreads, 3) void k_block_attn(BlockAttnArgs a
   }
 }
 
-// Joins a tile's pieces in order: a thread has a row and four channels.
+// Joins a tile's pieces: a wave has a row, each lane a piece's maximum and sum; then
+// half a wave adds the even pieces' channels, four a lane, the other the odd ones'.
 __global__ __launch_bounds__(kBlockThreads) void k_block_merge(BlockAttnArgs a) {
-  const int h = blockIdx.x % a.t.Hkv, tile = blockIdx.x / a.t.Hkv;
+  const int lane = threadIdx.x & 63, half = lane >> 5, d = 4 * (lane & 31);
+  const int row = (blockIdx.x & 3) * 4 + (threadIdx.x >> 6), unit = blockIdx.x >> 2;
+  const int h = unit % a.t.Hkv, tile = unit / a.t.Hkv;
   const int64_t t0 = (int64_t)tile * (16 >> a.t.lg);
-  const float* part = a.part + ((int64_t)tile * a.t.Hkv + h) * a.pieces * 16 * kPartStride;
-  for (int i = threadIdx.x; i < 16 * (kD / 4); i += kBlockThreads) {
-    const int row = i >> 5, d = 4 * (i & 31);
-    const float* p0 = part + (int64_t)row * kPartStride;
-    Partial p;
-    p.M = -INFINITY;
-    p.L = 0.f;
-    p.o = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int k = 0; k < a.pieces; ++k) p.M = fmaxf(p.M, p0[(int64_t)k * 16 * kPartStride]);
-    for (int k = 0; k < a.pieces; ++k) {
-      const float* x = p0 + (int64_t)k * 16 * kPartStride;
-      const float f = x[0] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x[0] - p.M);
-      const float4 o = *reinterpret_cast<const float4*>(x + 4 + d);
-      p.L = fmaf(f, x[1], p.L);
-      p.o.x = fmaf(f, o.x, p.o.x);
-      p.o.y = fmaf(f, o.y, p.o.y);
-      p.o.z = fmaf(f, o.z, p.o.z);
-      p.o.w = fmaf(f, o.w, p.o.w);
+  const float* part = a.part + ((int64_t)unit * a.pieces * 16 + row) * kPartStride;
+  auto piece = [&](int k) { return part + (int64_t)k * 16 * kPartStride; };
+  static_assert(kMaxPieces <= 64, "a lane a piece");
+  float m = -INFINITY, l = 0.f;
+  if (lane < a.pieces) m = piece(lane)[0], l = piece(lane)[1];
+  Partial p;
+  p.M = wave_max_f32(m);
+  const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - p.M);
+  p.L = wave_sum_f32(f * l);
+  p.o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < a.pieces; k0 += 16) {
+    float4 o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      o[i] = *reinterpret_cast<const float4*>(piece(min(k0 + 2 * i + half, a.pieces - 1)) + 4 + d);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int k = k0 + 2 * i + half;
+      const float w = __shfl(f, k & 63);
+      if (k >= a.pieces) continue;
+      p.o.x = fmaf(w, o[i].x, p.o.x);
+      p.o.y = fmaf(w, o[i].y, p.o.y);
+      p.o.z = fmaf(w, o[i].z, p.o.z);
+      p.o.w = fmaf(w, o[i].w, p.o.w);
     }
-    store_block_row(a, t0, h, row, d, p);
   }
+  p.o.x += __shfl_xor(p.o.x, 32);
+  p.o.y += __shfl_xor(p.o.y, 32);
+  p.o.z += __shfl_xor(p.o.z, 32);
+  p.o.w += __shfl_xor(p.o.w, 32);
+  if (half == 0) store_block_row(a, t0, h, row, d, p);
 }
 
 // ---- attention of many tokens --------------------------------------------------------
@@ -760,17 +812,6 @@ struct ManyLds {
   alignas(256) uint8_t rows[4 * kPagedTile * kRowBytes];  // [buffer][K, V][row]
   int32_t counts[64];
 };
-
-__device__ __forceinline__ uint32_t wave_min_u32(uint32_t x) {
-  x = min(x, dpp_u32<0x128, 0xF, false>(x));  // row_ror
-  x = min(x, dpp_u32<0x124, 0xF, false>(x));
-  x = min(x, dpp_u32<0x122, 0xF, false>(x));
-  x = min(x, dpp_u32<0x121, 0xF, false>(x));
-  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-  x = min(a[0], a[1]);
-  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-  return __builtin_amdgcn_readfirstlane(min(b[0], b[1]));
-}
 
 // 32 positions of a block, the same for the workgroup.
 struct ManyStep {
@@ -1151,7 +1192,7 @@ hipError_t launch_block_attn(const BlockAttnArgs& a, Kind kind, hipStream_t s) {
   });
   const hipError_t e = launch_status();
   if (e != hipSuccess || a.pieces == 1) return e;
-  launch_kernel(CKV_K_BLOCK_MERGE, k_block_merge, dim3((unsigned)units), dim3(kBlockThreads), s,
+  launch_kernel(CKV_K_BLOCK_MERGE, k_block_merge, dim3((unsigned)(4 * units)), dim3(kBlockThreads), s,
                 a);
   return launch_status();
 }
