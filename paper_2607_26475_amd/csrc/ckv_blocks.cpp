@@ -66,8 +66,10 @@ void cut_scores(BlockSelectArgs* a) {
   auto wgs = [&](int tiles, int cols) {
     return tiles_of(a->t, tiles) * a->t.Hkv * ((a->t.nb + cols - 1) / cols);
   };
+  // (about a token a request: four requests a tile and more, a wave each)
+  const int least = a->t.n <= a->t.B ? 16 : kMarkCols;
   a->row_tiles = wgs(4, kMarkCols) >= kScoreWgs ? 4 : 1;
-  a->cols = kMarkCols;
+  a->cols = least;
   while (a->cols < 1024 && wgs(a->row_tiles, 2 * a->cols) >= kScoreWgs) a->cols *= 2;
   a->chunks = (a->t.nb + a->cols - 1) / a->cols;
 }

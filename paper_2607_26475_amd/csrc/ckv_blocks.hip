@@ -162,10 +162,18 @@ __device__ __forceinline__ bool block_there(const PagedPages& pg, TablePtr table
 // head's; their largest |.|^2 is left for the selection's error bound.
 constexpr int kSelThreads = 256;
 
+// Sixteen landmarks of a request on their way.
+struct ScoreStep {
+  uint4 w[4];
+  int req, j, stop;  // j: the lane's, below stop
+  bool there;
+};
+
 template <int G, int MT>
-__global__ __launch_bounds__(kSelThreads) void k_block_scores(BlockSelectArgs a) {
+__global__ __launch_bounds__(kSelThreads, 4) void k_block_scores(BlockSelectArgs a) {
   constexpr int kTok = 16 / G, kTokens = kTok * MT;
   __shared__ int32_t req[kTokens], own[kTokens];
+  __shared__ int32_t each_req[kTokens], each_last[kTokens];  // requests, once each
   __shared__ float most[4];
   const BlockTokens& t = a.t;
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -173,13 +181,12 @@ __global__ __launch_bounds__(kSelThreads) void k_block_scores(BlockSelectArgs a)
   const int h = blockIdx.x % t.Hkv, rest = blockIdx.x / t.Hkv;
   const int tile = rest / a.chunks, chunk = rest - tile * a.chunks;
   const int64_t t0 = (int64_t)tile * kTokens;
+  const Token x = token_of(t, lane < kTokens ? t0 + lane : (int64_t)t.n);
+  const int my_own = x.pos >> t.lb;  // -1: none
   if (threadIdx.x < kTokens) {
-    const Token x = token_of(t, t0 + threadIdx.x);
-    req[threadIdx.x] = x.req;
-    own[threadIdx.x] = x.pos >> t.lb;  // -1: none
+    req[lane] = x.req;
+    own[lane] = my_own;
   }
-  __syncthreads();
-  const int my_req = lane < kTokens ? req[lane] : -1, my_own = lane < kTokens ? own[lane] : -1;
   bf16x8 q[MT][4];
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
@@ -188,62 +195,85 @@ __global__ __launch_bounds__(kSelThreads) void k_block_scores(BlockSelectArgs a)
 #pragma unroll
     for (int f = 0; f < 4; ++f) q[m][f] = as_bf16x8(ld16(row + 32 * f + 8 * g));
   }
-  float norm = 0.f;
-  uint64_t left = __ballot(my_req >= 0);
+  int requests = 0;
+  uint64_t left = __ballot(x.req >= 0);
   while (left) {
-    const int rq = __builtin_amdgcn_readlane(my_req, __builtin_ctzll(left));
-    const bool member = my_req == rq;
+    const int rq = __builtin_amdgcn_readlane(x.req, __builtin_ctzll(left));
+    const bool member = x.req == rq;
     left &= ~__ballot(member);
-    int last = member ? my_own : 0;  // blocks that some token of the request has behind it
+    // blocks that some token of the request has behind it
+    const int last = (int)~wave_min_u32(member ? ~(uint32_t)my_own : ~0u);
+    if (threadIdx.x == 0) {
+      each_req[requests] = rq;
+      each_last[requests] = last;
+    }
+    ++requests;
+  }
+  __syncthreads();
+  // A chunk's steps of 16 landmarks, request by request, go to the waves in turn.
+  const int per = a.cols / 16, items = requests * per;
+  int item = wave;
+  auto ask = [&](ScoreStep& s) {
+    for (; item < items; item += 4) {
+      const int i = item / per, j0 = chunk * a.cols + 16 * (item - i * per);
+      s.stop = min((chunk + 1) * a.cols, __builtin_amdgcn_readfirstlane(each_last[i]));
+      if (j0 >= s.stop) continue;
+      s.req = __builtin_amdgcn_readfirstlane(each_req[i]);
+      s.j = j0 + r;
+      const int j = min(s.j, s.stop - 1);
+      const uint16_t* mark = a.marks + (((int64_t)s.req * t.Hkv + h) * t.nb + j) * kD + 8 * g;
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) last = max(last, __shfl_xor(last, o));
-    const int stop = min((chunk + 1) * a.cols, last);
-    const TablePtr table = table_of(a.pg, rq);
-    const uint16_t* marks = a.marks + ((int64_t)rq * t.Hkv + h) * t.nb * kD;
-    for (int j0 = chunk * a.cols + 16 * wave; j0 < stop; j0 += 64) {
-      const int j = j0 + r;
-      const uint16_t* mark = marks + (int64_t)min(j, stop - 1) * kD + 8 * g;
-      uint4 w[4];
+      for (int f = 0; f < 4; ++f) s.w[f] = ld16(mark + 32 * f);
+      s.there = block_there(a.pg, table_of(a.pg, s.req), j, t.lb, t.max_ctx) && s.j < s.stop;
+      item += 4;
+      return true;
+    }
+    return false;
+  };
+  float norm = 0.f;
+  constexpr bool kAhead = MT == 1;  // (registers for it, and fewer waves to take turns)
+  ScoreStep s, next;
+  bool more = ask(s);
+  while (more) {
+    if (kAhead) more = ask(next);
+    float sq = 0.f;
 #pragma unroll
-      for (int f = 0; f < 4; ++f) w[f] = ld16(mark + 32 * f);
-      const bool there = j < stop && block_there(a.pg, table, j, t.lb, t.max_ctx);
-      float sq = 0.f;
+    for (int f = 0; f < 4; ++f) {
+      float y[8];
+      unpack8(s.w[f], y);
 #pragma unroll
-      for (int f = 0; f < 4; ++f) {
-        float x[8];
-        unpack8(w[f], x);
+      for (int i = 0; i < 8; ++i) sq = fmaf(y[i], y[i], sq);
+    }
+    sq += __shfl_xor(sq, 16);
+    sq += __shfl_xor(sq, 32);
+    if (s.there) norm = fmaxf(norm, sq);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sq = fmaf(x[i], x[i], sq);
+    for (int m = 0; m < MT; ++m) {
+      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int f = 0; f < 4; ++f) acc = mfma_16x16x32(q[m][f], as_bf16x8(s.w[f]), acc);
+      // register i of lane (g, r): query row 4g + i, landmark r
+      constexpr int kPer = G < 4 ? 4 / G : 1;  // tokens of a lane
+      float best[kPer];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        best[i] = acc[i * (G < 4 ? G : 4)];
+#pragma unroll
+        for (int k = 1; k < (G < 4 ? G : 4); ++k)
+          best[i] = fmaxf(best[i], acc[i * (G < 4 ? G : 4) + k]);
       }
-      sq += __shfl_xor(sq, 16);
-      sq += __shfl_xor(sq, 32);
-      if (there) norm = fmaxf(norm, sq);
+      if (G >= 8) best[0] = fmaxf(best[0], __shfl_xor(best[0], 16));
+      if (G == 16) best[0] = fmaxf(best[0], __shfl_xor(best[0], 32));
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int f = 0; f < 4; ++f) acc = mfma_16x16x32(q[m][f], as_bf16x8(w[f]), acc);
-        // register i of lane (g, r): query row 4g + i, landmark r
-        constexpr int kPer = G < 4 ? 4 / G : 1;  // tokens of a lane
-        float best[kPer];
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          best[i] = acc[i * (G < 4 ? G : 4)];
-#pragma unroll
-          for (int k = 1; k < (G < 4 ? G : 4); ++k)
-            best[i] = fmaxf(best[i], acc[i * (G < 4 ? G : 4) + k]);
-        }
-        if (G >= 8) best[0] = fmaxf(best[0], __shfl_xor(best[0], 16));
-        if (G == 16) best[0] = fmaxf(best[0], __shfl_xor(best[0], 32));
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const int tok = m * kTok + 4 * g / G + i;
-          if ((4 * g) % G == 0 && req[tok] == rq && j < own[tok] && j < stop)
-            a.scores[((t0 + tok) * t.Hkv + h) * t.nb + j] =
-                there ? fmaxf(best[i], -INFINITY) : -INFINITY;  // of NaN: -inf
-        }
+      for (int i = 0; i < kPer; ++i) {
+        const int tok = m * kTok + 4 * g / G + i;
+        if ((4 * g) % G == 0 && req[tok] == s.req && s.j < own[tok] && s.j < s.stop)
+          a.scores[((t0 + tok) * t.Hkv + h) * t.nb + s.j] =
+              s.there ? fmaxf(best[i], -INFINITY) : -INFINITY;  // of NaN: -inf
       }
     }
+    if (kAhead) s = next;
+    else more = ask(s);
   }
   norm = wave_max_f32(norm);
   if (lane == 0) most[wave] = norm;
@@ -262,25 +292,63 @@ __global__ __launch_bounds__(kSelThreads) void k_block_scores(BlockSelectArgs a)
 //   The r-th best is found by halving an interval of scores until exactly r lie
 // above (8 halvings or so; ties end it at neighbouring floats).  The scores of up
 // to 64 V blocks are held in registers, of more read again at each halving.
-// The group's best score of a block in fp64, the same in every lane: 64 / G lanes
-// a head, each 2 G channels in order.
+// Query rows of a group for scores in fp64: 64 / G lanes a head, each 2 G channels.
 template <int G>
-__device__ __forceinline__ double exact_score(const uint16_t* q, const uint16_t* mark) {
-  constexpr int kPer = 64 / G;
-  const int lane = threadIdx.x & 63, head = lane / kPer, at = 2 * G * (lane % kPer);
-  double s = 0.0;
-  for (int c = 0; c < 2 * G; c += 2) {
-    const uint32_t x = *reinterpret_cast<const uint32_t*>(q + head * kD + at + c);
-    const uint32_t y = *reinterpret_cast<const uint32_t*>(mark + at + c);
-    s += (double)__uint_as_float(x << 16) * (double)__uint_as_float(y << 16);
-    s += (double)__uint_as_float(x & 0xffff0000u) * (double)__uint_as_float(y & 0xffff0000u);
+struct GroupRows {
+  static constexpr int kPer = 64 / G;
+  uint32_t w[G];
+  int at;  // of the lane's channels
+  __device__ __forceinline__ void load(const uint16_t* q) {
+    const int lane = threadIdx.x & 63;
+    at = 2 * G * (lane % kPer);
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(q + lane / kPer * kD + at);
+#pragma unroll
+    for (int i = 0; i < G; ++i) w[i] = p[i];
   }
+  // The largest |.|^2 of a head.
+  __device__ __forceinline__ float norm() const {
+    float s = 0.f;
 #pragma unroll
-  for (int o = 1; o < kPer; o <<= 1) s += __shfl_xor(s, o);
+    for (int i = 0; i < G; ++i) {
+      const float y = __uint_as_float(w[i] << 16), z = __uint_as_float(w[i] & 0xffff0000u);
+      s = fmaf(y, y, fmaf(z, z, s));
+    }
 #pragma unroll
-  for (int o = kPer; o < 64; o <<= 1) s = fmax(s, __shfl_xor(s, o));
-  return s;
-}
+    for (int o = 1; o < kPer; o <<= 1) s += __shfl_xor(s, o);
+#pragma unroll
+    for (int o = kPer; o < 64; o <<= 1) s = fmaxf(s, __shfl_xor(s, o));
+    return s;
+  }
+  // The best scores of four blocks, the same in every lane.
+  __device__ __forceinline__ void scores(const uint16_t* marks, const int* j, double* out) const {
+    uint32_t m[4][G];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t* p = reinterpret_cast<const uint32_t*>(marks + (int64_t)j[k] * kD + at);
+#pragma unroll
+      for (int i = 0; i < G; ++i) m[k][i] = p[i];
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      double s = 0.0;
+#pragma unroll
+      for (int i = 0; i < G; ++i) {
+        s += (double)__uint_as_float(w[i] << 16) * (double)__uint_as_float(m[k][i] << 16);
+        s += (double)__uint_as_float(w[i] & 0xffff0000u) *
+             (double)__uint_as_float(m[k][i] & 0xffff0000u);
+      }
+      out[k] = s;
+    }
+#pragma unroll
+    for (int o = 1; o < kPer; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] += __shfl_xor(out[k], o);
+#pragma unroll
+    for (int o = kPer; o < 64; o <<= 1)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) out[k] = fmax(out[k], __shfl_xor(out[k], o));
+  }
+};
 
 __device__ __forceinline__ float float_of_key(uint32_t k) {
   return __uint_as_float(key_floor_bits(k));
@@ -301,6 +369,13 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
     return;
   }
   const int n = x.pos >> t.lb, want = t.k - 1;  // earlier blocks; of them kept
+  // asked for now, used by the error bound
+  GroupRows<G> rows;
+  rows.load(t.q + ((int64_t)tok * t.Hq + h * G) * kD);
+  const int per = (16 / G) * a.row_tiles;
+  const float* norms = a.norms + ((int64_t)(tok / per) * t.Hkv + h) * a.chunks;
+  float mm = 0.f;
+  for (int i = lane; i < (n + a.cols - 1) / a.cols; i += 64) mm = fmaxf(mm, norms[i]);
   const float* scores = a.scores + unit * t.nb;
   const int steps = V ? V : (n + 63) / 64;
   float held[V ? V : 1];
@@ -368,18 +443,7 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
       });
       in = wave_min_f32(in);
       out_s = wave_max_f32(out_s);
-      const uint16_t* q = t.q + ((int64_t)tok * t.Hq + h * G) * kD;
-      float qq = 0.f, mm = 0.f;
-#pragma unroll
-      for (int i = 0; i < G; ++i) {
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(q + i * kD + 2 * lane);
-        const float y = __uint_as_float(w << 16), z = __uint_as_float(w & 0xffff0000u);
-        qq = fmaf(y, y, fmaf(z, z, qq));
-      }
-      qq = wave_sum_f32(qq);
-      const int per = (16 / G) * a.row_tiles;
-      const float* norms = a.norms + ((int64_t)(tok / per) * t.Hkv + h) * a.chunks;
-      for (int i = lane; i < (n + a.cols - 1) / a.cols; i += 64) mm = fmaxf(mm, norms[i]);
+      const float qq = rows.norm();
       mm = wave_max_f32(mm);
       // (squares that vanish are below 2^-126: the bounds of 2^-100 cover them)
       const float e2 = 0x1p-14f * sqrtf(fmaxf(qq, 0x1p-100f)) * sqrtf(fmaxf(mm, 0x1p-100f));
@@ -391,22 +455,36 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
         int need = want;
         each([&](int, float s) { need -= __popcll(__ballot(s > sure)); });
         const uint16_t* marks = a.marks + ((int64_t)x.req * t.Hkv + h) * t.nb * kD;
+        auto between = [&](float s) { return s > -INFINITY && !(s > sure) && !(s < maybe); };
+        int total = 0;
+        each([&](int, float s) { total += __popcll(__ballot(between(s))); });
         double best = 0.0;  // lane i: the i-th best of those between
-        each([&](int i, float s) {
-          uint64_t some = __ballot(s > -INFINITY && !(s > sure) && !(s < maybe));
-          while (some) {
-            const int j = 64 * i + __builtin_ctzll(some);
-            some &= some - 1;
-            const double v = exact_score<G>(q, marks + (int64_t)j * kD);
-            const int at = __popcll(__ballot(lane < few && best >= v));
-            if (at >= need) continue;
-            const double up = __shfl_up(best, 1);
-            const int j_up = __shfl_up(mine, 1);
-            if (lane > at) best = up, mine = j_up;
-            if (lane == at) best = v, mine = j;
-            few = min(few + 1, need);
+        for (int base = 0; base < total; base += 64) {
+          int cand = -1, seen = -base;  // lane i: the i-th of 64 of them, four at a time
+          each([&](int i, float s) {
+            for (uint64_t some = __ballot(between(s)); some; some &= some - 1, ++seen)
+              if (lane == seen) cand = 64 * i + __builtin_ctzll(some);
+          });
+          const int count = min(total - base, 64);
+          for (int c0 = 0; c0 < count; c0 += 4) {
+            int j[4];
+            double v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              j[k] = __builtin_amdgcn_readlane(cand, min(c0 + k, count - 1));
+            rows.scores(marks, j, v);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const int at = __popcll(__ballot(lane < few && best >= v[k]));
+              if (c0 + k >= count || at >= need) continue;
+              const double up = __shfl_up(best, 1);
+              const int j_up = __shfl_up(mine, 1);
+              if (lane > at) best = up, mine = j_up;
+              if (lane == at) best = v[k], mine = j[k];
+              few = min(few + 1, need);
+            }
           }
-        });
+        }
       }
     }
   }
