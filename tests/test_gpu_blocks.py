@@ -214,6 +214,29 @@ def test_lists_of_a_caller():
     assert torch.all((c.out.cpu().double() - out).abs().amax(-1) <= tol)
 
 
+@pytest.mark.parametrize("kind,new,Hkv,G", [("e4m3", 30, 2, 4), ("bf16", 800, 2, 16)])
+def test_a_block_named_twice_counts_once(kind, new, Hkv, G):
+    """The same block twice in a list, blocks past the token's own after them."""
+    n, block = 900, 64
+    pool = make(kind, [n], Hkv, 16, seed=new)
+    pos = torch.arange(n - new, n, dtype=torch.int32)
+    own = pos // block
+    once = torch.full((new, Hkv, 6), -1, dtype=torch.int32)
+    once[:, :, 0], once[:, :, 1] = 0, own[:, None]
+    twice = torch.full((new, Hkv, 6), 1 << 28, dtype=torch.int32)
+    twice[:, :, :3], twice[:, :, 3:5] = 0, own[:, None, None]
+    q = torch.randn((new, G * Hkv, D), generator=torch.Generator().manual_seed(1))
+    q = q.to(torch.bfloat16).to(DEV)
+    got = []
+    for idx in (once, twice):
+        c = Call(pool, G, block, 6, new)
+        c.idx.copy_(idx)
+        c.attend(torch.zeros_like(pos).to(DEV), pos.to(DEV), q)
+        got += [c.out, c.lse]
+    assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3])
+    assert torch.isfinite(got[0]).all()
+
+
 def test_all_blocks_kept_is_the_whole_attention():
     """With every block kept a token gets what the decode attention gives it."""
     lens = [300, 450]
