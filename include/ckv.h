@@ -511,7 +511,8 @@ typedef struct ckv_paged_cache {
  * smallest integer in [-125, 125] with amax <= 6 * 2^e (or 125), the byte e + 127
  * and the codes of x / 2^e rounded to nearest, ties to the even code, 6 at most;
  * where one of the 32 is an infinity or NaN, the byte is 255 and the codes are
- * unspecified.  Every stored value is exact in bf16. */
+ * unspecified.  Every stored value is exact in bf16.  Keys rotated on the way are turned
+ * in fp64 (a code is decided at the middle between two). */
 int ckv_paged_write(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t num_tokens,
                     const int32_t* requests, const int32_t* positions, const uint16_t* k,
                     const uint16_t* v, int64_t kv_token_stride, const ckv_rope* rope,
@@ -551,8 +552,9 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
  * one launch.  Joins go in a fixed order: the same call gives the same bits.  The
  * one launch's join waits for its unit's other workgroups, at most about 20 s:
  * should other launches keep them off the device for so long, the unit's outputs
- * of that call are NaN (later calls and replays are not affected).
- * Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
+ * of that call are NaN (later calls and replays are not affected).  A row of V that
+ * holds NaN or an infinity reaches every token of its request in the call, those before
+ * it too.  Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
 int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
                           int32_t num_tokens, const uint16_t* q, const int32_t* ctx_lens,
                           float scale, float* out, float* lse, void* ws, size_t ws_bytes,
@@ -602,8 +604,9 @@ int ckv_select_blocks(const ckv_shape* shape, const ckv_paged_cache* cache, int3
  *   lse[t][g] = log sum_p exp(l_p)       (natural logarithm; may be NULL)
  * out [num_tokens][Hq][d] fp32, lse [num_tokens][Hq] fp32; nothing to attend to:
  * out = 0, lse = -inf.  Logits, weights and sums are fp32; 0 < scale <= 2^126.  The
- * same call gives the same bits.  Rows at positions up to the tokens' own are written
- * before.  ws: ckv_blocks_workspace_bytes. */
+ * same call gives the same bits.  A block named twice counts once.  Rows of K or V that
+ * hold NaN or infinities reach only the tokens that see them.  Rows at positions up to
+ * the tokens' own are written before.  ws: ckv_blocks_workspace_bytes. */
 int ckv_paged_block_attn(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t block,
                          int32_t k, int32_t num_tokens, const int32_t* requests,
                          const int32_t* positions, const uint16_t* q, const int32_t* idx,

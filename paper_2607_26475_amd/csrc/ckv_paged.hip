@@ -29,6 +29,37 @@ __device__ __forceinline__ float2 cos_sin(double quarters) {
   return make_float2(n == 1 || n == 2 ? -a : a, n >= 2 ? -b : b);
 }
 
+// The same in fp64 throughout (sine to x^17, remainder below 1e-19; cosine to x^18), for
+// keys that are made four bits: a code is decided at the middle between two, where the
+// fp32 form's error makes some codes of a prefill their neighbours (steps of up to half
+// the value).  22 k tokens written and read back 128 -> 135 us.
+__device__ __forceinline__ double2 cos_sin64(double quarters) {
+  const double whole = rint(quarters);
+  const double x = (quarters - whole) * 1.57079632679489661923;
+  const int n = (int)(whole - 4.0 * floor(whole * 0.25));  // 0 .. 3
+  const double x2 = x * x;
+  double s = 1.0 / 355687428096000.0, c = -1.0 / 6402373705728000.0;  // 17!, 18!
+  s = fma(x2, s, -1.0 / 1307674368000.0);
+  s = fma(x2, s, 1.0 / 6227020800.0);
+  s = fma(x2, s, -1.0 / 39916800.0);
+  s = fma(x2, s, 1.0 / 362880.0);
+  s = fma(x2, s, -1.0 / 5040.0);
+  s = fma(x2, s, 1.0 / 120.0);
+  s = fma(x2, s, -1.0 / 6.0);
+  s = fma(x * x2, s, x);
+  c = fma(x2, c, 1.0 / 20922789888000.0);
+  c = fma(x2, c, -1.0 / 87178291200.0);
+  c = fma(x2, c, 1.0 / 479001600.0);
+  c = fma(x2, c, -1.0 / 3628800.0);
+  c = fma(x2, c, 1.0 / 40320.0);
+  c = fma(x2, c, -1.0 / 720.0);
+  c = fma(x2, c, 1.0 / 24.0);
+  c = fma(x2, c, -0.5);
+  c = fma(x2, c, 1.0);
+  const double a = n & 1 ? s : c, b = n & 1 ? c : s;
+  return make_double2(n == 1 || n == 2 ? -a : a, n >= 2 ? -b : b);
+}
+
 constexpr int kRopeThreads = 256;
 constexpr int kRopeTokens = 4;       // tokens of a workgroup in a long call
 constexpr int kRopeMaxPairs = 512;
@@ -46,6 +77,20 @@ __device__ __forceinline__ void rope_table(const RopeSpec& r, const int32_t* pos
     cs.x *= r.scale;
     cs.y *= r.inverse ? -r.scale : r.scale;
     tab[e] = cs;
+  }
+}
+
+// The same from fp64 values, which are left in exact[] too.
+__device__ __forceinline__ void rope_table64(const RopeSpec& r, const int32_t* pos, int t0,
+                                             int tokens, float2* tab, double2* exact) {
+  const int pairs = r.rot >> 1;
+  for (int e = threadIdx.x; e < tokens * pairs; e += kRopeThreads) {
+    const int t = e / pairs, i = e - t * pairs;
+    double2 cs = cos_sin64((double)pos[t0 + t] * (r.inv_freq[i] * 0.63661977236758134308));
+    cs.x *= r.scale;
+    cs.y *= r.inverse ? -r.scale : r.scale;
+    exact[e] = cs;
+    tab[e] = make_float2((float)cs.x, (float)cs.y);
   }
 }
 
@@ -301,6 +346,48 @@ __device__ __forceinline__ void turn8(const RopeSpec& r, const uint16_t* row, in
   }
 }
 
+// x as fp32 so that a rounding to fewer bits gives what it would give for x: where it
+// is not exact, the neighbour with an odd last bit, which is no value of theirs and no
+// middle between two.
+__device__ __forceinline__ float to_odd(double x) {
+  const float f = (float)x;
+  const double less = x - (double)f;  // NaN: none, as for infinities
+  const uint32_t u = __float_as_uint(f);
+  if (!(less != 0.0) || less != less || (u & 1u)) return f;
+  if (f == 0.f) return __uint_as_float(less > 0.0 ? 1u : 0x80000001u);
+  return __uint_as_float((less > 0.0) == (f > 0.f) ? u + 1 : u - 1);
+}
+
+// turn8 in fp64, for rows of four bits.
+template <Turn TURN>
+__device__ __forceinline__ void turn8_64(const RopeSpec& r, const uint16_t* row, int c,
+                                         const double2* cs, u32x4 xv, u32x4 ov, float* y) {
+  float x[8], o[8];
+  unpack8(make_uint4(xv[0], xv[1], xv[2], xv[3]), x);
+  unpack8(make_uint4(ov[0], ov[1], ov[2], ov[3]), o);
+  const int half = r.rot >> 1;
+  if (TURN != Turn::kEach && 8 * c >= r.rot) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) y[j] = x[j];
+    return;
+  }
+  for (int j = 0; j < 8; ++j) {
+    const int e = 8 * c + j;
+    const bool halves = TURN == Turn::kHalf || (TURN == Turn::kEach && r.layout == CKV_ROPE_HALF);
+    const bool first = halves ? e < half : (e & 1) == 0;
+    const int other = halves ? (first ? e + half : e - half) : e ^ 1;
+    if (TURN == Turn::kEach && e >= r.rot) {
+      y[j] = x[j];
+      continue;
+    }
+    const double2 k = cs[halves ? (first ? e : other) : e >> 1];
+    const float p = TURN == Turn::kHalf    ? o[j]
+                    : TURN == Turn::kPairs ? x[j ^ 1]
+                                           : RopeVec<uint16_t>::one(row + other);
+    y[j] = to_odd(fma((double)(first ? -p : p), k.y, (double)x[j] * k.x));
+  }
+}
+
 // Sixteen lanes write a row: lane c its elements [8c, 8c + 8).
 template <Kind KIND>
 __device__ __forceinline__ void store_row(uint8_t* row, uint8_t* exp, int c, const float* y) {
@@ -363,6 +450,8 @@ __device__ __forceinline__ void store_row(uint8_t* row, uint8_t* exp, int c, con
 template <Kind KIND, Turn TURN>
 __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, int per) {
   __shared__ float2 tab[TURN == Turn::kNone ? 1 : kRopeTokens * (kD / 2)];
+  constexpr bool kExact = KIND == Kind::kE2M1 && TURN != Turn::kNone;
+  __shared__ double2 exact[kExact ? kRopeTokens * (kD / 2) : 1];
   __shared__ int64_t row_at[kRopeTokens], exp_at[kRopeTokens];  // of head 0; -1: not written
   const int t0 = blockIdx.x * per, tid = threadIdx.x;
   const int tokens = min(per, a.rope.tokens - t0);
@@ -375,7 +464,8 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
     row_at[tid] = page < 0 ? -1 : row_offset(a.pg, page, 0, pos);
     exp_at[tid] = page < 0 ? -1 : exps_of(KIND) * exp_offset(a.pg, page, 0, pos);
   }
-  if (TURN != Turn::kNone) rope_table(r, a.rope.pos, t0, tokens, tab);
+  if (kExact) rope_table64(r, a.rope.pos, t0, tokens, tab, exact);
+  else if (TURN != Turn::kNone) rope_table(r, a.rope.pos, t0, tokens, tab);
   __syncthreads();
   const int Hkv = a.pg.Hkv, n = tokens * 32 * Hkv;  // (token, head, K | V, 16 lanes)
   for (int e0 = tid; e0 < n; e0 += kRopeBatch * kRopeThreads) {
@@ -408,6 +498,7 @@ __global__ __launch_bounds__(kRopeThreads) void k_paged_write(PagedWriteArgs a, 
       }
       float y[8];
       if (TURN == Turn::kNone || is_v) unpack8(make_uint4(x[i][0], x[i][1], x[i][2], x[i][3]), y);
+      else if (kExact) turn8_64<TURN>(r, src[i], c, exact + tok[i] * (r.rot >> 1), x[i], o[i], y);
       else turn8<TURN>(r, src[i], c, tab + tok[i] * (r.rot >> 1), x[i], o[i], y);
       uint8_t* exp = nullptr;
       if (KIND != Kind::kBf16)

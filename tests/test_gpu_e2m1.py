@@ -166,6 +166,44 @@ def test_write_rotates(interleaved, rot):
         assert torch.equal(values4(vc[at], ve[at]), values4(*e2m1_64(v[i].double())))
 
 
+@pytest.mark.parametrize("interleaved,rot,scale", [(False, 128, 1.0), (True, 128, 0.75),
+                                                   (False, 64, 1.0), (True, 20, 2.0 ** -120)])
+def test_rotated_codes_are_those_of_64_bits(interleaved, rot, scale):
+    """Codes and exponents of keys turned by near and far positions are the ones that
+    the rotation in 64 bits has: its rounding, 2^-52 of an angle, meets the middle
+    between two codes in about one of 10^9 elements."""
+    _log("codes", interleaved, rot, scale)
+    n, page, far = 600, 16, 200000
+    g = torch.Generator().manual_seed(rot)
+    pos = torch.randperm(far, generator=g)[:n].sort().values
+    pos[0] = 0
+    pages = torch.unique(pos // page)
+    table = torch.full((1, far // page), -1, dtype=torch.int32)
+    table[0, pages] = torch.arange(len(pages), dtype=torch.int32)
+    kc, vc = (torch.zeros((len(pages), 1, page, D // 2), dtype=torch.uint8, device=DEV)
+              for _ in "kv")
+    ke, ve = (torch.zeros((len(pages), 1, page, 4), dtype=torch.uint8, device=DEV) for _ in "kv")
+    td = table.to(DEV)
+    cache = ckv.paged_cache_for(kc, vc, td, ke, ve)
+    freq, _ = ckv.rope_frequencies(rot, 10000.0)
+    fd = freq.to(DEV)
+    rope = ckv.rope_for(fd, rot_dim=rot, layout=int(interleaved), scale=scale)
+    x = torch.randn((n, 1, D), generator=g).to(torch.bfloat16)
+    x[5], x[6, 0, 3], x[7, 0, 40] = 0, 2.0 ** -130, 3e38
+    xd = x.to(DEV)
+    ckv.paged_write(ckv.shape_for(1, 1, 1, far), cache, torch.zeros(n, dtype=torch.int32, device=DEV),
+                    pos.int().to(DEV), xd, xd, rope=rope)
+    codes, exps = e2m1_64(rope64(x, pos, freq, rot, interleaved, False, scale))
+    at = (table[0, pos // page].long(), 0, pos % page)
+    assert torch.equal(ke.cpu()[at], exps[:, 0])
+    got, want = kc.cpu()[at], codes[:, 0]
+    # (a zero may have either sign: one of exact terms that cancel)
+    zero = values4(want, exps[:, 0]) == 0
+    assert torch.equal(values4(got, exps[:, 0]), values4(want, exps[:, 0]))
+    assert torch.equal(zero, values4(got, exps[:, 0]) == 0)
+    assert torch.equal(values4(vc.cpu()[at], ve.cpu()[at]), values4(*e2m1_64(x[:, 0].double())))
+
+
 @pytest.mark.parametrize("page,order", [(1, "rows"), (4, "heads"), (16, "pairs"), (128, "heads")])
 def test_read(page, order):
     _log("read", page, order)
