@@ -83,7 +83,8 @@ size_t norm_bytes(const BlockSelectArgs& a) {
 }
 
 // Pieces of a tile's list: as many as fill the device twice over, of two steps a
-// wave at least if every token keeps blocks of its own.
+// wave at least if every token keeps blocks of its own (16 tokens, 32 blocks of 64, 8
+// heads: 46 us all three operators; twice as many pieces 53).
 constexpr int kBlockWgs = 512;
 
 int cut_pieces(const BlockTokens& t) {

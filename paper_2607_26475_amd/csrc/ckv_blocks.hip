@@ -62,7 +62,10 @@ __device__ __forceinline__ float wave_sum_f32(float x) {
 // A wave a block: lane (s, c) adds elements [8c, 8c + 8) of rows s, s + 4, ... in
 // fp64, the four sums are added in one order, and the mean is rounded once.  Blocks
 // are those from first[b]'s on, `slices` workgroups of four waves a unit over them,
-// so that the grid does not grow with max_ctx where only the last block is new.
+// so that the grid does not grow with max_ctx where only the last block is new.  What
+// bounds it are dependent loads (length, first, pages, rows) and the fp64 sums' joining:
+// pages of 64 rows at once, then all rows, and each lane the join of two channels (128
+// new blocks 12.1 -> 5.8 us, those of 2048 new tokens 14.5 -> 9.3).
 constexpr int kMarkThreads = 256, kMarkRows = 64;  // rows in flight
 
 template <Kind KIND>
@@ -159,7 +162,9 @@ __device__ __forceinline__ bool block_there(const PagedPages& pg, TablePtr table
 // query rows x landmarks on 16x16x32 products.  A workgroup has MT tiles of query
 // rows and a chunk of landmarks, whose 16-column steps its waves share out; the
 // tokens of each request in turn.  Landmarks come from the L2, which holds a
-// head's; their largest |.|^2 is left for the selection's error bound.
+// head's; their largest |.|^2 is left for the selection's error bound.  16 tokens over
+// 22 MB of landmarks 10 us; 2048 tokens over 256 landmarks of each of 8 heads 23, of
+// which the 17 MB of scores are 4: short chains of loads and products, 1024 workgroups.
 constexpr int kSelThreads = 256;
 
 // Sixteen landmarks of a request on their way.
@@ -291,7 +296,9 @@ __global__ __launch_bounds__(kSelThreads, 4) void k_block_scores(BlockSelectArgs
 // scores in fp64, the lower block first where these are equal.
 //   The r-th best is found by halving an interval of scores until exactly r lie
 // above (8 halvings or so; ties end it at neighbouring floats).  The scores of up
-// to 64 V blocks are held in registers, of more read again at each halving.
+// to 64 V blocks are held in registers, of more read again at each halving.  A chain of
+// about 2000 instructions of one wave: 13 us for 128 (token, KV head) pairs of up to
+// 1024 blocks, 25 for 16384 of 256.
 // Query rows of a group for scores in fp64: 64 / G lanes a head, each 2 G channels.
 template <int G>
 struct GroupRows {
@@ -514,6 +521,11 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
 // attention; rows whose token does not keep the block, or that lie before the
 // position, are masked.  Few tiles: the steps of a list are cut into pieces, a
 // workgroup each, and joined by a second launch.
+//   Codes have to be made bf16 and V's rows transposed by byte permutes at every step:
+// the vector unit bounds it, 370 instructions a step of 32 four-bit positions (2103
+// tokens, 8 blocks of 128, groups of 8: 135 us; without masks where a step needs none,
+// the maximum raised lazily, three workgroups a CU: 107).  16 tokens of as many
+// requests, 32 blocks of 64 each: 17 us, and 4 of joining.
 constexpr int kBlockThreads = 256;
 constexpr int kStepLg = 5;  // log2 of a wave's positions
 static_assert(1 << kStepLg == kPagedTile, "a step");
@@ -876,7 +888,10 @@ __global__ __launch_bounds__(kBlockThreads) void k_block_merge(BlockAttnArgs a) 
 // operands are made by transposing LDS reads, without byte permutes, and no waves are
 // joined.  All workgroups go through the positions alike, so that a head's L2 has what
 // they need (2048 tokens, 16 of 256 blocks of 64 each: 0.4 GB of 2.4 from behind it;
-// a workgroup a tile reads 5.1, 3.3 of it from behind).
+// a workgroup a tile reads 5.1, 3.3 of it from behind): 297 us, a workgroup a tile 606.
+// What bounds it now is the chain of a step (barrier, the next step's place, products,
+// weights, products: 2 us with four workgroups a CU) of which a wave takes part in half.
+// Three buffers, loads two steps ahead, leave three workgroups a CU: 422 us.
 //   The blocks' order is a merge of the tokens' lists, each lane the cursor of a
 // token: the least head of all is next, the lanes that have it are its tokens.
 //   Rows are 256 bytes, the 16-byte part p of row i = 8 a + b (a < 2) at p ^ (2 b + a):
