@@ -97,12 +97,13 @@ int cut_pieces(const BlockTokens& t) {
 
 // Many tokens of a bf16 cache: four tiles share the staging of a block that one of them
 // keeps.  A tile a workgroup against it, us, 16 blocks of 64, 8 KV heads of 4 query
-// heads: 512 tokens (256 workgroups of four tiles) 202 / 218, 1024 386 / 253, 2048 756 /
-// 304, 1024 tokens and 4 heads of 8 259 / 182; 1500 tokens, 8 heads of 1 (192) 248 / 317.
-// Rows of codes are less to read and have to be made bf16: 2048 tokens e4m3 362 / 359,
-// e2m1 269 / 337.  With fewer tokens a request than four tiles have a block would be of
+// heads: 512 tokens (256 workgroups of four tiles) 161 / 219, 1024 (512) 267 / 252, 2048
+// 487 / 299, 4096 949 / 569; 1024 tokens and 4 heads of 8 (512) 180 / 182, 2048 and 2 of
+// 16 (1024) 211 / 158, 1500 and 8 of 1 (192) 187 / 319; 48 blocks, 2048 tokens 1171 / 619.
+// Rows of codes are less to read and have to be made bf16: 2048 tokens e4m3 297 / 359,
+// e2m1 262 / 337.  With fewer tokens a request than four tiles have a block would be of
 // use to one wave.
-constexpr int kManyWgs = 384;
+constexpr int kManyWgs = 512;
 
 bool many_tokens(const BlockTokens& t, Kind kind) {
   return kind == Kind::kBf16 && (int64_t)t.n >= (int64_t)t.B * (kManyTiles * 16 >> t.lg) &&

@@ -756,7 +756,7 @@ __device__ __forceinline__ void load_score_step(const PagedPages& pg, const Ctx&
       const int first = half_first(p, i, x.n);
       const uint8_t* base = pg.k + row_offset(pg, has ? t.row[i] : 0, x.h, first);
       const int32_t cap = half_last(first, x.n) * pg.row_bytes;
-      s.k[i].load_lines(base, pg.row_bytes, cap, g, r);
+      s.k[i].template load_lines<true>(base, pg.row_bytes, cap, g, r);
       if (KIND == Kind::kE2M1)
         s.k[i].e = pg.k_exps[4 * (exp_offset(pg, has ? t.row[i] : 0, x.h, first) +
                                   min(r, half_last(first, x.n))) + g];

@@ -78,6 +78,19 @@ __device__ __forceinline__ uint32_t ld4_nt(const uint8_t* p) {
   return __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p));
 }
 
+// N bytes of a row: streamed past the caches, or (STREAM false) kept for others.
+template <int N, bool STREAM>
+__device__ __forceinline__ auto ld_row(const uint8_t* p) {
+  if constexpr (N == 16) {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p);
+    return STREAM ? ld16_nt(q) : ld16(q);
+  } else if constexpr (N == 8) {
+    return STREAM ? ld8_nt(p) : *reinterpret_cast<const uint2*>(p);
+  } else {
+    return STREAM ? ld4_nt(p) : *reinterpret_cast<const uint32_t*>(p);
+  }
+}
+
 // What a kernel only reads, for scalar loads where the index is the wave's.
 typedef const __attribute__((address_space(4))) int32_t* TablePtr;
 
@@ -140,11 +153,11 @@ struct KRaw {
   // stay for the second): each load takes both halves of a line of eight rows, the
   // second half through the lanes of r >= 8; lanes r and r ^ 8 then swap what
   // belongs to the other's row.
+  template <bool STREAM>
   __device__ __forceinline__ void load_lines(const uint8_t* base, int32_t row_bytes, int32_t cap,
                                              int g, int r) {
     if constexpr (KIND == Kind::kE2M1) {  // rows of 64 bytes: 16 of them a load
-      w[0] = ld16_nt(reinterpret_cast<const uint16_t*>(base + (uint32_t)min(r * row_bytes, cap) +
-                                                       16 * g));
+      w[0] = ld_row<16, STREAM>(base + (uint32_t)min(r * row_bytes, cap) + 16 * g);
       return;
     }
     const uint8_t* p = base + 8 * (r & 8) + 16 * g;
@@ -152,7 +165,7 @@ struct KRaw {
                             (uint32_t)min(((r & 7) + 8) * row_bytes, cap)};
 #pragma unroll
     for (int i = 0; i < kN; ++i)
-      w[i] = ld16_nt(reinterpret_cast<const uint16_t*>(p + at[i & 1] + 128 * (i >> 1)));
+      w[i] = ld_row<16, STREAM>(p + at[i & 1] + 128 * (i >> 1));
   }
   __device__ __forceinline__ void swap_halves(int r) {
     const bool lo = r < 8;
@@ -263,7 +276,7 @@ __device__ __forceinline__ int64_t half_base(const PagedPages& pg, const Ctx& x,
   return row_offset(pg, max(at.page[i], 0), x.h, at.first[i]);
 }
 
-template <Kind KIND, bool WIDE>
+template <Kind KIND, bool WIDE, bool STREAM = true>
 __device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const TileAt<WIDE>& at,
                                        Tile<KIND>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -271,14 +284,14 @@ __device__ __forceinline__ void load_k(const PagedPages& pg, const Ctx& x, const
   for (int i = 0; i < 2; ++i) {
     const int page = max(at.page[i], 0), row = min(at.first[i] + r, x.n - 1);
     if constexpr (WIDE)
-      t.k[i].load_lines(pg.k + half_base(pg, x, at, i), pg.row_bytes, at.cap[i], g, r);
+      t.k[i].template load_lines<STREAM>(pg.k + half_base(pg, x, at, i), pg.row_bytes, at.cap[i], g, r);
     else
       t.k[i].load(pg.k + row_offset(pg, page, x.h, row), g);
     if (KIND == Kind::kE2M1) t.k[i].e = pg.k_exps[4 * exp_offset(pg, page, x.h, row) + g];
   }
 }
 
-template <Kind KIND, bool WIDE>
+template <Kind KIND, bool WIDE, bool STREAM = true>
 __device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const TileAt<WIDE>& at,
                                        Tile<KIND>& t) {
   const int lane = threadIdx.x & 63, g = lane >> 4, r = lane & 15;
@@ -331,12 +344,12 @@ __device__ __forceinline__ void load_v(const PagedPages& pg, const Ctx& x, const
       p = pg.v + row_offset(pg, max(at.v_page[j], 0), x.h, min(at.first[i] + row, x.n - 1));
     uint32_t* v = t.v[j];
     if constexpr (KIND == Kind::kE2M1) {
-      v[0] = ld4_nt(p + 4 * r);
+      v[0] = ld_row<4, STREAM>(p + 4 * r);
     } else if constexpr (KIND == Kind::kE4M3) {
-      const uint2 w = ld8_nt(p + 8 * r);
+      const uint2 w = ld_row<8, STREAM>(p + 8 * r);
       v[0] = w.x, v[1] = w.y;
     } else {
-      const uint4 w = ld16_nt(reinterpret_cast<const uint16_t*>(p) + 8 * r);
+      const uint4 w = ld_row<16, STREAM>(p + 16 * r);
       v[0] = w.x, v[1] = w.y, v[2] = w.z, v[3] = w.w;
     }
   }

@@ -129,9 +129,9 @@ def test_many_tokens_of_one_request():
     check(pool, 1, 64, 6, ragged_tokens([2600], 1100))
 
 
-@pytest.mark.parametrize("nb", [300, 1500])
+@pytest.mark.parametrize("nb", [300, 1500, 3001, 4200])
 def test_many_blocks(nb):
-    """Scores held in 16 registers a lane, and read again at each halving."""
+    """Scores held in 16, 32 and 64 registers a lane, and read again at each halving."""
     n = 32 * nb - 5
     pool = make("e2m1", [n, n - 1000], 1, 64, seed=nb)
     check(pool, 4, 32, 33, [(0, n - 1), (0, n // 2), (1, n - 1001), (1, 3), (0, 31), (0, 32)])
@@ -214,10 +214,11 @@ def test_lists_of_a_caller():
     assert torch.all((c.out.cpu().double() - out).abs().amax(-1) <= tol)
 
 
-@pytest.mark.parametrize("kind,new,Hkv,G", [("e4m3", 30, 2, 4), ("bf16", 800, 2, 16)])
+@pytest.mark.parametrize("kind,new,Hkv,G", [("e4m3", 30, 2, 4), ("bf16", 800, 2, 16),
+                                             ("bf16", 1030, 2, 16)])
 def test_a_block_named_twice_counts_once(kind, new, Hkv, G):
     """The same block twice in a list, blocks past the token's own after them."""
-    n, block = 900, 64
+    n, block = max(900, new + 70), 64
     pool = make(kind, [n], Hkv, 16, seed=new)
     pos = torch.arange(n - new, n, dtype=torch.int32)
     own = pos // block
@@ -293,8 +294,8 @@ def test_captured_and_replayed_and_on_another_stream(new, G):
 
 
 @pytest.mark.parametrize("Hkv,G,block,k,page,order,new", [
-    (2, 16, 64, 6, 16, "pairs", 300), (8, 4, 32, 17, 64, "heads", 280),
-    (16, 1, 128, 3, 16, "rows", 560), (4, 8, 256, 2, 32, "heads", 290)])
+    (2, 16, 64, 6, 16, "pairs", 400), (8, 4, 32, 17, 64, "heads", 350),
+    (16, 1, 128, 3, 16, "rows", 700), (4, 8, 256, 2, 32, "heads", 350)])
 def test_many_tokens_of_a_bf16_cache(Hkv, G, block, k, page, order, new):
     """Four tiles a workgroup: chunks of three requests, holes, padding and a
     request's tokens apart from each other; every seventh token is compared."""
@@ -327,12 +328,12 @@ def test_many_tokens_of_a_bf16_cache(Hkv, G, block, k, page, order, new):
 
 @pytest.mark.parametrize("kind,new,Hkv,G", [
     ("bf16", 40, 2, 4), ("e4m3", 40, 2, 2), ("e2m1", 40, 2, 8), ("bf16", 3, 2, 1),
-    ("e2m1", 3, 2, 4), ("bf16", 780, 2, 16), ("bf16", 820, 8, 4)])
+    ("e2m1", 3, 2, 4), ("bf16", 780, 2, 16), ("bf16", 1030, 2, 16), ("bf16", 1030, 8, 4)])
 def test_rows_that_are_no_numbers_reach_only_who_sees_them(kind, new, Hkv, G):
     """NaN and infinite rows of K and V, seen by some tokens of a tile and not by
     others (another block, a later position): the others' outputs are as without."""
     _log("no numbers", kind, new, Hkv, G)
-    n, block, k = 1000, 32, 4
+    n, block, k = max(1000, new + 200), 32, 4
     pool = make(kind, [n], Hkv, 16, seed=new)
     g = torch.Generator().manual_seed(5)
     pos = list(range(n - new, n))
@@ -362,6 +363,38 @@ def test_rows_that_are_no_numbers_reach_only_who_sees_them(kind, new, Hkv, G):
     assert rows.any()
     err = (got - out)[rows].abs().amax(-1)
     assert torch.all(err <= tol[rows])
+
+
+def test_many_tokens_captured_and_replayed():
+    """Staged blocks of four tiles in a graph: changing queries and positions, eager
+    calls on another stream between the replays."""
+    n, Hkv, G = 1030, 2, 16
+    pool = make("bf16", [1200], Hkv, 16, seed=4)
+    c, e = Call(pool, G, 64, 5, n), Call(pool, G, 64, 5, n)
+    p = torch.arange(1200 - n, 1200, dtype=torch.int32, device=DEV)
+    r = torch.zeros_like(p)
+    q = torch.randn((n, G * Hkv, D), device=DEV).to(torch.bfloat16)
+
+    def run(x, stream=None):
+        x.select(r, p, q, stream=stream)
+        x.attend(r, p, q, stream=stream)
+
+    for x in (c, e):
+        x.landmarks()
+        run(x)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(c)
+    side = torch.cuda.Stream()
+    for i in range(4):
+        q.copy_(torch.randn(q.shape, device=DEV))
+        p.sub_(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        run(e, side if i % 2 else None)
+        torch.cuda.synchronize()
+        assert torch.equal(c.idx, e.idx) and torch.equal(c.out, e.out) and torch.equal(c.lse, e.lse)
 
 
 def test_debug_mode_names_bad_tokens():
