@@ -598,8 +598,8 @@ int ckv_select_blocks(const ckv_shape* shape, const ckv_paged_cache* cache, int3
                       int32_t* idx, void* ws, size_t ws_bytes, void* stream);
 
 /* Attention of every query token over the positions p <= positions[t] of the blocks
- * idx [num_tokens][Hkv][k] (ascending, -1 and blocks past its own are passed over)
- * that are there:
+ * idx [num_tokens][Hkv][k] (ascending; -1 and blocks past its own may stand anywhere
+ * between them and are passed over) that are there:
  *   l_p = scale * q[t][g] . K_p,  out[t][g] = sum_p softmax(l)_p V_p,
  *   lse[t][g] = log sum_p exp(l_p)       (natural logarithm; may be NULL)
  * out [num_tokens][Hq][d] fp32, lse [num_tokens][Hq] fp32; nothing to attend to:

@@ -545,7 +545,7 @@ struct BlockLds {
   };
 };
 
-// Whether token i's ascending list holds block v.
+// Whether token i's list, ascending and then all ones, holds block v.
 __device__ __forceinline__ bool holds(const BlockLds& lds, int i, int k, uint32_t v) {
   int lo = 0, hi = k;
   while (lo < hi) {
@@ -568,14 +568,26 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
     lds.pos[tid] = x.pos;
   }
   __syncthreads();
-  for (int e = tid; e < n; e += kBlockThreads) {
-    const int i = e / t.k;
-    uint32_t v = ~0u;
-    if (lds.req[i] >= 0) {
-      const int j = a.idx[((t0 + i) * t.Hkv + h) * t.k + (e - i * t.k)];
-      if ((unsigned)j <= (unsigned)(lds.pos[i] >> t.lb)) v = (uint32_t)j;
-    }
-    lds.list[e] = v;
+  // A token's blocks together at the front of its list, where a search finds them and
+  // finds them ascending: a wave a token, all of its lists asked for at once.
+  static_assert(kMaxKept == 64, "a lane an entry");
+  uint32_t mine[4];
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int i = 4 * x + wave;
+    mine[x] = ~0u;
+    if (i < tokens && lds.req[i] >= 0 && lane < t.k)
+      mine[x] = (uint32_t)a.idx[((t0 + i) * t.Hkv + h) * t.k + lane];
+  }
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    const int i = 4 * x + wave;
+    if (i >= tokens) break;
+    const bool counts = (int)mine[x] >= 0 && (int)mine[x] <= lds.pos[i] >> t.lb;
+    const uint64_t all = __ballot(counts);
+    const int before = __popcll(all & ((1ull << lane) - 1)), count = __popcll(all);
+    if (lane < t.k)  // (what does not count, behind what does)
+      lds.list[i * t.k + (counts ? before : count + lane - before)] = counts ? mine[x] : ~0u;
   }
   if (tid < tokens) {  // positions that the request's tokens of this tile see
     int end = 0;
@@ -1193,8 +1205,10 @@ __device__ __forceinline__ bool many_tiles(const BlockAttnArgs& a, ManyLds& lds,
       const int j = a.idx[((t0 + i) * bt.Hkv + h) * bt.k + lane];
       if ((unsigned)j <= (unsigned)(pos >> bt.lb)) v = (uint32_t)j;
     }
-    const uint32_t before = __shfl_up(v, 1);
-    const bool keep = v != ~0u && (lane == 0 || before != v);
+    // once each: the entry before is the last one that counts
+    const uint64_t some = __ballot(v != ~0u) & ((1ull << lane) - 1);
+    const uint32_t before = __shfl(v, some ? 63 - __builtin_clzll(some) : lane);
+    const bool keep = v != ~0u && (some == 0 || before != v);
     const uint64_t all = __ballot(keep);
     if (keep) lists[i * bt.k + __popcll(all & ((1ull << lane) - 1))] = v;
     if (lane == 0) lds.counts[i] = __popcll(all);
