@@ -577,9 +577,9 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
  *
  * ckv_paged_landmarks: landmarks [B][Hkv][nb][d] bf16, of block j the mean of the
  * keys at its positions below n_b that are there, summed in fp64 and rounded once
- * (NaN or infinite sums: NaN).  Only the blocks from first[b] / block on (first NULL:
- * from 0 on) that have such a position are written, so that a step renews what its
- * new tokens touched. */
+ * (NaN or infinite sums: NaN; finite means past the largest bf16: infinities).  Only
+ * the blocks from first[b] / block on (first NULL: from 0 on) that have such a position
+ * are written, so that a step renews what its new tokens touched. */
 int ckv_paged_landmarks(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t block,
                         const int32_t* ctx_lens, const int32_t* first, uint16_t* landmarks,
                         void* stream);

@@ -329,9 +329,10 @@ __device__ __forceinline__ void unpack8(uint4 v, float* f) {
   }
 }
 
-// Nearest bf16 to x, ties to the even significand, from the binary64 fields:
+// Nearest bf16 to a finite x, ties to the even significand, from the binary64 fields:
 // normal results keep 7 of the 52 stored significand bits; below the
-// smallest normal bf16 (2^-126) the quantum is 2^-133.
+// smallest normal bf16 (2^-126) the quantum is 2^-133; from halfway between the
+// largest bf16 and 2^128 on, an infinity.
 __device__ __forceinline__ uint16_t f64_to_bf16_rne(double x) {
   uint64_t b = (uint64_t)__double_as_longlong(x);
   const uint16_t sign = (uint16_t)((b >> 48) & 0x8000u);
@@ -343,6 +344,7 @@ __device__ __forceinline__ uint16_t f64_to_bf16_rne(double x) {
   }
   b += 0x00000fffffffffffull + ((b >> 45) & 1u);  // 2^44 - 1 + kept lsb
   const uint32_t e = (uint32_t)(b >> 52) - 1023u + 127u;
+  if (e > 254u) return (uint16_t)(sign | 0x7f80u);
   return (uint16_t)(sign | (e << 7) | (uint32_t)((b >> 45) & 0x7fu));
 }
 
