@@ -554,7 +554,9 @@ int ckv_paged_score_keys(const ckv_shape* shape, const ckv_paged_cache* cache,
  * should other launches keep them off the device for so long, the unit's outputs
  * of that call are NaN (later calls and replays are not affected).  A row of V that
  * holds NaN or an infinity reaches every token of its request in the call, those before
- * it too.  Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
+ * it too.  An E4M3 row's weight carries the row's exponent, and what of it is below
+ * 2^-126 is lost: rows of V under 2^-100 keep fewer bits.
+ *   Workspace: CKV_ENTRY_PAGED_DECODE_ATTN with k = num_tokens. */
 int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
                           int32_t num_tokens, const uint16_t* q, const int32_t* ctx_lens,
                           float scale, float* out, float* lse, void* ws, size_t ws_bytes,
@@ -605,8 +607,9 @@ int ckv_select_blocks(const ckv_shape* shape, const ckv_paged_cache* cache, int3
  * out [num_tokens][Hq][d] fp32, lse [num_tokens][Hq] fp32; nothing to attend to:
  * out = 0, lse = -inf.  Logits, weights and sums are fp32; 0 < scale <= 2^126.  The
  * same call gives the same bits.  A block named twice counts once.  Rows of K or V that
- * hold NaN or infinities reach only the tokens that see them.  Rows at positions up to
- * the tokens' own are written before.  ws: ckv_blocks_workspace_bytes. */
+ * hold NaN or infinities reach only the tokens that see them; E4M3 rows of V under
+ * 2^-100 keep fewer bits, as in ckv_paged_decode_attn.  Rows at positions up to the
+ * tokens' own are written before.  ws: ckv_blocks_workspace_bytes. */
 int ckv_paged_block_attn(const ckv_shape* shape, const ckv_paged_cache* cache, int32_t block,
                          int32_t k, int32_t num_tokens, const int32_t* requests,
                          const int32_t* positions, const uint16_t* q, const int32_t* idx,

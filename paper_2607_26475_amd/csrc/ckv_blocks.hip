@@ -524,7 +524,7 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
 //   Codes have to be made bf16 and V's rows transposed by byte permutes at every step:
 // the vector unit bounds it, 370 instructions a step of 32 four-bit positions (2103
 // tokens, 8 blocks of 128, groups of 8: 135 us; without masks where a step needs none,
-// the maximum raised lazily, three workgroups a CU: 107; blocks in ascending order and
+// the maximum raised ahead, three workgroups a CU: 107; blocks in ascending order and
 // rows kept in the caches: 104).  16 tokens of as many
 // requests, 32 blocks of 64 each: 17 us, and 4 of joining.
 constexpr int kBlockThreads = 256;
@@ -682,22 +682,30 @@ __device__ __forceinline__ void store_block_row(const BlockAttnArgs& a, int64_t 
   if (a.lse && d == 0) a.lse[at] = log_sum(p.M, p.L);
 }
 
-// raise_max for a maximum that may lie up to 2^8 below what it stands for: weights
-// are then at most 2^8 and sums as exact as before, and scaling is needed at the
-// first steps only.
-__device__ __forceinline__ void raise_max_lazily(float top, float c, WaveState& st) {
+// raise_max to HEAD above the largest logit, so that it stays until one passes that:
+// sums are scaled at the first steps only, and no weight is above 1 (sums of V next to
+// its type's largest would else pass fp32's range).
+template <int HEAD>
+__device__ __forceinline__ void raise_max_above(float top, float c, WaveState& st) {
   const float m = query_row_max(top) * c;
-  const bool more = m > st.m + 8.f;
+  const bool more = m > st.m;
   if (__any(more)) {
-    const float f = !more ? 1.f : st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - m);
+    const float to = m + HEAD;
+    const float f = !more ? 1.f : st.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st.m - to);
     st.l *= f;
 #pragma unroll
     for (int e = 0; e < 8; ++e)
 #pragma unroll
       for (int j = 0; j < 4; ++j) st.o[e][j] *= f;
-    if (more) st.m = m;
+    if (more) st.m = to;
   }
 }
+
+// Powers of two that the maximum is raised above the logits: an e4m3 row's weight takes
+// the row's exponent with it, down to 2^-128, where products lose what is below 2^-126
+// (8 as for the others: 2048 tokens 300 -> 291 us).
+template <Kind KIND>
+constexpr int kHead = KIND == Kind::kE4M3 ? 1 : 8;
 
 // The weights of a step and its products with V.  APART: these a token at a time,
 // without the rows that it does not see, for V rows whose product with a weight of
@@ -715,7 +723,7 @@ __device__ __forceinline__ void block_rest(const BlockAttnArgs& a, Tile<KIND>& t
   const bool kept = limit > p0;
   if (APART || t.there != 255u || __any(kept && limit < p0 + kPagedTile))
     tile_mask<KIND>(t, p0, limit, n, lg);
-  raise_max_lazily(kept ? top_of(lg) : -INFINITY, c, st);
+  raise_max_above<kHead<KIND>>(kept ? top_of(lg) : -INFINITY, c, st);
   uint32_t part[3][8];
   tile_weights<KIND>(t.ve, c, kept ? less_max(st) : -INFINITY, lg, part, st);
   if (!APART) {
@@ -1100,7 +1108,7 @@ __device__ __forceinline__ void many_step(const BlockAttnArgs& a, const ManyLds&
     }
   };
   read_rows(0);  // on their way while the weights are made
-  raise_max_lazily(kept ? top_of(lg) : -INFINITY, c, st);
+  raise_max_above<kHead<Kind::kBf16>>(kept ? top_of(lg) : -INFINITY, c, st);
   uint32_t part[3][8];
   tile_weights<Kind::kBf16>(nullptr, c, kept ? less_max(st) : -INFINITY, lg, part, st);
   bf16x8 w[3];

@@ -6,9 +6,9 @@ import math
 import pytest
 import torch
 
-from blocks_helpers import landmarks64, select64
-from paged_helpers import D
-from test_gpu_blocks import DEV, Call, _i32, make
+from blocks_helpers import attend64, landmarks64, select64
+from paged_helpers import D, SCALE
+from test_gpu_blocks import DEV, Call, _i32, _log, make
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,53 @@ def test_landmarks_past_the_largest_bf16():
     q = torch.randn((1, 8, D), generator=torch.Generator().manual_seed(2)).to(torch.bfloat16)
     c.select(_i32([0]), _i32([16 * block - 1]), q.to(DEV))
     assert torch.equal(c.idx.cpu(), select64(pool, block, 5, [0], [16 * block - 1], q, want))
+
+
+def _rising(pool, block, G, Hkv):
+    """Keys along one direction whose logits rise by about 5 (a factor of 2^7.1 of the
+    weights) in four blocks, and queries along it."""
+    u = torch.ones(D, dtype=torch.float64)
+    q = (u / 4).expand(1, G * Hkv, D).to(torch.bfloat16)      # q . u * SCALE = 2.83
+    for p in range(pool.lens[0]):
+        x = u * (0.4375 * (p // block) + 0.0625 * (p % 4))
+        if pool.kind == "e4m3":
+            _put(pool, "k", p, x.float().to(torch.float8_e4m3fn).double(), 127)
+        else:
+            x = x.to(torch.bfloat16)
+            pool.k[int(pool.table[0, p // pool.page]), :, p % pool.page] = x.to(DEV)
+            pool.K[0, :, p] = x.double()
+    return q
+
+
+@pytest.mark.parametrize("kind,new,Hkv,G", [("e4m3", 1, 1, 16), ("e4m3", 40, 2, 16),
+                                            ("bf16", 40, 2, 16), ("bf16", 1030, 2, 16)])
+def test_large_values_under_rising_logits(kind, new, Hkv, G):
+    """Values far up in their types' ranges, each block's logits a little above the
+    one before's: every output is a mean of finite values, and finite."""
+    _log("rising", kind, new, Hkv, G)
+    block, k = 32, 16
+    n = block * k + max(64, new)
+    pool = make(kind, [n], Hkv, 16, seed=3)
+    q = _rising(pool, block, G, Hkv).expand(new, -1, -1).contiguous()
+    g = torch.Generator().manual_seed(4)
+    for p in range(n):
+        v = (torch.randint(1, 8, (D,), generator=g) - 4).double()
+        v[3] = 2.0
+        if kind == "e4m3":  # 2^120 and less, as subnormal codes under the largest exponents
+            _put(pool, "v", p, v * 2.0 ** -9, 254 - p % 7)
+        else:
+            v = (v * 2.0 ** 117).to(torch.bfloat16)
+            pool.v[int(pool.table[0, p // pool.page]), :, p % pool.page] = v.to(DEV)
+            pool.V[0, :, p] = v.double()
+    pos = list(range(n - new, n))
+    idx = torch.arange(k, dtype=torch.int32).expand(new, Hkv, k).contiguous()
+    c = Call(pool, G, block, k, new)
+    c.idx.copy_(idx)
+    c.attend(_i32([0] * new), _i32(pos), q.to(DEV))
+    some = sorted({0, new // 2, new - 1})
+    out, lse, tol = attend64(pool, block, [0] * len(some), [pos[i] for i in some], q[some],
+                             idx[some])
+    got = c.out.cpu().double()[some]
+    assert torch.isfinite(got).all()
+    err = (got - out).abs().amax(-1)
+    assert torch.all(err <= tol), float((err / tol).max())
