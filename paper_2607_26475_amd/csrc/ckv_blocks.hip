@@ -533,7 +533,7 @@ static_assert(1 << kStepLg == kPagedTile, "a step");
 
 struct BlockLds {
   float m[4][16], l[4][16];
-  int32_t pos[16], req[16], end[16];
+  int32_t pos[16], req[16];
   int32_t count[4];
   union {
     float o[4][16][kPartStride];
@@ -541,6 +541,7 @@ struct BlockLds {
       uint32_t list[16 * kMaxKept];  // the tokens' blocks (all ones: none)
       int32_t block[16 * kMaxKept];  // of the tile, each once
       uint32_t who[16 * kMaxKept];   // its tokens' bits, and the first of them << 16
+    int32_t end[16 * kMaxKept];    // the positions that these see
     };
   };
 };
@@ -589,17 +590,12 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
     if (lane < t.k)  // (what does not count, behind what does)
       lds.list[i * t.k + (counts ? before : count + lane - before)] = counts ? mine[x] : ~0u;
   }
-  if (tid < tokens) {  // positions that the request's tokens of this tile see
-    int end = 0;
-    for (int i = 0; i < tokens; ++i)
-      if (lds.req[i] == lds.req[tid]) end = max(end, lds.pos[i] + 1);
-    lds.end[tid] = end;
-  }
   __syncthreads();
   int total = 0;
   for (int e0 = 0; e0 < n; e0 += kBlockThreads) {
     const int e = e0 + tid, i = e / t.k;
     uint32_t who = 0, v = ~0u;
+    int end = 0;
     if (e < n && (v = lds.list[e]) != ~0u && (e == i * t.k || lds.list[e - 1] != v)) {
       for (int o = 0; o < tokens; ++o) {
         if (lds.req[o] != lds.req[i] || !(o == i || holds(lds, o, t.k, v))) continue;
@@ -608,6 +604,7 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
           break;
         }
         who |= 1u << o;
+        end = max(end, lds.pos[o] + 1);
       }
     }
     const uint64_t some = __ballot(who != 0);
@@ -621,6 +618,7 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
     if (who) {
       lds.block[at] = (int)v;
       lds.who[at] = who | (uint32_t)i << 16;
+      lds.end[at] = end;
     }
     __syncthreads();
   }
@@ -629,10 +627,11 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
   // 360 -> 298; with rows streamed past the caches the order changes nothing).
   if (a.pieces > 1 || total > kBlockThreads) return total;
   uint32_t block = 0, who = 0;
-  int rank = 0;
+  int rank = 0, end = 0;
   if (tid < total) {
     block = (uint32_t)lds.block[tid];
     who = lds.who[tid];
+    end = lds.end[tid];
     for (int e = 0; e < total; ++e) {
       const uint32_t other = (uint32_t)lds.block[e];
       rank += other < block || (other == block && e < tid);
@@ -642,6 +641,7 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
   if (tid < total) {
     lds.block[rank] = (int)block;
     lds.who[rank] = who;
+    lds.end[rank] = end;
   }
   __syncthreads();
   return total;
@@ -655,18 +655,26 @@ struct BlockStep {
   TileAt<true> at;
 };
 
+// Step s (below s1) or, where none of its block's tokens sees that, the wave's next one
+// that is seen: rows behind what they see may not have been written, and bytes of theirs
+// that make a NaN would have the sums made again (64 tokens 5 positions into blocks of
+// 256, 75 us and 163).  From s1 on the place of the last step, which nobody takes.
 __device__ __forceinline__ BlockStep block_step(const BlockAttnArgs& a, const BlockLds& lds, int h,
-                                                int s) {
-  const int lg = a.t.lb - kStepLg, e = s >> lg;
+                                                int& s, int s1) {
+  const int lg = a.t.lb - kStepLg;
   BlockStep b;
-  b.who = __builtin_amdgcn_readfirstlane(lds.who[e]);
-  const int first = b.who >> 16;
-  b.x.b = __builtin_amdgcn_readfirstlane(lds.req[first]);
-  b.x.n = __builtin_amdgcn_readfirstlane(lds.end[first]);
+  for (int e;; s += 4) {
+    const int at = min(s, s1 - 1);
+    e = at >> lg;
+    b.who = __builtin_amdgcn_readfirstlane(lds.who[e]);
+    b.x.n = __builtin_amdgcn_readfirstlane(lds.end[e]);
+    b.p0 = (__builtin_amdgcn_readfirstlane(lds.block[e]) << a.t.lb) +
+           ((at - (e << lg)) << kStepLg);
+    if (s >= s1 || b.p0 < b.x.n) break;
+  }
+  b.x.b = __builtin_amdgcn_readfirstlane(lds.req[b.who >> 16]);
   b.x.h = h;
   b.x.table = table_of(a.pg, b.x.b);
-  b.p0 = (__builtin_amdgcn_readfirstlane(lds.block[e]) << a.t.lb) +
-         ((s - (e << lg)) << kStepLg);
   b.at = tile_at<true>(a.pg, b.x, b.p0);
   return b;
 }
@@ -781,14 +789,15 @@ __device__ __forceinline__ bool block_sums(const BlockAttnArgs& a, BlockLds& lds
   // (as constants the sums would be held twice, and copied at each step)
 #pragma unroll
   for (int e = 0; e < 8; ++e) asm("" : "+v"(st.o[e]));
+  BlockStep now;
+  if (s < s1) now = block_step(a, lds, h, s, s1);
   if (s < s1) {
     Tile<KIND> t;
     float lg[8];
-    BlockStep now = block_step(a, lds, h, s);
     load_k<KIND, true, false>(a.pg, now.x, now.at, t);
     load_v<KIND, true, false>(a.pg, now.x, now.at, t);
     s += 4;
-    BlockStep next = block_step(a, lds, h, min(s, s1 - 1));
+    BlockStep next = block_step(a, lds, h, s, s1);
     auto limit = [&] { return now.who >> row_tok & 1u ? my_end : 0; };
     for (;;) {  // (the last step asks for K rows that nobody takes)
       tile_logits<KIND, true>(t, q, lg);
@@ -800,7 +809,7 @@ __device__ __forceinline__ bool block_sums(const BlockAttnArgs& a, BlockLds& lds
       load_v<KIND, true, false>(a.pg, next.x, next.at, t);
       now = next;
       s += 4;
-      next = block_step(a, lds, h, min(s, s1 - 1));
+      next = block_step(a, lds, h, s, s1);
     }
   }
   bool bad = false;
