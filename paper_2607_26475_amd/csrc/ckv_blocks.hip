@@ -272,9 +272,10 @@ __global__ __launch_bounds__(kSelThreads, 4) void k_block_scores(BlockSelectArgs
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
         const int tok = m * kTok + 4 * g / G + i;
+        // (what is no finite number, +inf here, is summed again by the selection)
         if ((4 * g) % G == 0 && req[tok] == s.req && s.j < own[tok] && s.j < s.stop)
           a.scores[((t0 + tok) * t.Hkv + h) * t.nb + s.j] =
-              s.there ? fmaxf(best[i], -INFINITY) : -INFINITY;  // of NaN: -inf
+              !s.there ? -INFINITY : fabsf(best[i]) < INFINITY ? best[i] : INFINITY;
       }
     }
     if (kAhead) s = next;
@@ -298,7 +299,9 @@ __global__ __launch_bounds__(kSelThreads, 4) void k_block_scores(BlockSelectArgs
 // above (8 halvings or so; ties end it at neighbouring floats).  The scores of up
 // to 64 V blocks are held in registers, of more read again at each halving.  A chain of
 // about 2000 instructions of one wave: 13 us for 128 (token, KV head) pairs of up to
-// 1024 blocks, 25 for 16384 of 256; 64 pairs of 1900 blocks read again 71, held 21.
+// 1024 blocks, 26 for 16384 of 256; 64 pairs of 1900 blocks read again 71, held 22
+// (the second look at sums that are no finite numbers costs these 1 us).  Of 64 V
+// blocks few groups fit in 256 registers, two workgroups a CU.
 // Query rows of a group for scores in fp64: 64 / G lanes a head, each 2 G channels.
 template <int G>
 struct GroupRows {
@@ -357,12 +360,33 @@ struct GroupRows {
   }
 };
 
+// A score whose fp32 sum is no finite number, summed in fp64: past fp32's range its
+// largest, so that what is not there or no number stays below.  (|q|^2 or |landmark|^2
+// passes that range too, so the error bound is infinite, and such scores are ranked in
+// fp64.)
+template <int G>
+__device__ __forceinline__ float wide_score(const uint16_t* q, const uint16_t* mark) {
+  double best = -INFINITY;
+#pragma unroll 1
+  for (int k = 0; k < G; ++k) {
+    double s = 0.0;
+#pragma unroll 1
+    for (int i = 0; i < kD; ++i)
+      s += (double)__uint_as_float((uint32_t)q[k * kD + i] << 16) *
+           (double)__uint_as_float((uint32_t)mark[i] << 16);
+    best = fmax(best, s);  // of NaN: -inf
+  }
+  const double most = 3.4028234663852886e38;
+  return (float)(best - best == 0.0 ? fmin(fmax(best, -most), most) : best);
+}
+
 __device__ __forceinline__ float float_of_key(uint32_t k) {
   return __uint_as_float(key_floor_bits(k));
 }
 
 template <int G, int V>
-__global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a) {
+__global__ __launch_bounds__(kSelThreads, V == 64 && G <= 4 ? 2 : 1) void k_select_blocks(
+    BlockSelectArgs a) {
   const BlockTokens& t = a.t;
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * (kSelThreads / 64) +
@@ -383,12 +407,9 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
   const float* norms = a.norms + ((int64_t)(tok / per) * t.Hkv + h) * a.chunks;
   float mm = 0.f;
   for (int i = lane; i < (n + a.cols - 1) / a.cols; i += 64) mm = fmaxf(mm, norms[i]);
-  const float* scores = a.scores + unit * t.nb;
+  float* scores = a.scores + unit * t.nb;
   const int steps = V ? V : (n + 63) / 64;
   float held[V ? V : 1];
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    held[i] = 64 * i + lane < n ? scores[64 * i + lane] : -INFINITY;
   auto score = [&](int i) {
     if constexpr (V > 0) return held[i];
     else return 64 * i + lane < n ? scores[64 * i + lane] : -INFINITY;
@@ -406,14 +427,25 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
     each([&](int, float s) { m += __popcll(__ballot(s >= x)); });
     return m;
   };
-  float lo_s = INFINITY, hi_s = -INFINITY;
-  int avail = 0;
-  each([&](int, float s) {
-    const bool is = s > -INFINITY;
-    avail += __popcll(__ballot(is));
-    lo_s = fminf(lo_s, is ? s : INFINITY);
-    hi_s = fmaxf(hi_s, s);
-  });
+  float lo_s, hi_s;
+  int avail;
+  const uint16_t* marks = a.marks + ((int64_t)x.req * t.Hkv + h) * t.nb * kD;
+  for (bool again = false;; again = true) {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      held[i] = 64 * i + lane < n ? scores[64 * i + lane] : -INFINITY;
+    lo_s = INFINITY, hi_s = -INFINITY, avail = 0;
+    each([&](int, float s) {
+      const bool is = s > -INFINITY;
+      avail += __popcll(__ballot(is));
+      lo_s = fminf(lo_s, is ? s : INFINITY);
+      hi_s = fmaxf(hi_s, s);
+    });
+    if (again || !__any(hi_s == INFINITY)) break;
+    for (int j = lane; j < n; j += 64)
+      if (scores[j] == INFINITY)
+        scores[j] = wide_score<G>(t.q + ((int64_t)tok * t.Hq + h * G) * kD, marks + (int64_t)j * kD);
+  }
   // those above `sure` are in; of those from `maybe` on the ones in `mine` (lanes
   // below `few`)
   float sure = -INFINITY, maybe = INFINITY;
@@ -461,7 +493,6 @@ __global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a
         maybe = in - e2;
         int need = want;
         each([&](int, float s) { need -= __popcll(__ballot(s > sure)); });
-        const uint16_t* marks = a.marks + ((int64_t)x.req * t.Hkv + h) * t.nb * kD;
         auto between = [&](float s) { return s > -INFINITY && !(s > sure) && !(s < maybe); };
         int total = 0;
         each([&](int, float s) { total += __popcll(__ballot(between(s))); });

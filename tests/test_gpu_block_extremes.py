@@ -106,6 +106,48 @@ def test_large_values_under_rising_logits(kind, new, Hkv, G):
     assert torch.all(err <= tol), float((err / tol).max())
 
 
+def _best(marks, q, want):
+    """The best of the blocks by exactly rounded sums (in fp64 one after the other, terms
+    that cancel may take the others with them), ascending."""
+    terms = (marks.double()[:, None] * q.double()).tolist()
+    s = [max(math.fsum(h) if all(map(math.isfinite, h)) else
+             (lambda x: x if x == x else -math.inf)(sum(h)) for h in b) for b in terms]
+    order = sorted((j for j in range(len(s)) if s[j] > -math.inf), key=lambda j: (-s[j], j))
+    return sorted(order[:want])
+
+
+def test_scores_past_fp32():
+    """Sums of finite products that pass fp32's range, either way or on the way:
+    they rank as what they are."""
+    block, nb, k = 32, 40, 9
+    n = block * nb
+    pool = make("bf16", [n], 1, 16, seed=1)
+    g = torch.Generator().manual_seed(8)
+    far = torch.randn((nb, D), generator=g).double()
+    q = torch.randn((1, 2, D), generator=g).double()
+    cases = [(2.0 ** 70 * far, 2.0 ** 70 * q), (-2.0 ** 70 * far.abs(), 2.0 ** 70 * q.abs())]
+    cancel, qc = far.clone(), q.clone()      # infinite terms that cancel
+    qc[..., :2], cancel[:, 0], cancel[:, 1] = 2.0 ** 80, 2.0 ** 60, -2.0 ** 60
+    cases.append((cancel, qc))
+    one = far.clone()                        # one head of the two passes it downwards
+    one[:, 0] = -2.0 ** 100
+    q1 = q.clone()
+    q1[0, 0, 0], q1[0, 1, 0] = 2.0 ** 100, 0.0
+    cases.append((one, q1))
+    gone = 2.0 ** 70 * far                   # and landmarks that are no numbers among them
+    gone[3, 5], gone[7, 2] = math.nan, -math.inf
+    cases.append((gone, 2.0 ** 70 * q.abs()))
+    for kept in (k, 64):
+        c = Call(pool, 2, block, kept, 1)
+        for i, (m, x) in enumerate(cases):
+            _log("case", kept, i)
+            marks, x = m[None, None].to(torch.bfloat16), x.to(torch.bfloat16)
+            c.marks.copy_(marks)
+            c.select(_i32([0]), _i32([n - 1]), x.to(DEV))
+            best = _best(marks[0, 0, :nb - 1], x[0], kept - 1) + [nb - 1]
+            assert c.idx.flatten().tolist() == best + [-1] * (kept - len(best)), i
+
+
 @pytest.mark.parametrize("page", [16, 256])
 def test_bytes_of_unwritten_rows_cost_nothing(page):
     """Decode tokens early in their own blocks of 256 four-bit positions: exponent
