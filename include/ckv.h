@@ -570,7 +570,9 @@ int ckv_paged_decode_attn(const ckv_shape* shape, const ckv_paged_cache* cache,
  * block and the k - 1 earlier blocks whose landmarks score best (Sec. 2.2 chunk
  * landmarks, one set per GQA group, selected per query token).  1 <= k <= 64;
  * pages of at least 16 positions (CKV_EUNSUPPORTED otherwise).
- *   Query token t (0 <= t < num_tokens <= 2^24) is position positions[t] of request
+ *   num_tokens <= 2^24, and num_tokens * Hkv < 2^24 (CKV_EUNSUPPORTED otherwise; so is
+ * a selection of 2^24 and more pieces of 64 query rows by 1024 blocks of max_ctx).
+ * Query token t (0 <= t < num_tokens) is position positions[t] of request
  * requests[t] (NULL: request t), its query row q[t] of [num_tokens][Hq][d] bf16; a
  * token whose position is outside [0, max_ctx) (-1: padding) or whose request is
  * outside [0, B) keeps nothing and gets out = 0 and lse = -inf.  Tokens may come in
