@@ -796,7 +796,8 @@ typedef enum ckv_kernel_id {
   CKV_K_BLOCK_SELECT = 24, /* each token's blocks                           */
   CKV_K_BLOCK_ATTN = 25,  /* attention over selected blocks                 */
   CKV_K_BLOCK_MERGE = 26, /* join of a tile's pieces                        */
-  CKV_K_TOTAL = 27        /* all classes (ckv_profile_end_n)                */
+  CKV_K_BLOCK_MANY = 27,  /* attention over selected blocks, many tokens    */
+  CKV_K_TOTAL = 28        /* all classes (ckv_profile_end_n)                */
 } ckv_kernel_id;
 
 #define CKV_K_ALL ((1u << CKV_K_COUNT) - 1u)     /* those of ckv_profile_end */

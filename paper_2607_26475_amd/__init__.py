@@ -62,7 +62,7 @@ EXPORTS = ("ckv_abi_version", "ckv_status_str", "ckv_last_error_detail",
            "ckv_paged_write", "ckv_paged_read", "ckv_paged_score_keys",
            "ckv_paged_decode_attn", "ckv_paged_landmarks", "ckv_select_blocks",
            "ckv_paged_block_attn", "ckv_blocks_workspace_bytes")
-KERNEL_COUNT = 27
+KERNEL_COUNT = 28
 MAX_RANK = 4096
 ABI_VERSION = 9  # CKV_ABI_VERSION of include/ckv.h that this binding marshals for
 
@@ -721,7 +721,8 @@ KERNEL_IDS = {"zero": 0, "score": 1, "hist": 2, "filter": 3, "finish": 4, "attn"
               "expand": 11, "reconstruct": 12, "select_attn": 13, "probe": 14,
               "critical": 15, "rope": 16, "paged_write": 17, "paged_read": 18,
               "paged_score": 19, "paged_attn": 20, "paged_merge": 21, "block_marks": 22,
-              "block_score": 23, "block_select": 24, "block_attn": 25, "block_merge": 26}
+              "block_score": 23, "block_select": 24, "block_attn": 25, "block_merge": 26,
+              "block_many": 27}
 
 
 def profile_begin(kernels=None, every: int = 1) -> None:

@@ -1360,7 +1360,7 @@ hipError_t launch_select_blocks(const BlockSelectArgs& a, hipStream_t s) {
 hipError_t launch_block_attn(const BlockAttnArgs& a, Kind kind, hipStream_t s) {
   if (a.many) {
     const size_t lists = sizeof(uint32_t) * (a.t.k * (kManyTiles * 16 >> a.t.lg) + 1);
-    launch_kernel_lds(CKV_K_BLOCK_ATTN, k_block_attn_many,
+    launch_kernel_lds(CKV_K_BLOCK_MANY, k_block_attn_many,
                       dim3((unsigned)(tiles_of(a.t, kManyTiles) * a.t.Hkv)), dim3(kManyThreads),
                       lists, s, a);
     return launch_status();

@@ -100,7 +100,7 @@ const char* ckv_kernel_name(int id) {
                                            "paged_write", "paged_read", "paged_score",
                                            "paged_attn", "paged_merge", "block_marks",
                                            "block_score", "block_select", "block_attn",
-                                           "block_merge"};
+                                           "block_merge", "block_many"};
   return (id >= 0 && id < CKV_K_TOTAL) ? names[id] : "";
 }
 
