@@ -846,7 +846,9 @@ int ckv_profile_end_n(ckv_kernel_stats* stats, int count);
  *   length (below max_ctx where the entry takes no ctx_lens);
  *   page_table entries of positions below n_b are -1 or in [0, num_pages);
  *   written tokens: positions[t] is -1 or in [0, max_ctx), and then
- *   requests[t] is in [0, B) and the page's entry in [0, num_pages).
+ *   requests[t] is in [0, B) and the page's entry in [0, num_pages);
+ *   query tokens the same, but for the page; of a list of blocks those from 0 to the
+ *   token's own ascend.
  * Outside debug mode these are the caller's preconditions, and kernels only
  * clamp what they read.  Every kernel launch then also synchronises its
  * stream, so that a failing kernel is reported by the entry that launched it

@@ -49,6 +49,23 @@ int check_query(const Dims& d, int32_t block, int32_t k, int32_t tokens, BlockTo
   return check_grid((int64_t)tokens * d.Hkv);
 }
 
+// Debug mode: the order of the lists (after the tokens' own check).
+int debug_check_lists(hipStream_t s, const BlockTokens& t, const int32_t* idx) {
+  if (!debug_on()) return CKV_OK;
+  BlockListArgs a = {t, idx, nullptr};
+  unsigned long long got = 0;
+  CKV_RC(debug_run(
+      s,
+      [&](unsigned long long* flag) {
+        a.flag = flag;
+        return launch_check_lists(a, s);
+      },
+      &got));
+  if (got == ~0ull) return CKV_OK;
+  return fail(CKV_EINVAL, "debug check: the blocks of idx[%lld][%lld] do not ascend",
+              (long long)got / t.Hkv, (long long)got % t.Hkv);
+}
+
 int check_ws(const void* ws, size_t bytes, size_t need) {
   if (!ws) return fail(CKV_EWORKSPACE, "workspace is NULL (%zu bytes needed)", need);
   if (reinterpret_cast<uintptr_t>(ws) & 255u)
@@ -240,6 +257,7 @@ int ckv_paged_block_attn(const ckv_shape* shape, const ckv_paged_cache* cache, i
   hipStream_t s = (hipStream_t)stream;
   CKV_RC(debug_check_paged(s, a.pg, nullptr, requests, positions, d.B, d.max_ctx, num_tokens,
                            true));
+  CKV_RC(debug_check_lists(s, a.t, idx));
   CKV_TRY_HIP(launch_block_attn(a, (Kind)cache->kind, s), "block attention launch");
   return CKV_OK;
 }

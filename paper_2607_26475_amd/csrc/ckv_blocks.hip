@@ -1313,6 +1313,13 @@ __global__ __launch_bounds__(kManyThreads, 4) void k_block_attn_many(BlockAttnAr
                      lds_address(lists), blockIdx.x);
 }
 
+// ---- debug mode ------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void k_check_lists(BlockListArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i < (int64_t)a.t.n * a.t.Hkv && !block_list_ascends(a, i))
+    atomicMin(a.flag, (unsigned long long)i);
+}
+
 // ---- launchers ---------------------------------------------------------------------------
 hipError_t launch_marks(const MarkArgs& a, Kind kind, hipStream_t s) {
   of_kind(kind, [&](auto k) {
@@ -1320,6 +1327,12 @@ hipError_t launch_marks(const MarkArgs& a, Kind kind, hipStream_t s) {
                   dim3(kMarkThreads), s, a);
   });
   return launch_status();
+}
+
+hipError_t launch_check_lists(const BlockListArgs& a, hipStream_t s) {
+  const int64_t n = (int64_t)a.t.n * a.t.Hkv;
+  hipLaunchKernelGGL(k_check_lists, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, s, a);
+  return hipGetLastError();
 }
 
 template <class Fn>

@@ -52,6 +52,27 @@ struct BlockAttnArgs {
   int32_t many;            // 64 query rows a workgroup, blocks staged for its waves
 };
 
+// Debug mode's check of the lists that an attention is given.
+struct BlockListArgs {
+  BlockTokens t;
+  const int32_t* idx;      // [N][Hkv][k]
+  unsigned long long* flag;
+};
+
+// Whether the blocks that count of list i (token i / Hkv, head i % Hkv) ascend.
+__host__ __device__ inline bool block_list_ascends(const BlockListArgs& a, int64_t i) {
+  const int64_t tok = i / a.t.Hkv;
+  const int own = a.t.pos[tok] >> a.t.lb;  // -1 (padding): none counts
+  int last = -1;
+  for (int e = 0; e < a.t.k; ++e) {
+    const int j = a.idx[i * a.t.k + e];
+    if (j < 0 || j > own) continue;
+    if (j < last) return false;
+    last = j;
+  }
+  return true;
+}
+
 inline int64_t tiles_of(const BlockTokens& t, int row_tiles = 1) {
   const int per = (16 >> t.lg) * row_tiles;
   return (t.n + per - 1) / per;
@@ -62,5 +83,6 @@ constexpr int kManyTiles = 4;  // tiles of a workgroup that stages blocks
 hipError_t launch_marks(const MarkArgs& a, Kind kind, hipStream_t s);
 hipError_t launch_select_blocks(const BlockSelectArgs& a, hipStream_t s);
 hipError_t launch_block_attn(const BlockAttnArgs& a, Kind kind, hipStream_t s);
+hipError_t launch_check_lists(const BlockListArgs& a, hipStream_t s);
 
 }  // namespace ckv

@@ -7,6 +7,7 @@ import math
 import pytest
 import torch
 
+import paper_2607_26475_amd as ckv
 from blocks_helpers import attend64
 from paged_helpers import D
 from test_gpu_blocks import Call, _i32, _log, make
@@ -85,3 +86,25 @@ def test_two_tokens_of_a_tile(lists):
     out, lse, tol = attend64(pool, 32, [0, 0], pos, q, idx)
     assert torch.all((c.out.cpu().double() - out).abs().amax(-1) <= tol)
     assert torch.all((c.lse.cpu().double() - lse).abs() <= tol + 1e-6 + 2.0 ** -22 * lse.abs())
+
+
+def test_debug_mode_names_a_list_that_does_not_ascend():
+    pool = make("bf16", [300], 2, 16, seed=1)
+    q = torch.zeros((3, 2, D), dtype=torch.bfloat16, device=DEV)
+    c = Call(pool, 1, 32, 4, 3)
+    req, pos = _i32([0, 0, 0]), _i32([299, 200, -1])
+    good = [[[0, 3, 3, 9], [-1, 4, -1, 5]], [[3, 8, 2, -1], [-1, -1, -1, -1]],
+            [[5, 4, 3, 2], [9, 8, 7, 6]]]   # 8 is past the second's own; the third is padding
+    c.idx.copy_(_i32(good))
+    ckv.set_debug(True)
+    try:
+        with pytest.raises(ckv.CkvError, match=r"idx\[1\]\[0\] do not ascend"):
+            c.attend(req, pos, q)
+        c.idx[1, 0, 0] = 1
+        c.attend(req, pos, q)
+        c.idx[1, 1, 0], c.idx[1, 1, 3] = 6, 5
+        c.idx[2, 1, 0] = 1
+        with pytest.raises(ckv.CkvError, match=r"idx\[1\]\[1\] do not ascend"):
+            c.attend(req, pos, q)
+    finally:
+        ckv.set_debug(False)
