@@ -299,9 +299,7 @@ __global__ __launch_bounds__(kSelThreads, 4) void k_block_scores(BlockSelectArgs
 // above (8 halvings or so; ties end it at neighbouring floats).  The scores of up
 // to 64 V blocks are held in registers, of more read again at each halving.  A chain of
 // about 2000 instructions of one wave: 13 us for 128 (token, KV head) pairs of up to
-// 1024 blocks, 26 for 16384 of 256; 64 pairs of 1900 blocks read again 71, held 22
-// (the second look at sums that are no finite numbers costs these 1 us).  Of 64 V
-// blocks few groups fit in 256 registers, two workgroups a CU.
+// 1024 blocks, 26 for 16384 of 256; 64 pairs of 1900 blocks read again 71, held 21.
 // Query rows of a group for scores in fp64: 64 / G lanes a head, each 2 G channels.
 template <int G>
 struct GroupRows {
@@ -385,8 +383,7 @@ __device__ __forceinline__ float float_of_key(uint32_t k) {
 }
 
 template <int G, int V>
-__global__ __launch_bounds__(kSelThreads, V == 64 && G <= 4 ? 2 : 1) void k_select_blocks(
-    BlockSelectArgs a) {
+__global__ __launch_bounds__(kSelThreads) void k_select_blocks(BlockSelectArgs a) {
   const BlockTokens& t = a.t;
   const int lane = threadIdx.x & 63;
   const int64_t unit = (int64_t)blockIdx.x * (kSelThreads / 64) +
@@ -431,9 +428,12 @@ __global__ __launch_bounds__(kSelThreads, V == 64 && G <= 4 ? 2 : 1) void k_sele
   int avail;
   const uint16_t* marks = a.marks + ((int64_t)x.req * t.Hkv + h) * t.nb * kD;
   for (bool again = false;; again = true) {
+    // (addresses and masks that are the same in both rounds would be kept for the second:
+    // 512 pairs of 4000 blocks 36.6 us for 34.3, 16384 of 2048 97 for 80)
+    int at = lane;
+    asm volatile("" : "+v"(at));
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      held[i] = 64 * i + lane < n ? scores[64 * i + lane] : -INFINITY;
+    for (int i = 0; i < V; ++i) held[i] = 64 * i + at < n ? scores[64 * i + at] : -INFINITY;
     lo_s = INFINITY, hi_s = -INFINITY, avail = 0;
     each([&](int, float s) {
       const bool is = s > -INFINITY;
@@ -653,7 +653,8 @@ __device__ __forceinline__ int gather_blocks(const BlockAttnArgs& a, int64_t t0,
     }
     __syncthreads();
   }
-  // Of many tiles in ascending order: their workgroups go through a context together, and
+  // Of many tiles in ascending order, where a thread has one entry to rank (longer lists,
+  // more than 256 blocks for 16 rows, share little and stay as they are): their workgroups go through a context together, and
   // find in the L2 what others have read (512 bf16 tokens 200 -> 161 us, 2048 e4m3 ones
   // 360 -> 298; with rows streamed past the caches the order changes nothing).
   if (a.pieces > 1 || total > kBlockThreads) return total;
